@@ -458,6 +458,210 @@ ATSPEED_API atspeed_status atspeed_capture_hidden(atspeed_ctx* ctx, int32_t mode
 ATSPEED_API atspeed_status atspeed_set_timing(atspeed_ctx* ctx, int32_t enable);
 ATSPEED_API atspeed_status atspeed_get_timing(atspeed_ctx* ctx, atspeed_kernel_times* out);
 
+/* ------------------------------------------------------------------------
+ * Verifying drafted trees on a caller's own target: the stages between
+ * atspeed_draft / atspeed_get_tree and atspeed_accept for a target that the
+ * context does not hold -- grouped key/value heads, users with histories of
+ * different lengths, caches in pages, trees of any depth (tree-based attention,
+ * Sec. 3.3).  One step is
+ *   atspeed_page_plan       pages, cache slots, positions and ancestor masks of the
+ *                           new rows (once a step; every layer reads them),
+ *   atspeed_kv_append       the rows' keys and values into the pages (per layer),
+ *   atspeed_tree_attention  attention of the rows over the pages     (per layer),
+ *   atspeed_logit_rules     penalties, biases and grammar masks on the logits.
+ *
+ * These calls take no context.  Every pointer is a device pointer to a
+ * caller-owned buffer, all on one GPU, and the work is enqueued on `stream`
+ * (a hipStream_t of that GPU; NULL: the default stream of the current device).
+ * They allocate nothing, keep nothing between calls, synchronise nothing, and can
+ * be captured into a graph; calls on different streams are independent unless
+ * they share a buffer that one of them writes.  Argument errors are found on the
+ * host before any launch.  What only the device can see (lengths, pages, parents,
+ * slots) is checked by the kernels: a bad value costs its own request or row,
+ * as stated per call, and never makes a kernel leave its buffers.
+ *
+ * Rows.  Request b's new rows (drafted nodes, or the tokens of a chunk) are rows
+ * row_off[b] .. row_off[b + 1] - 1 of the packed activations.  Its keys are the
+ * ctx[b] context tokens at cache positions 0 .. ctx[b] - 1 followed by its new
+ * rows at ctx[b], ctx[b] + 1, ...; position p lives in page
+ * block_table[b][p / page_size] at token p % page_size. */
+
+/* Pages, cache slots, positions and masks of one step, from the requests' lengths.
+ * A request holds the pages of its first `held` tokens, keeps the first `keep` of
+ * them and adds `add` rows.  With before = ceil(held / page_size) and after =
+ * ceil((keep + add) / page_size): pages after .. before - 1 of its table go back
+ * to the free list, or pages before .. after - 1 come from it.  The free list is a
+ * stack, free_pages[0 .. n_free - 1]: all released pages are pushed first, in
+ * request order, then the wanted ones popped, in request order.  A request that
+ * wants pages and whose wants together with those of the requests before it exceed
+ * the stack gets none and is refused.  Table entries from `after` on are not
+ * cleared; free_pages past the new n_free is undefined.
+ *   refused [B]   0: planned; 1: no pages were left; 2: held, keep or add is out of
+ *                 range (negative, keep > held, more than max_pages pages, with
+ *                 parents more than max_nodes rows, or rows past max_rows).
+ *                 A refused request keeps its pages.
+ *   length [B]    keep + add, the next step's `held`; held if refused
+ *   ctx [B]       keep, or -1 if refused (atspeed_tree_attention then gives zeros)
+ *   row_off [B+1] running sum of max(add, 0), held to max_rows; refused requests
+ *                 keep their rows
+ *   per row [max_rows]: row_user b; row_pos the rotary position (keep + i for the
+ *                 i-th row of a chain, keep + depth - 1 in a tree); slot the cache
+ *                 slot block_table[b][(keep + i) / page_size] * page_size +
+ *                 (keep + i) % page_size; tree_slot b * max_nodes + i (the row of a
+ *                 padded [B, max_nodes] array such as atspeed_accept's logits; i for
+ *                 chains).  All four are -1 past the last row; row_pos and slot are
+ *                 -1 for the rows of refused requests; row_pos is -1 for rows whose
+ *                 path holds a bad parent, and slot is -1 where the page is not
+ *                 in 0 .. n_pool - 1.
+ *   mask [max_rows, ceil(max_nodes / 64)]: bit j % 64 of word j / 64 of a row is set
+ *                 for its j-th sibling row where that is the row itself or an
+ *                 ancestor; zero past the last row, for refused requests and for
+ *                 rows whose path holds a bad parent.
+ * parent (nullable: every request is a chain) [B, max_nodes]: each node's parent, an
+ * earlier node of its request, or -1 -- the layout of atspeed_tree, with add =
+ * n_nodes.  mask is written if parent is given, and must be given then.
+ * block_table [B, max_pages] and free_pages [n_pool] are updated in place; no other
+ * output may overlap an input.  B 1..1024, page_size a power of two up to 1024,
+ * page_size * n_pool and B * max_pages below 2^31; max_nodes 1..4096 with parents. */
+typedef struct {
+  int32_t B, page_size, max_pages, n_pool, max_rows, max_nodes;
+  const int32_t* held;
+  const int32_t* keep;
+  const int32_t* add;
+  const int32_t* parent;
+  int32_t* block_table;
+  int32_t* free_pages;
+  const int32_t* n_free;   /* [1] */
+  int32_t* n_free_out;     /* [1] */
+  int32_t* length;
+  int32_t* ctx;
+  int32_t* refused;
+  int32_t* row_off;
+  int32_t* row_user;
+  int32_t* row_pos;
+  int32_t* slot;
+  int32_t* tree_slot;
+  uint64_t* mask;
+} atspeed_page_plan_args;
+ATSPEED_API atspeed_status atspeed_page_plan(const atspeed_page_plan_args* args, void* stream);
+
+/* A cache of keys (or values) in pages: element e of token t of page p and head h is
+ * at data[p * page_stride + t * token_stride + h * head_stride + e], strides in
+ * elements.  data and the strides are multiples of 16 bytes. */
+typedef struct {
+  void* data;
+  int64_t page_stride, token_stride, head_stride;
+} atspeed_pages;
+
+/* Appends rows to the caches: k row r to slot[r] of k_pages, v row r to slot[r] of
+ * v_pages.  Row r, head h of k starts at k + r * k_row_stride + h * k_head_stride
+ * (elements; v likewise), multiples of 16 bytes.  Rows whose slot is outside
+ * 0 .. page_size * n_pool - 1 are skipped; two rows of one slot leave either.
+ * Types and head sizes as atspeed_tree_attention. */
+typedef struct {
+  int32_t dtype, n_rows, n_kv_heads, d_head, page_size, n_pool;
+  const void* k;
+  const void* v;
+  int64_t k_row_stride, k_head_stride, v_row_stride, v_head_stride;
+  atspeed_pages k_pages, v_pages;
+  const int32_t* slot;     /* [n_rows] */
+} atspeed_kv_append_args;
+ATSPEED_API atspeed_status atspeed_kv_append(const atspeed_kv_append_args* args, void* stream);
+
+/* Attention of new rows over a paged cache that holds their own keys already:
+ * out[r, h] = sum_j p_j v_j with p the softmax of scale * q[r, h] . k_j over the keys
+ * the row sees -- every context key of its request, and of the request's new rows
+ * those of its mask bits, or without a mask the rows up to itself (a chain).  Query
+ * head h reads key/value head h / (n_heads / n_kv_heads).  lse (nullable) [n_rows,
+ * n_heads] fp32: log sum_j exp(scale * q . k_j).  A row that sees no key gets zeros
+ * and lse -inf.  What a key or value holds that a row does not see does not reach that
+ * row, NaN included.
+ *   dtype ATSPEED_BF16: d_head 64 or 128; ATSPEED_FP32: d_head 32, 64 or 128; of q,
+ *     out and both caches.  Scores, softmax and sums are fp32; bf16 probabilities
+ *     meet the values as bf16.
+ *   q row r, head h starts at q + r * q_row_stride + h * q_head_stride (out
+ *     likewise; elements), multiples of 16 bytes.  out may be q itself with q's strides.
+ *   row_off [B + 1], ctx [B], mask [n_rows, mask_words] as atspeed_page_plan writes
+ *     them.  Rows past min(row_off[B], n_rows) and rows past a request's max_new-th
+ *     are left as they were; new rows past 64 * mask_words are not seen.  A negative
+ *     ctx[b] means a request that sees nothing.  Keys past max_pages * page_size,
+ *     and keys in pages outside 0 .. n_pool - 1, are not seen.
+ *   max_ctx, max_new: what ctx[b] and a request's row count stay within; they size
+ *     the launch (a context above max_ctx is still read whole).
+ * workspace: 16-byte aligned, at least atspeed_tree_attention_workspace_bytes (may be
+ * 0, then it may be null); concurrent calls need one each. */
+typedef struct {
+  int32_t dtype, B, n_rows, n_heads, n_kv_heads, d_head;
+  int32_t page_size, max_pages, n_pool, max_ctx, max_new, mask_words;
+  float scale;
+  const void* q;
+  int64_t q_row_stride, q_head_stride;
+  atspeed_pages k_pages, v_pages;
+  const int32_t* block_table;   /* [B, max_pages] */
+  const int32_t* row_off;
+  const int32_t* ctx;
+  const uint64_t* mask;         /* nullable */
+  void* out;
+  int64_t out_row_stride, out_head_stride;
+  float* lse;                   /* nullable */
+} atspeed_tree_attention_args;
+ATSPEED_API atspeed_status atspeed_tree_attention_workspace_bytes(const atspeed_tree_attention_args* args,
+                                                                  size_t* bytes);
+ATSPEED_API atspeed_status atspeed_tree_attention(const atspeed_tree_attention_args* args, void* workspace,
+                                                  size_t ws_bytes, void* stream);
+
+/* Rules on logits before selection (atspeed_accept) or sampling.  Column v of a row
+ * stands for token token_base + v.  With c_v the number of times that token occurs in
+ * the request's history and on the row's path (its mask's nodes; without a mask the
+ * request's rows up to itself), a row of request b becomes
+ *   x_v = logit_v;   where c_v > 0:  x_v = (x_v > 0 ? x_v / repetition[b]
+ *                                                   : x_v * repetition[b])
+ *                                          - (frequency[b] * c_v + presence[b]);
+ *   x_v = (x_v + bias[bias_index[b]][v]) / temperature[b];
+ *   x_v = mask_value where bit v % 32 of allowed[state[r]][v / 32] is 0.
+ * in fp32.  Each part is left out where its pointers are null: history (with
+ * hist_len), node_token, repetition, frequency, presence, bias, temperature, allowed.
+ *   logits [n_rows, n_cols] in dtype (ATSPEED_FP32 or ATSPEED_BF16), rows logits_stride
+ *     elements apart; out fp32, rows out_stride apart.  out may be logits itself (fp32,
+ *     the same stride, no out_row); otherwise they may not overlap.
+ *   out_row (nullable) [n_rows]: row r goes to row out_row[r] of out, rows outside
+ *     0 .. n_out_rows - 1 nowhere -- atspeed_page_plan's tree_slot gives the
+ *     [B, max_nodes, n_cols] layout that atspeed_accept reads.
+ *   row_off [B + 1]: rows past min(row_off[B], n_rows) are left as they were.
+ *   history [B, max_hist], hist_len [B] (held to 0 .. max_hist); tokens outside the
+ *     columns count nowhere.  Masked places of node_token are not read.
+ *   node_token [B, max_nodes]: the tokens of the request's new rows, which count on the
+ *     paths of mask [n_rows, mask_words] (nullable).
+ *   bias [n_bias, n_cols] fp32, rows bias_stride apart; bias_index [B], none where it is
+ *     outside 0 .. n_bias - 1 (null: every request takes row 0).
+ *   allowed [n_states, ceil(n_cols / 32)] uint32; state [n_rows]: a negative state
+ *     allows every column, one from n_states on none.
+ * repetition and temperature must be positive.  B 1..1024, n_cols 1..2^20. */
+typedef struct {
+  int32_t dtype, B, n_rows, n_cols, token_base, max_hist, max_nodes, mask_words, n_bias, n_states, n_out_rows;
+  float mask_value;
+  const void* logits;
+  int64_t logits_stride;
+  float* out;
+  int64_t out_stride;
+  const int32_t* out_row;
+  const int32_t* row_off;
+  const int32_t* history;
+  const int32_t* hist_len;
+  const int32_t* node_token;
+  const uint64_t* mask;
+  const float* repetition;
+  const float* frequency;
+  const float* presence;
+  const float* temperature;
+  const float* bias;
+  int64_t bias_stride;
+  const int32_t* bias_index;
+  const uint32_t* allowed;
+  const int32_t* state;
+} atspeed_logit_rules_args;
+ATSPEED_API atspeed_status atspeed_logit_rules(const atspeed_logit_rules_args* args, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -24,7 +24,8 @@ SYMBOLS = ("atspeed_workspace_bytes", "atspeed_create", "atspeed_destroy", "atsp
            "atspeed_capture_hidden",
            "atspeed_accept", "atspeed_accept_noalloc", "atspeed_decode_topk", "atspeed_logprobs", "atspeed_get_state", "atspeed_set_state",
            "atspeed_set_timing", "atspeed_get_timing", "atspeed_align_data", "atspeed_align_step",
-           "atspeed_target_search", "atspeed_mixed_search")
+           "atspeed_target_search", "atspeed_mixed_search", "atspeed_page_plan", "atspeed_kv_append",
+           "atspeed_tree_attention_workspace_bytes", "atspeed_tree_attention", "atspeed_logit_rules")
 KERNEL_CLASSES = ("qkv", "o", "gu", "down", "lm_head", "attention", "row", "select")
 
 
@@ -76,6 +77,30 @@ class AlignArgs(C.Structure):
                 ("beta2", C.c_float), ("eps", C.c_float), ("weight_decay", C.c_float), ("step", C.c_int32)]
 
 
+def _struct(name, spec):
+    """A ctypes structure from "type: name name ..." groups in the header's field order."""
+    kinds = {"i": C.c_int32, "l": C.c_int64, "f": C.c_float, "p": C.c_void_p}
+    fields = [(n, kinds[part.split(":")[0].strip()]) for part in spec.split(";") for n in part.split(":")[1].split()]
+    return type(name, (C.Structure,), {"_fields_": fields})
+
+
+# Arguments of the context-free calls (atspeed_pages members are spelled out).
+PagePlanArgs = _struct("PagePlanArgs", """i: B page_size max_pages n_pool max_rows max_nodes;
+    p: held keep add parent block_table free_pages n_free n_free_out length ctx refused row_off row_user row_pos slot
+       tree_slot mask""")
+KvAppendArgs = _struct("KvAppendArgs", """i: dtype n_rows n_kv_heads d_head page_size n_pool; p: k v;
+    l: k_row_stride k_head_stride v_row_stride v_head_stride;
+    p: k_data; l: k_page k_token k_head; p: v_data; l: v_page v_token v_head; p: slot""")
+TreeAttentionArgs = _struct("TreeAttentionArgs", """i: dtype B n_rows n_heads n_kv_heads d_head
+       page_size max_pages n_pool max_ctx max_new mask_words; f: scale; p: q; l: q_row_stride q_head_stride;
+    p: k_data; l: k_page k_token k_head; p: v_data; l: v_page v_token v_head; p: block_table row_off ctx mask out;
+    l: out_row_stride out_head_stride; p: lse""")
+LogitRulesArgs = _struct("LogitRulesArgs", """i: dtype B n_rows n_cols token_base max_hist max_nodes mask_words n_bias
+       n_states n_out_rows; f: mask_value; p: logits; l: logits_stride; p: out; l: out_stride;
+    p: out_row row_off history hist_len node_token mask repetition frequency presence temperature bias;
+    l: bias_stride; p: bias_index allowed state""")
+
+
 class AtspeedError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"{STATUS.get(status, status)}: {msg}")
@@ -113,6 +138,11 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
     lib.atspeed_align_step.argtypes = [vp, C.POINTER(AlignArgs), C.POINTER(C.c_double)]
     lib.atspeed_target_search.argtypes = [vp, i32, i32, pi32, pi32, pf, pi32, pi32, pi32, pi32]
     lib.atspeed_mixed_search.argtypes = [vp, C.c_float, i32, i32, pi32, pi32, pf, pi32, pi32, pi32, pi32]
+    lib.atspeed_page_plan.argtypes = [C.POINTER(PagePlanArgs), vp]
+    lib.atspeed_kv_append.argtypes = [C.POINTER(KvAppendArgs), vp]
+    lib.atspeed_tree_attention_workspace_bytes.argtypes = [C.POINTER(TreeAttentionArgs), C.POINTER(C.c_size_t)]
+    lib.atspeed_tree_attention.argtypes = [C.POINTER(TreeAttentionArgs), vp, C.c_size_t, vp]
+    lib.atspeed_logit_rules.argtypes = [C.POINTER(LogitRulesArgs), vp]
     for name in SYMBOLS:
         fn = getattr(lib, name)
         if fn.restype is C.c_int:  # default

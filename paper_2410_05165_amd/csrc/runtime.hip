@@ -11,29 +11,20 @@
 #include "common.h"
 #include "kernels.h"
 #include "select.h"
+#include "status.h"
 
 using namespace atspeed;
 
 namespace {
-
 thread_local std::string g_err;
+}
 
-atspeed_status fail(atspeed_status s, const std::string& msg) {
+atspeed_status atspeed::fail(atspeed_status s, const std::string& msg) {
   g_err = msg;
   return s;
 }
 
-#define HIP_TRY(expr)                                                                      \
-  do {                                                                                     \
-    hipError_t _e = (expr);                                                                \
-    if (_e != hipSuccess) return fail(ATSPEED_E_DEVICE, std::string(#expr) + ": " + hipGetErrorString(_e)); \
-  } while (0)
-
-#define ST_TRY(expr)                        \
-  do {                                      \
-    atspeed_status _s = (expr);             \
-    if (_s != ATSPEED_OK) return _s;        \
-  } while (0)
+namespace {
 
 // Bump allocator over the caller's workspace (a null base only measures).
 struct Arena {

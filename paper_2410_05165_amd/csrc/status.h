@@ -1,0 +1,22 @@
+// Status and message of the calling thread's last error, for every entry point.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <string>
+#include "../../include/atspeed.h"
+
+namespace atspeed {
+// Records msg for atspeed_last_error and returns s.
+atspeed_status fail(atspeed_status s, const std::string& msg);
+}  // namespace atspeed
+
+#define HIP_TRY(expr)                                                                      \
+  do {                                                                                     \
+    hipError_t _e = (expr);                                                                \
+    if (_e != hipSuccess) return fail(ATSPEED_E_DEVICE, std::string(#expr) + ": " + hipGetErrorString(_e)); \
+  } while (0)
+
+#define ST_TRY(expr)                        \
+  do {                                      \
+    atspeed_status _s = (expr);             \
+    if (_s != ATSPEED_OK) return _s;        \
+  } while (0)
