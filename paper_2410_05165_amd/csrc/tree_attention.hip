@@ -10,7 +10,11 @@ namespace atspeed {
 struct TreeAttnArgs {
   const char* q;
   int64_t q_row, q_head;       // bytes
-  PagesDev k, v;
+  const char* k;
+  const char* v;
+  int64_t k_head, v_head;      // bytes
+  // where a token's row starts, in units of `unit` bytes: page * *_page + token * *_token
+  uint32_t k_page, k_token, v_page, v_token, unit;
   const int* table;
   const int* row_off;
   const int* ctx;
@@ -31,226 +35,206 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 8.f;  // a maximum moves when a score passes it by 2^8
 
 typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4_t;
+typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4_t;
 typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
-
-// Keys of a request as the rows of one query tile see them.
-struct KeySpan {
-  int64_t ctx;      // context keys (0 where the request sees nothing)
-  int64_t total;    // keys of the request: what the splits divide
-};
-__device__ __forceinline__ KeySpan key_span(const TreeAttnArgs& a, int b, int count) {
-  const int64_t ctx = a.ctx[b];
-  if (ctx < 0) return {0, 0};
-  const int64_t cap = (int64_t)a.max_pages << a.shift;
-  return {ctx < cap ? ctx : cap, min(ctx + (a.mask ? min((int64_t)count, (int64_t)a.words * 64) : (int64_t)count), cap)};
-}
-
-// Bits kk of a 64-key tile at k0 that the row sees: context keys, then its mask words
-// (or the keys up to its own, at ctx + i).
-__device__ __forceinline__ uint64_t tile_bits(const uint64_t* words, int n_words, int64_t ctx, int i, int64_t k0) {
-  const int64_t j0 = k0 - ctx;
-  if (!words) {
-    const int64_t n = i + 1 - j0;
-    return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1;
-  }
-  if (j0 <= -64) return ~0ull;
-  if (j0 < 0) return (words[0] << -j0) | ((1ull << -j0) - 1);
-  const int64_t w = j0 >> 6;
-  const int sh = (int)(j0 & 63);
-  const uint64_t lo = w < n_words ? words[w] >> sh : 0ull;
-  const uint64_t hi = sh && w + 1 < n_words ? words[w + 1] << (64 - sh) : 0ull;
-  return lo | hi;
-}
+typedef __attribute__((address_space(3))) void lds_void_t;
 
 // Pieces of a request's keys; the last one takes what a context above max_ctx holds more.
 __device__ __forceinline__ int split_count(const TreeAttnArgs& a, int64_t total) {
   return total <= a.chunk ? 1 : (int)min((total + a.chunk - 1) / a.chunk, (int64_t)a.splits);
 }
 
-template <class T, int DH, int NQ, int WQ, int KW>
-__global__ void __launch_bounds__(256)
-tree_attn_kernel(TreeAttnArgs a) {
-  constexpr bool BF = sizeof(T) == 2;
-  constexpr int WK = 4 / WQ;                    // key groups
-  constexpr int TG = 64 * WQ;                   // threads of a key group
-  constexpr int ROWB = DH * (int)sizeof(T);     // bytes of a row
-  constexpr int CPR = ROWB / 16;                // 16-byte chunks of a row
-  constexpr int NKS = CPR / 4;                  // chunk groups of a score
-  constexpr int NDB = DH / 16;                  // 16-dim blocks of the output
-  constexpr int NKB = KW / 16;                  // 16-key blocks of a tile
-  constexpr int NCH = KW * CPR / TG;            // chunks of K (and of V) a thread stages
-  constexpr int QB = 16 * NQ * WQ;              // queries of a workgroup
-  constexpr int TILE = KW * ROWB;
-  constexpr int JOIN = WK > 1 ? 4 * NDB * 64 * 16 : 0;
-  constexpr int LDS = WK * 2 * TILE > JOIN ? WK * 2 * TILE : JOIN;
-  __shared__ __align__(16) char lds[LDS];
-  __shared__ float2 ml_s[4][16];
-  auto kswz = [](int key) { return BF ? key & (CPR - 1) : CPR >= 16 ? key & 15 : (key >> 1) & 7; };
-  auto vswz = [](int key) {
+// One workgroup's share: a request, a key/value head, a tile of its queries (row i, head
+// h of the group: query i * G + h), a range of its keys.
+struct Share {
+  int kvh, r0, nq, q0, split, nsplit;
+  int64_t ctx, kbeg, kend;   // context keys; this workgroup's keys
+  int64_t clear;             // from this key on some query may not see a key
+  const int* table;
+
+  // False where there is nothing to do.  QB queries a tile.
+  __device__ __forceinline__ bool init(const TreeAttnArgs& a, int QB) {
+    // Workgroup L runs on XCD L % 8: the tiles and splits of one pair stay on one
+    // XCD, whose L2 then holds the pair's keys; the pairs are dealt round-robin.
+    const int L = blockIdx.x, Z = a.qtiles * a.splits;
+    const int pair = ((L >> 3) / Z) * 8 + (L & 7), z = (L >> 3) % Z;
+    if (pair >= a.B * a.KH) return false;
+    const int b = pair / a.KH;
+    kvh = pair % a.KH;
+    split = z / a.qtiles;
+    // chains: the tiles with the most keys first
+    const int qt = a.mask ? z % a.qtiles : a.qtiles - 1 - z % a.qtiles;
+    r0 = a.row_off[b];
+    const int count = a.row_off[b + 1] - r0;
+    nq = min(min(count, a.n_rows - r0), a.max_new) * a.G;
+    q0 = qt * QB;
+    if (q0 >= nq) return false;
+    const int64_t total = keys(a, b, count);
+    nsplit = split_count(a, total);
+    if (split >= nsplit) return false;
+    kbeg = split * a.chunk;
+    kend = split + 1 < nsplit ? kbeg + a.chunk : total;
+    if (!a.mask) kend = min(kend, ctx + (min(q0 + QB, nq) - 1) / a.G + 1);
+    clear = a.mask ? ctx : ctx + q0 / a.G + 1;
+    table = a.table + (int64_t)b * a.max_pages;
+    return true;
+  }
+  // Keys of request b with `count` new rows (none where ctx is negative); sets ctx.
+  __device__ __forceinline__ int64_t keys(const TreeAttnArgs& a, int b, int count) {
+    const int64_t cap = (int64_t)a.max_pages << a.shift, c = a.ctx[b];
+    ctx = c < 0 ? 0 : min(c, cap);
+    return c < 0 ? 0 : min(c + (a.mask ? min((int64_t)count, (int64_t)a.words * 64) : (int64_t)count), cap);
+  }
+  // Page of key k0 + lane for the first n lanes, -1 where the key is not there.
+  __device__ __forceinline__ int page(const TreeAttnArgs& a, int64_t k0, int n) const {
+    const int lane = threadIdx.x & 63;
+    const int64_t key = k0 + lane;
+    return lane < n && key < kend ? table[key >> a.shift] : -1;
+  }
+};
+
+// Rows of keys and values of one tile: lane i holds key i's.
+struct TileRows {
+  uint32_t k, v;     // units; a readable row where the key is not there
+  uint64_t there;    // bit i: key i is there
+  __device__ __forceinline__ void set(const TreeAttnArgs& a, int64_t k0, int page) {
+    const bool ok = (unsigned)page < (unsigned)a.n_pool;
+    const uint32_t pg = ok ? page : 0, tok = (uint32_t)(k0 + (threadIdx.x & 63)) & a.tail;
+    k = pg * a.k_page + tok * a.k_token;
+    v = pg * a.v_page + tok * a.v_token;
+    there = __ballot(ok);
+  }
+};
+
+// The mask words that hold bits j0 .. j0 + 63 of a row, and those bits.  Context keys
+// (j < 0) are always seen, bits past the words never.
+struct MaskWords {
+  uint64_t lo, hi;
+  __device__ __forceinline__ void load(const uint64_t* words, int n, int64_t j0) {
+    const int64_t w = j0 < 0 ? 0 : j0 >> 6;
+    lo = j0 > -64 && w < n ? words[w] : 0ull;
+    hi = j0 > 0 && (j0 & 63) && w + 1 < n ? words[w + 1] : 0ull;
+  }
+  __device__ __forceinline__ uint64_t bits(int64_t j0) const {
+    if (j0 <= -64) return ~0ull;
+    if (j0 < 0) return (lo << -j0) | ((1ull << -j0) - 1);
+    const int s = (int)(j0 & 63);
+    return s ? (lo >> s) | (hi << (64 - s)) : lo;
+  }
+};
+// Without a mask: the keys up to the row's own, at ctx + i.
+__device__ __forceinline__ uint64_t chain_bits(int i, int64_t j0) {
+  const int64_t n = i + 1 - j0;
+  return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1;
+}
+
+// A wave's arithmetic on NQ blocks of 16 queries and a tile of KW keys whose K and V
+// rows lie in LDS.  S^T = K Q^T (v_mfma 16x16, A = K rows, B = Q): lane l holds the
+// scores of query l % 16 with keys 4g .. 4g + 3 (g = l / 16) of each 16-key block, which
+// is the B operand of O^T = V^T P^T, so probabilities stay in registers.  bf16: V^T's
+// fragments come from a transposing LDS read (4 keys x 16 dims per 16 lanes) and the 32
+// keys of a step are ordered {4g .. 4g + 3, 16 + 4g .. 16 + 4g + 3} on both operands;
+// fp32: MFMA e of a block takes keys {e, 4 + e, 8 + e, 12 + e}.  Softmax in fp32 with a
+// running maximum that moves only when a score passes it by 2^8 (probabilities up to
+// 2^8 keep their relative precision, and the exchange between the lanes of a query and
+// the rescaling are rare); lsum is each lane's own part until the end.  bf16
+// probabilities are rounded to bf16 for the product with V, as V itself is held: 2^-9
+// of each, about the rounding of the output; the sum takes them unrounded.
+template <class T, int DH, int NQ, int KW>
+struct Tile {
+  static constexpr bool BF = sizeof(T) == 2;
+  static constexpr int ROWB = DH * (int)sizeof(T);   // bytes of a row
+  static constexpr int CPR = ROWB / 16;              // 16-byte chunks of a row
+  static constexpr int NKS = CPR / 4;                // chunk groups of a score
+  static constexpr int NDB = DH / 16;                // 16-dim blocks of the output
+  static constexpr int NKB = KW / 16;                // 16-key blocks of the tile
+  static constexpr int BYTES = KW * ROWB;            // of K, and of V
+  static constexpr uint64_t ALL = KW == 64 ? ~0ull : (1ull << KW) - 1;
+
+  // Chunk swizzles: K fragments are read 16 rows at one chunk; V (bf16) 8 rows at one
+  // 16-dim block (two chunks), (fp32) 4 rows, 4 apart, at one 16-dim block.
+  static __device__ __forceinline__ int kswz(int key) { return BF ? key & (CPR - 1) : CPR >= 16 ? key & 15 : (key >> 1) & 7; }
+  static __device__ __forceinline__ int vswz(int key) {
     return BF ? (DH == 128 ? key & 7 : (key >> 1) & 3) << 1 : ((key >> 2) & (NDB >= 4 ? 3 : 1)) << 2;
-  };
+  }
 
-  const int Lw = blockIdx.x, xcd = Lw & 7, rest = Lw >> 3, Z = a.qtiles * a.splits;
-  const int pair = (rest / Z) * 8 + xcd, z = rest % Z;
-  if (pair >= a.B * a.KH) return;
-  const int b = pair / a.KH, kvh = pair % a.KH;
-  const int split = z / a.qtiles, qt = a.mask ? z % a.qtiles : a.qtiles - 1 - z % a.qtiles;   // chains: longest first
-  const int r0 = a.row_off[b], count = a.row_off[b + 1] - r0;
-  const int nr = min(min(count, a.n_rows - r0), a.max_new);
-  const int nq = nr * a.G, q0 = qt * QB;
-  if (q0 >= nq) return;
-  const KeySpan span = key_span(a, b, count);
-  const int nsplit = split_count(a, span.total);
-  if (split >= nsplit) return;
-
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wq = wave % WQ, wk = wave / WQ, gt = wq * 64 + lane;
-  const int g = lane >> 4, ql = lane & 15;
-  char* ks = lds + wk * 2 * TILE;
-  char* vs = ks + TILE;
-
-  // this lane's queries, one per 16-query block
-  int qi[NQ];           // new-row index
+  int g, ql;
+  int qi[NQ], qhead[NQ];     // the lane's queries: new-row index, head
   int64_t qrow[NQ];
-  int qhead[NQ];
   bool qok[NQ];
   f32x4_t qf[NQ][NKS];
-#pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    const int c = q0 + (wq * NQ + n) * 16 + ql;
-    qok[n] = c < nq;
-    const int cc = qok[n] ? c : nq - 1;
-    qi[n] = cc / a.G;
-    qrow[n] = r0 + qi[n];
-    qhead[n] = kvh * a.G + cc % a.G;
-    const char* p = a.q + qrow[n] * a.q_row + qhead[n] * a.q_head + g * 16;
-#pragma unroll
-    for (int s = 0; s < NKS; ++s) {
-      u32x4_t w = *reinterpret_cast<const u32x4_t*>(p + s * 64);
-      w ^= a.q_flip;
-      qf[n][s] = __builtin_bit_cast(f32x4_t, w);
-    }
-  }
-  const int i_first = (q0 + wq * NQ * 16 < nq ? q0 + wq * NQ * 16 : nq - 1) / a.G;   // first row of the wave
-  const int i_last = (min(q0 + QB, nq) - 1) / a.G;                                    // last row of the workgroup
-  const int64_t kbeg = split * a.chunk;
-  int64_t kend = split + 1 < nsplit ? kbeg + a.chunk : span.total;
-  if (!a.mask) kend = min(kend, span.ctx + i_last + 1);
-  // from this key on some query of the workgroup may not see a key
-  const int64_t clear = a.mask ? span.ctx : span.ctx + q0 / a.G + 1;
-  const int nit = kend > kbeg ? (int)((kend - kbeg + WK * KW - 1) / (WK * KW)) : 0;
-  const int* table = a.table + (int64_t)b * a.max_pages;
-
-  auto key0 = [&](int it) { return kbeg + (int64_t)(it * WK + wk) * KW; };
-  // page of key k0 + lane, -1 where there is none
-  auto load_page = [&](int it) {
-    const int64_t key = key0(it) + lane;
-    int pg = -1;
-    if (lane < KW && key < kend) pg = table[key >> a.shift];
-    return pg;
-  };
-  u32x4_t kreg[NCH], vreg[NCH];
-  auto fetch = [&](int it, int pg) {
-    const int64_t k0 = key0(it);
-#pragma unroll
-    for (int c = 0; c < NCH; ++c) {
-      const int idx = gt + c * TG, key = idx / CPR, j = idx % CPR;
-      const int page = __shfl(pg, key);
-      const int64_t tok = (k0 + key) & a.tail;
-      kreg[c] = vreg[c] = u32x4_t{0u, 0u, 0u, 0u};
-      if ((unsigned)page < (unsigned)a.n_pool) {
-        kreg[c] = *reinterpret_cast<const u32x4_t*>(a.k.data + page * a.k.page + tok * a.k.token + kvh * a.k.head + j * 16);
-        vreg[c] = *reinterpret_cast<const u32x4_t*>(a.v.data + page * a.v.page + tok * a.v.token + kvh * a.v.head + j * 16);
-      }
-    }
-  };
-
   f32x4_t o[NQ][NDB];
   float m[NQ], lsum[NQ];
-#pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    m[n] = -INFINITY;
-    lsum[n] = 0.f;
-#pragma unroll
-    for (int d = 0; d < NDB; ++d) o[n][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  }
-  bool bad = false;                    // a value that not every query sees is not finite
-  const uint64_t whole = KW == 64 ? ~0ull : (1ull << KW) - 1;
-  int pg = load_page(0);
-  uint64_t vm = __ballot((unsigned)pg < (unsigned)a.n_pool);
-  if (nit > 0) fetch(0, pg);
-  pg = load_page(1);
 
-  for (int it = 0; it < nit; ++it) {
-    const int64_t k0 = key0(it);
-    const bool partial = k0 + KW > clear;
-    if (partial) {
-      // 0 times a value that is not finite is not 0: such values are left out of the
-      // product and reach the rows that see them below
+  // first: the wave's first query.
+  __device__ __forceinline__ void init(const TreeAttnArgs& a, const Share& s, int first) {
+    const int lane = threadIdx.x & 63;
+    g = lane >> 4;
+    ql = lane & 15;
 #pragma unroll
-      for (int c = 0; c < NCH; ++c) {
+    for (int n = 0; n < NQ; ++n) {
+      const int c = first + n * 16 + ql;
+      qok[n] = c < s.nq;
+      const int cc = qok[n] ? c : s.nq - 1;
+      qi[n] = cc / a.G;
+      qrow[n] = s.r0 + qi[n];
+      qhead[n] = s.kvh * a.G + cc % a.G;
+      const char* p = a.q + qrow[n] * a.q_row + qhead[n] * a.q_head + g * 16;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t w = vreg[c][e];
-          if constexpr (BF) {
-            if ((w & 0x7f800000u) == 0x7f800000u) { vreg[c][e] &= 0x0000ffffu; bad = true; }
-            if ((w & 0x00007f80u) == 0x00007f80u) { vreg[c][e] &= 0xffff0000u; bad = true; }
-          } else {
-            if ((w & 0x7f800000u) == 0x7f800000u) { vreg[c][e] = 0u; bad = true; }
-          }
-        }
+      for (int k = 0; k < NKS; ++k) {
+        u32x4_t w = *reinterpret_cast<const u32x4_t*>(p + k * 64);
+        w ^= a.q_flip;
+        qf[n][k] = __builtin_bit_cast(f32x4_t, w);
       }
-    }
+      m[n] = -INFINITY;
+      lsum[n] = 0.f;
 #pragma unroll
-    for (int c = 0; c < NCH; ++c) {
-      const int idx = gt + c * TG, key = idx / CPR, j = idx % CPR;
-      *reinterpret_cast<u32x4_t*>(ks + key * ROWB + (j ^ kswz(key)) * 16) = kreg[c];
-      *reinterpret_cast<u32x4_t*>(vs + key * ROWB + (j ^ vswz(key)) * 16) = vreg[c];
+      for (int d = 0; d < NDB; ++d) o[n][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
-    if (WQ > 1) __syncthreads();
-    const uint64_t tile_vm = vm;
-    if (it + 1 < nit) {
-      vm = __ballot((unsigned)pg < (unsigned)a.n_pool);
-      fetch(it + 1, pg);
-      pg = load_page(it + 2);
-    }
-    // scores
+  }
+
+  // bits: the keys each query sees, if not `full` (all of them).
+  __device__ __forceinline__ void step(const TreeAttnArgs& a, const char* ks, const char* vs, bool full,
+                                       const uint64_t (&bits)[NQ]) {
     f32x4_t sc[NQ][NKB];
 #pragma unroll
-    for (int kb = 0; kb < NKB; ++kb) {
-      const int key = kb * 16 + ql;
+    for (int n = 0; n < NQ; ++n)
 #pragma unroll
-      for (int n = 0; n < NQ; ++n) sc[n][kb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      for (int kb = 0; kb < NKB; ++kb) sc[n][kb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int s = 0; s < NKS; ++s) {
-        const f32x4_t kf = *reinterpret_cast<const f32x4_t*>(ks + key * ROWB + ((s * 4 + g) ^ kswz(key)) * 16);
+    for (int k = 0; k < NKS; ++k) {
+#pragma unroll
+      for (int kb = 0; kb < NKB; ++kb) {
+        const int key = kb * 16 + ql;
+        const f32x4_t kf = *reinterpret_cast<const f32x4_t*>(ks + key * ROWB + ((k * 4 + g) ^ kswz(key)) * 16);
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
           if constexpr (BF) {
             sc[n][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf),
-                                                                 __builtin_bit_cast(bf16x8_t, qf[n][s]), sc[n][kb], 0, 0, 0);
+                                                                 __builtin_bit_cast(bf16x8_t, qf[n][k]), sc[n][kb], 0, 0, 0);
           } else {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              sc[n][kb] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[n][s][e], sc[n][kb], 0, 0, 0);
+              sc[n][kb] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[n][k][e], sc[n][kb], 0, 0, 0);
           }
         }
       }
     }
-    const bool full = tile_vm == whole && (k0 + KW <= span.ctx || (!a.mask && k0 + KW <= span.ctx + i_first + 1));
-    float mx[NQ];
-    bool moved = false;
+    if (!full) {
 #pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-      if (!full) {
-        const uint64_t bits =
-            tile_vm & tile_bits(a.mask ? a.mask + qrow[n] * a.words : nullptr, a.words, span.ctx, qi[n], k0);
+      for (int n = 0; n < NQ; ++n) {
+        const uint64_t mine = bits[n] >> (g * 4);
 #pragma unroll
         for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (!((bits >> (kb * 16 + g * 4 + i)) & 1)) sc[n][kb][i] = -INFINITY;
+            if (!((mine >> (kb * 16 + i)) & 1)) sc[n][kb][i] = -INFINITY;
       }
+    }
+    float mx[NQ];
+    bool moved = false;
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
       float x = sc[n][0][0];
 #pragma unroll
       for (int kb = 0; kb < NKB; ++kb)
@@ -274,7 +258,7 @@ tree_attn_kernel(TreeAttnArgs a) {
     }
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
-      const float ref = m[n] != -INFINITY ? m[n] : 0.f;
+      const float ref = m[n] != -INFINITY ? m[n] : 0.f;   // a query that has seen nothing yet
       float ps = 0.f;
 #pragma unroll
       for (int kb = 0; kb < NKB; ++kb)
@@ -286,7 +270,6 @@ tree_attn_kernel(TreeAttnArgs a) {
         }
       lsum[n] += ps;
     }
-    // values
     if constexpr (BF) {
 #pragma unroll
       for (int kk = 0; kk < KW / 32; ++kk) {
@@ -302,8 +285,8 @@ tree_attn_kernel(TreeAttnArgs a) {
 #pragma unroll
         for (int d = 0; d < NDB; ++d) {
           const int j = d * 2 + ((ql >> 1) & 1);
-          char* v0 = vs + key * ROWB + ((j ^ vswz(key)) << 4) + (ql & 1) * 8;
-          char* v1 = vs + (key + 16) * ROWB + ((j ^ vswz(key + 16)) << 4) + (ql & 1) * 8;
+          const char* v0 = vs + key * ROWB + ((j ^ vswz(key)) << 4) + (ql & 1) * 8;
+          const char* v1 = vs + (key + 16) * ROWB + ((j ^ vswz(key + 16)) << 4) + (ql & 1) * 8;
           const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)v0);
           const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)v1);
           const auto w8 = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -327,48 +310,77 @@ tree_attn_kernel(TreeAttnArgs a) {
           }
         }
     }
-    if (WQ > 1) __syncthreads();
   }
 
-  if (__syncthreads_or(bad) && wk == 0) {
-    // p is positive where the row sees the key, so such a value is what it adds
-    for (int64_t key = max(kbeg, clear - KW); key < kend; ++key) {
-      const int page = table[key >> a.shift];
+  // Chunk w of V without its values that are not finite; true if there were any.  0
+  // times such a value is not 0, so in tiles that not every query sees whole they are
+  // left out of the product.
+  static __device__ __forceinline__ bool finite(u32x4_t& w) {
+    bool bad = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (BF) {
+        if ((w[e] & 0x7f800000u) == 0x7f800000u) { w[e] &= 0x0000ffffu; bad = true; }
+        if ((w[e] & 0x00007f80u) == 0x00007f80u) { w[e] &= 0xffff0000u; bad = true; }
+      } else {
+        if ((w[e] & 0x7f800000u) == 0x7f800000u) { w[e] = 0u; bad = true; }
+      }
+    }
+    return bad;
+  }
+  // ... and here they reach the rows that see them: p is positive there, so they are
+  // what they add.
+  __device__ __forceinline__ void add_not_finite(const TreeAttnArgs& a, const Share& s) {
+    for (int64_t key = s.kbeg; key < s.kend; ++key) {
+      const int page = s.table[key >> a.shift];
       if ((unsigned)page >= (unsigned)a.n_pool) continue;
-      const char* vp = a.v.data + page * a.v.page + (key & a.tail) * a.v.token + kvh * a.v.head;
+      const uint32_t row = page * a.v_page + ((uint32_t)key & a.tail) * a.v_token;
+      const T* vp = reinterpret_cast<const T*>(a.v + (uint64_t)row * a.unit + s.kvh * a.v_head);
 #pragma unroll
       for (int n = 0; n < NQ; ++n) {
-        if (!(tile_bits(a.mask ? a.mask + qrow[n] * a.words : nullptr, a.words, span.ctx, qi[n], key) & 1)) continue;
+        const int64_t j0 = key - s.ctx;
+        uint64_t bits;
+        if (a.mask) {
+          MaskWords w;
+          w.load(a.mask + qrow[n] * a.words, a.words, j0);
+          bits = w.bits(j0);
+        } else {
+          bits = chain_bits(qi[n], j0);
+        }
+        if (!(bits & 1)) continue;
 #pragma unroll
         for (int d = 0; d < NDB; ++d)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float v = St<T>::ld(reinterpret_cast<const T*>(vp) + d * 16 + g * 4 + e);
+            const float v = St<T>::ld(vp + d * 16 + g * 4 + e);
             if (!(fabsf(v) < INFINITY)) o[n][d][e] += v;
           }
       }
     }
   }
-#pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    lsum[n] += __shfl_xor(lsum[n], 16);
-    lsum[n] += __shfl_xor(lsum[n], 32);
-  }
 
-  // dims d * 16 + 4 g .. + 3 of one query: the result, or this split's part of it
-  auto put = [&](int n, int d, f32x4_t x, float mm, float ll) {
+  __device__ __forceinline__ void sum_lanes() {
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      lsum[n] += __shfl_xor(lsum[n], 16);
+      lsum[n] += __shfl_xor(lsum[n], 32);
+    }
+  }
+  // Dims d * 16 + 4g .. + 3 of query block n: the result, or this split's part of it.
+  __device__ __forceinline__ void put(const TreeAttnArgs& a, const Share& s, int n, int d, f32x4_t x, float mm,
+                                      float ll) const {
     if (!qok[n]) return;
-    if (nsplit > 1) {
-      const int64_t at = (split * (int64_t)a.n_rows + qrow[n]) * a.H + qhead[n];
-      *reinterpret_cast<f32x4_t*>(a.part + at * DH + d * 16 + g * 4) = x;
-      if (d == 0 && g == 0) a.part_ml[at] = float2{mm, ll};
+    const int64_t at = qrow[n] * a.H + qhead[n];
+    if (s.nsplit > 1) {
+      const int64_t pt = s.split * (int64_t)a.n_rows * a.H + at;
+      *reinterpret_cast<f32x4_t*>(a.part + pt * DH + d * 16 + g * 4) = x;
+      if (d == 0 && g == 0) a.part_ml[pt] = float2{mm, ll};
       return;
     }
-    const float inv = ll > 0.f || ll != ll ? 1.f / ll : 0.f;
-    x *= inv;
+    const bool some = ll > 0.f || ll != ll;
+    x *= some ? 1.f / ll : 0.f;
     char* p = a.out + qrow[n] * a.o_row + qhead[n] * a.o_head + (d * 16 + g * 4) * (int)sizeof(T);
     if constexpr (BF) {
-      typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4_t;
       bf16x4_t w;
 #pragma unroll
       for (int e = 0; e < 4; ++e) w[e] = (__bf16)x[e];
@@ -376,44 +388,215 @@ tree_attn_kernel(TreeAttnArgs a) {
     } else {
       *reinterpret_cast<f32x4_t*>(p) = x;
     }
-    if (a.lse && d == 0 && g == 0)
-      a.lse[qrow[n] * a.H + qhead[n]] = ll > 0.f || ll != ll ? (mm + __log2f(ll)) * kLn2 : -INFINITY;
+    if (a.lse && d == 0 && g == 0) a.lse[at] = some ? (mm + __log2f(ll)) * kLn2 : -INFINITY;
+  }
+};
+
+// ---------------------------------------------------------------- few queries
+// Up to 16 NQ queries a workgroup, all of them in each of its four waves; the waves take
+// key tiles of their own in turn, staged through registers into a part of LDS that only
+// they use, so there is no barrier until the four results are joined.  Bound by the reads
+// of the cache: two workgroups of a CU hold 128 KB of rows in flight.
+template <class T, int DH, int NQ>
+__global__ void __launch_bounds__(256, 2) tree_attn_stream_kernel(TreeAttnArgs a) {
+  constexpr int KW = sizeof(T) == 2 ? 32 : 16;
+  typedef Tile<T, DH, NQ, KW> Tl;
+  constexpr int CPR = Tl::CPR, ROWB = Tl::ROWB, NDB = Tl::NDB, NCH = KW * CPR / 64;
+  __shared__ __align__(16) char lds[4 * 2 * Tl::BYTES];
+  __shared__ float2 ml_s[4][16];
+  static_assert(4 * NDB * 64 * 16 <= 4 * 2 * Tl::BYTES, "the join fits the tiles");
+  Share s;
+  if (!s.init(a, 16 * NQ)) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  char* ks = lds + wave * 2 * Tl::BYTES;
+  char* vs = ks + Tl::BYTES;
+  const int64_t first = s.kbeg + wave * KW;
+  int pg = s.page(a, first, KW);
+  TileRows rows;
+  u32x4_t kreg[NCH], vreg[NCH];
+  auto fetch = [&]() {
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) {
+      const int key = (c * 64 + lane) / CPR, j = (c * 64 + lane) % CPR;
+      kreg[c] = *reinterpret_cast<const u32x4_t*>(a.k + s.kvh * a.k_head + j * 16 + (uint64_t)__shfl(rows.k, key) * a.unit);
+      vreg[c] = *reinterpret_cast<const u32x4_t*>(a.v + s.kvh * a.v_head + j * 16 + (uint64_t)__shfl(rows.v, key) * a.unit);
+    }
   };
-  if constexpr (WK == 1) {
+  rows.set(a, first, pg);
+  if (first < s.kend) fetch();
+  pg = s.page(a, first + 4 * KW, KW);
+  Tl t;
+  t.init(a, s, s.q0);
+  const int i_first = s.q0 / a.G;
+  bool bad = false;
+
+  for (int64_t k0 = first; k0 < s.kend; k0 += 4 * KW) {
+    const uint64_t there = rows.there;
+    if (there != Tl::ALL || k0 + KW > s.clear) {
 #pragma unroll
-    for (int n = 0; n < NQ; ++n)
+      for (int c = 0; c < NCH; ++c) bad |= Tl::finite(vreg[c]);
+    }
 #pragma unroll
-      for (int d = 0; d < NDB; ++d) put(n, d, o[n][d], m[n], lsum[n]);
-  } else {
-    // join of the key groups: each block of 16 queries through LDS, the output's dims shared out
-    f32x4_t* ob = reinterpret_cast<f32x4_t*>(lds);
+    for (int c = 0; c < NCH; ++c) {
+      const int key = (c * 64 + lane) / CPR, j = (c * 64 + lane) % CPR;
+      *reinterpret_cast<u32x4_t*>(ks + key * ROWB + (j ^ Tl::kswz(key)) * 16) = kreg[c];
+      *reinterpret_cast<u32x4_t*>(vs + key * ROWB + (j ^ Tl::vswz(key)) * 16) = vreg[c];
+    }
+    if (k0 + 4 * KW < s.kend) {
+      rows.set(a, k0 + 4 * KW, pg);
+      fetch();
+      pg = s.page(a, k0 + 8 * KW, KW);
+    }
+    const int64_t j0 = k0 - s.ctx;
+    const bool full = there == Tl::ALL && (j0 + KW <= 0 || (!a.mask && j0 + KW <= i_first + 1));
+    uint64_t bits[NQ];
+    if (!full) {
 #pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-      __syncthreads();
-#pragma unroll
-      for (int d = 0; d < NDB; ++d) ob[(wave * NDB + d) * 64 + lane] = o[n][d];
-      if (g == 0) ml_s[wave][ql] = float2{m[n], lsum[n]};
-      __syncthreads();
-      float mm = -INFINITY, ll = 0.f, w[WK];
-#pragma unroll
-      for (int k = 0; k < WK; ++k) mm = fmaxf(mm, ml_s[k * WQ + wq][ql].x);
-#pragma unroll
-      for (int k = 0; k < WK; ++k) {
-        const float2 x = ml_s[k * WQ + wq][ql];
-        w[k] = x.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x.x - mm);
-        ll += x.y * w[k];
+      for (int n = 0; n < NQ; ++n) {
+        if (a.mask) {
+          MaskWords w;
+          w.load(a.mask + t.qrow[n] * a.words, a.words, j0);
+          bits[n] = there & w.bits(j0);
+        } else {
+          bits[n] = there & chain_bits(t.qi[n], j0);
+        }
       }
-      for (int d = wk; d < NDB; d += WK) {
-        f32x4_t x = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    t.step(a, ks, vs, full, bits);
+  }
+
+  if (__syncthreads_or(bad) && wave == 0) t.add_not_finite(a, s);
+  t.sum_lanes();
+  // join of the four waves, 16 queries at a time; each wave writes a share of the dims
+  f32x4_t* ob = reinterpret_cast<f32x4_t*>(lds);
 #pragma unroll
-        for (int k = 0; k < WK; ++k) x += ob[((k * WQ + wq) * NDB + d) * 64 + lane] * w[k];
-        put(n, d, x, mm, ll);
-      }
+  for (int n = 0; n < NQ; ++n) {
+    __syncthreads();
+#pragma unroll
+    for (int d = 0; d < NDB; ++d) ob[(wave * NDB + d) * 64 + lane] = t.o[n][d];
+    if (t.g == 0) ml_s[wave][t.ql] = float2{t.m[n], t.lsum[n]};
+    __syncthreads();
+    float mm = -INFINITY, ll = 0.f, w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) mm = fmaxf(mm, ml_s[k][t.ql].x);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float2 x = ml_s[k][t.ql];
+      w[k] = x.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x.x - mm);
+      ll += x.y * w[k];
+    }
+    for (int d = wave; d < NDB; d += 4) {
+      f32x4_t x = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x += ob[(k * NDB + d) * 64 + lane] * w[k];
+      t.put(a, s, n, d, x, mm, ll);
     }
   }
 }
 
+// ---------------------------------------------------------------- many queries
+// 64 NQ queries a workgroup, 16 NQ in each of its four waves, all on the same key tiles.
+// Tiles go from the cache to LDS without passing registers (global_load_lds, 1 KB a wave
+// instruction: the swizzle is in which chunk a lane asks for), two stages, the next tile
+// in flight during the present one's matrix work.  The loads are written so that the
+// compiler does not count them; the wait for them is explicit.
+template <class T, int DH, int NQ>
+__global__ void __launch_bounds__(256, 2) tree_attn_tile_kernel(TreeAttnArgs a) {
+  constexpr int KW = DH * (int)sizeof(T) > 256 ? 32 : 64;
+  typedef Tile<T, DH, NQ, KW> Tl;
+  constexpr int CPR = Tl::CPR, NIN = Tl::BYTES / 4096;   // wave instructions per wave for K, and for V
+  constexpr int KPI = 64 / CPR > 0 ? 64 / CPR : 1;        // keys of an instruction
+  __shared__ __align__(1024) char lds[2 * 2 * Tl::BYTES];
+  Share s;
+  if (!s.init(a, 64 * NQ)) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int first = s.q0 + wave * 16 * NQ;
+  const bool active = first < s.nq;
+  int pg = s.page(a, s.kbeg, KW);
+  TileRows rows;
+  auto dma = [&](const char* p, char* dst) {
+    const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void_t*)dst);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(p) : "memory", "m0");
+  };
+  auto fetch = [&](int stage) {
+    char* ks = lds + stage * 2 * Tl::BYTES;
+#pragma unroll
+    for (int c = 0; c < NIN; ++c) {
+      const int in = c * 4 + wave, key = in * KPI + lane / CPR, j = lane % CPR;
+      dma(a.k + s.kvh * a.k_head + (j ^ Tl::kswz(key)) * 16 + (uint64_t)__shfl(rows.k, key) * a.unit, ks + in * 1024);
+      dma(a.v + s.kvh * a.v_head + (j ^ Tl::vswz(key)) * 16 + (uint64_t)__shfl(rows.v, key) * a.unit,
+          ks + Tl::BYTES + in * 1024);
+    }
+  };
+  rows.set(a, s.kbeg, pg);
+  if (s.kbeg < s.kend) fetch(0);
+  pg = s.page(a, s.kbeg + KW, KW);
+  Tl t;
+  t.init(a, s, active ? first : s.nq - 1);
+  const int i_first = (active ? first : s.nq - 1) / a.G;
+  bool bad = false;
+  MaskWords words[NQ];
+  auto load_words = [&](int64_t k0) {
+    if (a.mask && k0 + KW > s.ctx) {
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) words[n].load(a.mask + t.qrow[n] * a.words, a.words, k0 - s.ctx);
+    }
+  };
+  load_words(s.kbeg);
+
+  int stage = 0;
+  for (int64_t k0 = s.kbeg; k0 < s.kend; k0 += KW, stage ^= 1) {
+    const uint64_t there = rows.there;
+    char* ks = lds + stage * 2 * Tl::BYTES;
+    char* vs = ks + Tl::BYTES;
+    const int64_t j0 = k0 - s.ctx;
+    const bool full = there == Tl::ALL && (j0 + KW <= 0 || (!a.mask && j0 + KW <= i_first + 1));
+    uint64_t bits[NQ];
+    if (!full) {
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) bits[n] = there & (a.mask ? words[n].bits(j0) : chain_bits(t.qi[n], j0));
+    }
+    // this tile has landed, and the other stage has been read
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (k0 + KW < s.kend) {
+      rows.set(a, k0 + KW, pg);
+      load_words(k0 + KW);
+      fetch(stage ^ 1);
+      pg = s.page(a, k0 + 2 * KW, KW);
+    }
+    if (there != Tl::ALL || k0 + KW > s.clear) {
+#pragma unroll
+      for (int c = 0; c < NIN; ++c) {
+        u32x4_t* p = reinterpret_cast<u32x4_t*>(vs) + c * 256 + threadIdx.x;
+        u32x4_t w = *p;
+        if (Tl::finite(w)) {
+          *p = w;
+          bad = true;
+        }
+      }
+      __syncthreads();
+    }
+    bool some = full;
+    if (!full) {
+      uint64_t any = 0;
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) any |= bits[n];
+      some = __any(any != 0);
+    }
+    if (active && some) t.step(a, ks, vs, full, bits);   // no query of the wave sees the tile: nothing to add
+  }
+  if (__syncthreads_or(bad)) t.add_not_finite(a, s);
+  t.sum_lanes();
+  if (!active) return;
+#pragma unroll
+  for (int n = 0; n < NQ; ++n)
+#pragma unroll
+    for (int d = 0; d < Tl::NDB; ++d) t.put(a, s, n, d, t.o[n][d], t.m[n], t.lsum[n]);
+}
+
 // Joins the parts of requests whose keys were split: DH / 4 lanes per row and head.
+// The lanes first take a split's maximum and sum each, then all of them its dims.
 template <class T, int DH>
 __global__ void __launch_bounds__(256) tree_attn_join_kernel(TreeAttnArgs a) {
   constexpr int LPR = DH / 4;
@@ -424,19 +607,31 @@ __global__ void __launch_bounds__(256) tree_attn_join_kernel(TreeAttnArgs a) {
   if (b >= a.B) return;
   const int r0 = a.row_off[b], count = a.row_off[b + 1] - r0;
   if (i >= min(count, a.n_rows - r0)) return;
-  const KeySpan span = key_span(a, b, count);
-  const int n = split_count(a, span.total);
+  Share s;
+  const int n = split_count(a, s.keys(a, b, count));
   if (n <= 1) return;
   const int64_t row = ((int64_t)r0 + i) * a.H + h, step = (int64_t)a.n_rows * a.H;
-  float mm = -INFINITY;
-  for (int s = 0; s < n; ++s) mm = fmaxf(mm, a.part_ml[s * step + row].x);
-  float ll = 0.f;
+  float mm = -INFINITY, ll = 0.f;
   f32x4_t x = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < n; ++s) {
-    const float2 ml = a.part_ml[s * step + row];
-    const float w = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - mm);
-    ll += ml.y * w;
-    x += *reinterpret_cast<const f32x4_t*>(a.part + (s * step + row) * DH + lane * 4) * w;
+  for (int s0 = 0; s0 < n; s0 += LPR) {
+    const int here = min(LPR, n - s0);
+    const float2 ml = lane < here ? a.part_ml[(s0 + lane) * step + row] : float2{-INFINITY, 0.f};
+    float mx = ml.x;
+#pragma unroll
+    for (int w = 1; w < LPR; w <<= 1) mx = fmaxf(mx, __shfl_xor(mx, w));
+    const float mnew = fmaxf(mm, mx);
+    const float alpha = mm == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mm - mnew);
+    mm = mnew;
+    const float wt = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - mm);
+    float sum = ml.y * wt;
+#pragma unroll
+    for (int w = 1; w < LPR; w <<= 1) sum += __shfl_xor(sum, w);
+    ll = ll * alpha + sum;
+    x *= alpha;
+    const float* p = a.part + (s0 * step + row) * DH + lane * 4;
+    const int l0 = (threadIdx.x & 63) / LPR * LPR;
+#pragma unroll 8
+    for (int k = 0; k < here; ++k) x += *reinterpret_cast<const f32x4_t*>(p + k * step * DH) * __shfl(wt, l0 + k);
   }
   const bool some = ll > 0.f || ll != ll;
   x *= some ? 1.f / ll : 0.f;
@@ -479,12 +674,19 @@ struct AttnPlan {
 AttnPlan plan_attention(const atspeed_tree_attention_args& a) {
   AttnPlan p{};
   const int64_t nq = (int64_t)std::min(a.max_new, a.n_rows) * (a.n_heads / a.n_kv_heads);
-  p.tile = nq <= 16 ? 16 : nq <= 32 ? 32 : nq <= 64 ? 64 : 128;
+  const bool bf = a.dtype == ATSPEED_BF16;
+  p.tile = nq <= 16 ? 16 : nq <= 32 && bf ? 32 : nq <= 64 || !bf ? 64 : 128;
   p.qtiles = (int)((nq + p.tile - 1) / p.tile);
   const int64_t cap = (int64_t)a.max_pages * a.page_size;
   const int64_t keys = std::max<int64_t>(1, std::min<int64_t>((int64_t)a.max_ctx + a.max_new, cap));
   const int64_t base = (int64_t)a.B * a.n_kv_heads * p.qtiles;
-  const int64_t want = std::max<int64_t>(1, 2048 / base);
+  // Keys are split until the launch has 8 workgroups for each of the 256 CUs, 32 of the
+  // short ones of few queries: the bounds count every context as the longest, and what
+  // ragged contexts leave over is spread evenly only if the pieces are many (64 single
+  // tokens over up to 8,192 keys: 208 us with 2,048, 175 with 4,096, 155 with 8,192; trees
+  // over up to 65,536 keys: 171 us with 1,024, 158 with 2,048, 199 with 4,096, where the
+  // join of the pieces costs more than the spread gains).
+  const int64_t want = std::max<int64_t>(1, (p.tile <= 32 ? 8192 : 2048) / base);
   p.chunk = std::max<int64_t>(256, ((keys + want - 1) / want + 127) / 128 * 128);
   p.splits = (int)((keys + p.chunk - 1) / p.chunk);
   const size_t rows = (size_t)p.splits * a.n_rows * a.n_heads;
@@ -493,11 +695,11 @@ AttnPlan plan_attention(const atspeed_tree_attention_args& a) {
   return p;
 }
 
-template <class T, int DH, int NQ, int WQ, int KW>
-atspeed_status launch_attention(const TreeAttnArgs& p, hipStream_t st) {
+template <class T, int DH, class F>
+atspeed_status launch_attention(const TreeAttnArgs& p, F kernel, hipStream_t st) {
   const long long pairs = (long long)p.B * p.KH, n = (pairs + 7) / 8 * 8 * p.qtiles * p.splits;
   if (n >= (1LL << 31)) return fail(ATSPEED_E_SHAPE, "tree attention: too many query tiles");
-  hipLaunchKernelGGL((tree_attn_kernel<T, DH, NQ, WQ, KW>), dim3((unsigned)n), dim3(256), 0, st, p);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)n), dim3(256), 0, st, p);
   HIP_TRY(hipGetLastError());
   if (p.splits > 1) {
     const long long rows = (long long)p.B * p.max_new * p.H, per = 256 / (DH / 4);
@@ -509,11 +711,13 @@ atspeed_status launch_attention(const TreeAttnArgs& p, hipStream_t st) {
 
 template <class T, int DH>
 atspeed_status run_attention(const TreeAttnArgs& p, int tile, hipStream_t st) {
-  constexpr int KW1 = sizeof(T) == 2 ? 32 : 16;
-  if (tile == 16) return launch_attention<T, DH, 1, 1, KW1>(p, st);
-  if (tile == 32) return launch_attention<T, DH, 2, 1, KW1>(p, st);
-  if (tile == 64) return launch_attention<T, DH, 1, 4, 64>(p, st);
-  return launch_attention<T, DH, 2, 4, 64>(p, st);
+  if (tile == 16) return launch_attention<T, DH>(p, tree_attn_stream_kernel<T, DH, 1>, st);
+  if (tile == 64) return launch_attention<T, DH>(p, tree_attn_tile_kernel<T, DH, 1>, st);
+  if constexpr (sizeof(T) == 2) {
+    if (tile == 32) return launch_attention<T, DH>(p, tree_attn_stream_kernel<T, DH, 2>, st);
+    return launch_attention<T, DH>(p, tree_attn_tile_kernel<T, DH, 2>, st);
+  }
+  return fail(ATSPEED_E_DEVICE, "tree attention: no such tile");
 }
 
 }  // namespace
@@ -543,7 +747,22 @@ atspeed_status atspeed_tree_attention(const atspeed_tree_attention_args* args, v
     return fail(ATSPEED_E_WORKSPACE, "tree attention: workspace is too small or not 16-byte aligned");
   TreeAttnArgs p{};
   p.q = (const char*)a.q; p.q_row = a.q_row_stride * es; p.q_head = a.q_head_stride * es;
-  p.k = pages_dev(a.k_pages, es); p.v = pages_dev(a.v_pages, es);
+  p.k = (const char*)a.k_pages.data; p.v = (const char*)a.v_pages.data;
+  p.k_head = a.k_pages.head_stride * es; p.v_head = a.v_pages.head_stride * es;
+  // rows of the caches by 32-bit numbers of the largest unit that divides the strides
+  const int64_t strides[] = {a.k_pages.page_stride * es, a.k_pages.token_stride * es, a.v_pages.page_stride * es,
+                             a.v_pages.token_stride * es};
+  uint64_t any = 1u << 20;
+  for (int64_t s : strides) {
+    if (s < 0) return fail(ATSPEED_E_INVALID, "tree attention: negative cache strides");
+    any |= (uint64_t)s;
+  }
+  p.unit = (uint32_t)(any & (~any + 1));
+  for (int i = 0; i < 4; i += 2)
+    if ((double)strides[i] / p.unit * a.n_pool + (double)strides[i + 1] / p.unit * a.page_size >= 4294967296.0)
+      return fail(ATSPEED_E_SHAPE, "tree attention: a cache of 2^32 or more of the largest unit dividing its strides");
+  p.k_page = (uint32_t)(strides[0] / p.unit); p.k_token = (uint32_t)(strides[1] / p.unit);
+  p.v_page = (uint32_t)(strides[2] / p.unit); p.v_token = (uint32_t)(strides[3] / p.unit);
   p.table = a.block_table; p.row_off = a.row_off; p.ctx = a.ctx; p.mask = a.mask;
   p.out = (char*)a.out; p.o_row = a.out_row_stride * es; p.o_head = a.out_head_stride * es;
   p.lse = a.lse;

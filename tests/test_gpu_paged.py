@@ -342,6 +342,25 @@ def test_attention_keeps_what_is_masked_out(dtype, dh, tree, poison):
     assert bool(got[hurt].isnan().all())
 
 
+@pytest.mark.parametrize("dtype,dh", [(BF16, 128), (BF16, 64), (F32, 32), (F32, 128)])
+@pytest.mark.parametrize("new", [3, 40, 150])
+@pytest.mark.parametrize("poison", [math.nan, math.inf, -math.inf])
+def test_attention_values_of_the_context_reach_every_row(dtype, dh, new, poison):
+    """A value that is not finite in the context, in a tile with new keys or with a bad page too: every row has it."""
+    c = attention_case(13, [100, 37], [new, 2], 4, 2, dh, 16, dtype, True)
+    c["block_table"][0, 2] = -1
+    table = c["block_table"].cpu().numpy()
+    clean = atspeed_tree_attention(**c)
+    for p, dim in ((50, 3), (99, 17)):                 # beside the bad page, and in the last context token
+        c["v_cache"].view(-1, 2, dh)[table[0, p // 16] * 16 + p % 16, 1, dim] = poison
+        got = atspeed_tree_attention(**c).float()[:new, 2:, dim]
+        assert bool((got.isnan() if math.isnan(poison) else got == poison).all())
+    got, clean = atspeed_tree_attention(**c).float(), clean.float()
+    got[:new, 2:, 3] = clean[:new, 2:, 3]
+    got[:new, 2:, 17] = clean[:new, 2:, 17]
+    assert torch.equal(got, clean)
+
+
 @pytest.mark.parametrize("dtype,dh", [(BF16, 128), (F32, 64)])
 def test_attention_seen_infinite_values_reach_their_rows(dtype, dh):
     c = attention_case(12, [21, 5], [30, 8], 4, 2, dh, 16, dtype, True, levels=2)
