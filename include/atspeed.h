@@ -584,8 +584,8 @@ ATSPEED_API atspeed_status atspeed_kv_append(const atspeed_kv_append_args* args,
  *   row_off [B + 1], ctx [B], mask [n_rows, mask_words] as atspeed_page_plan writes
  *     them.  Rows past min(row_off[B], n_rows) and rows past a request's max_new-th
  *     are left as they were; new rows past 64 * mask_words are not seen.  A negative
- *     ctx[b] means a request that sees nothing.  Keys past max_pages * page_size,
- *     and keys in pages outside 0 .. n_pool - 1, are not seen.
+ *     ctx[b] means a request that sees nothing.  Keys past max_pages * page_size
+ *     or 2^30, and keys in pages outside 0 .. n_pool - 1, are not seen.
  *   max_ctx, max_new: what ctx[b] and a request's row count stay within; they size
  *     the launch (a context above max_ctx is still read whole).
  * workspace: 16-byte aligned, at least atspeed_tree_attention_workspace_bytes (may be

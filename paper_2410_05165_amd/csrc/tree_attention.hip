@@ -26,7 +26,8 @@ struct TreeAttnArgs {
   float2* part_ml;             // [splits][n_rows][H] running maximum and sum
   int B, n_rows, H, G, KH, max_pages, n_pool, max_new, words, shift, tail;
   int qtiles, splits;
-  int64_t chunk;               // keys of a split
+  int cap;                     // keys a request can have: max_pages pages, at most 2^30
+  int chunk;                   // keys of a split
   uint32_t q_flip;             // sign bits of the queries' elements (negative scale)
   float scale;                 // |scale| log2(e)
 };
@@ -40,16 +41,16 @@ typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
 typedef __attribute__((address_space(3))) void lds_void_t;
 
 // Pieces of a request's keys; the last one takes what a context above max_ctx holds more.
-__device__ __forceinline__ int split_count(const TreeAttnArgs& a, int64_t total) {
-  return total <= a.chunk ? 1 : (int)min((total + a.chunk - 1) / a.chunk, (int64_t)a.splits);
+__device__ __forceinline__ int split_count(const TreeAttnArgs& a, int total) {
+  return total <= a.chunk ? 1 : min((total - 1) / a.chunk + 1, a.splits);
 }
 
 // One workgroup's share: a request, a key/value head, a tile of its queries (row i, head
 // h of the group: query i * G + h), a range of its keys.
 struct Share {
   int kvh, r0, nq, q0, split, nsplit;
-  int64_t ctx, kbeg, kend;   // context keys; this workgroup's keys
-  int64_t clear;             // from this key on some query may not see a key
+  int ctx, kbeg, kend;   // context keys; this workgroup's keys
+  int clear;             // from this key on some query may not see a key
   const int* table;
 
   // False where there is nothing to do.  QB queries a tile.
@@ -69,7 +70,7 @@ struct Share {
     nq = min(min(count, a.n_rows - r0), a.max_new) * a.G;
     q0 = qt * QB;
     if (q0 >= nq) return false;
-    const int64_t total = keys(a, b, count);
+    const int total = keys(a, b, count);
     nsplit = split_count(a, total);
     if (split >= nsplit) return false;
     kbeg = split * a.chunk;
@@ -80,15 +81,15 @@ struct Share {
     return true;
   }
   // Keys of request b with `count` new rows (none where ctx is negative); sets ctx.
-  __device__ __forceinline__ int64_t keys(const TreeAttnArgs& a, int b, int count) {
-    const int64_t cap = (int64_t)a.max_pages << a.shift, c = a.ctx[b];
-    ctx = c < 0 ? 0 : min(c, cap);
-    return c < 0 ? 0 : min(c + (a.mask ? min((int64_t)count, (int64_t)a.words * 64) : (int64_t)count), cap);
+  __device__ __forceinline__ int keys(const TreeAttnArgs& a, int b, int count) {
+    const int c = a.ctx[b];
+    ctx = min(max(c, 0), a.cap);
+    const int64_t n = a.mask ? min((int64_t)count, (int64_t)a.words * 64) : (int64_t)count;
+    return c < 0 ? 0 : (int)min(c + n, (int64_t)a.cap);
   }
   // Page of key k0 + lane for the first n lanes, -1 where the key is not there.
-  __device__ __forceinline__ int page(const TreeAttnArgs& a, int64_t k0, int n) const {
-    const int lane = threadIdx.x & 63;
-    const int64_t key = k0 + lane;
+  __device__ __forceinline__ int page(const TreeAttnArgs& a, int k0, int n) const {
+    const int lane = threadIdx.x & 63, key = k0 + lane;
     return lane < n && key < kend ? table[key >> a.shift] : -1;
   }
 };
@@ -97,9 +98,9 @@ struct Share {
 struct TileRows {
   uint32_t k, v;     // units; a readable row where the key is not there
   uint64_t there;    // bit i: key i is there
-  __device__ __forceinline__ void set(const TreeAttnArgs& a, int64_t k0, int page) {
+  __device__ __forceinline__ void set(const TreeAttnArgs& a, int k0, int page) {
     const bool ok = (unsigned)page < (unsigned)a.n_pool;
-    const uint32_t pg = ok ? page : 0, tok = (uint32_t)(k0 + (threadIdx.x & 63)) & a.tail;
+    const uint32_t pg = ok ? page : 0, tok = (k0 + (threadIdx.x & 63)) & a.tail;
     k = pg * a.k_page + tok * a.k_token;
     v = pg * a.v_page + tok * a.v_token;
     there = __ballot(ok);
@@ -110,21 +111,21 @@ struct TileRows {
 // (j < 0) are always seen, bits past the words never.
 struct MaskWords {
   uint64_t lo, hi;
-  __device__ __forceinline__ void load(const uint64_t* words, int n, int64_t j0) {
-    const int64_t w = j0 < 0 ? 0 : j0 >> 6;
+  __device__ __forceinline__ void load(const uint64_t* words, int n, int j0) {
+    const int w = j0 < 0 ? 0 : j0 >> 6;
     lo = j0 > -64 && w < n ? words[w] : 0ull;
     hi = j0 > 0 && (j0 & 63) && w + 1 < n ? words[w + 1] : 0ull;
   }
-  __device__ __forceinline__ uint64_t bits(int64_t j0) const {
+  __device__ __forceinline__ uint64_t bits(int j0) const {
     if (j0 <= -64) return ~0ull;
     if (j0 < 0) return (lo << -j0) | ((1ull << -j0) - 1);
-    const int s = (int)(j0 & 63);
+    const int s = j0 & 63;
     return s ? (lo >> s) | (hi << (64 - s)) : lo;
   }
 };
 // Without a mask: the keys up to the row's own, at ctx + i.
-__device__ __forceinline__ uint64_t chain_bits(int i, int64_t j0) {
-  const int64_t n = i + 1 - j0;
+__device__ __forceinline__ uint64_t chain_bits(int i, int j0) {
+  const int n = i + 1 - j0;
   return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1;
 }
 
@@ -331,14 +332,14 @@ struct Tile {
   // ... and here they reach the rows that see them: p is positive there, so they are
   // what they add.
   __device__ __forceinline__ void add_not_finite(const TreeAttnArgs& a, const Share& s) {
-    for (int64_t key = s.kbeg; key < s.kend; ++key) {
+    for (int key = s.kbeg; key < s.kend; ++key) {
       const int page = s.table[key >> a.shift];
       if ((unsigned)page >= (unsigned)a.n_pool) continue;
-      const uint32_t row = page * a.v_page + ((uint32_t)key & a.tail) * a.v_token;
+      const uint32_t row = page * a.v_page + (key & a.tail) * a.v_token;
       const T* vp = reinterpret_cast<const T*>(a.v + (uint64_t)row * a.unit + s.kvh * a.v_head);
 #pragma unroll
       for (int n = 0; n < NQ; ++n) {
-        const int64_t j0 = key - s.ctx;
+        const int j0 = key - s.ctx;
         uint64_t bits;
         if (a.mask) {
           MaskWords w;
@@ -410,7 +411,7 @@ __global__ void __launch_bounds__(256, 2) tree_attn_stream_kernel(TreeAttnArgs a
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   char* ks = lds + wave * 2 * Tl::BYTES;
   char* vs = ks + Tl::BYTES;
-  const int64_t first = s.kbeg + wave * KW;
+  const int first = s.kbeg + wave * KW;
   int pg = s.page(a, first, KW);
   TileRows rows;
   u32x4_t kreg[NCH], vreg[NCH];
@@ -430,7 +431,7 @@ __global__ void __launch_bounds__(256, 2) tree_attn_stream_kernel(TreeAttnArgs a
   const int i_first = s.q0 / a.G;
   bool bad = false;
 
-  for (int64_t k0 = first; k0 < s.kend; k0 += 4 * KW) {
+  for (int k0 = first; k0 < s.kend; k0 += 4 * KW) {
     const uint64_t there = rows.there;
     if (there != Tl::ALL || k0 + KW > s.clear) {
 #pragma unroll
@@ -447,7 +448,7 @@ __global__ void __launch_bounds__(256, 2) tree_attn_stream_kernel(TreeAttnArgs a
       fetch();
       pg = s.page(a, k0 + 8 * KW, KW);
     }
-    const int64_t j0 = k0 - s.ctx;
+    const int j0 = k0 - s.ctx;
     const bool full = there == Tl::ALL && (j0 + KW <= 0 || (!a.mask && j0 + KW <= i_first + 1));
     uint64_t bits[NQ];
     if (!full) {
@@ -502,7 +503,7 @@ __global__ void __launch_bounds__(256, 2) tree_attn_stream_kernel(TreeAttnArgs a
 // compiler does not count them; the wait for them is explicit.
 template <class T, int DH, int NQ>
 __global__ void __launch_bounds__(256, 2) tree_attn_tile_kernel(TreeAttnArgs a) {
-  constexpr int KW = DH * (int)sizeof(T) > 256 ? 32 : 64;
+  constexpr int KW = NQ * 8192 / (DH * (int)sizeof(T)) > 64 ? 64 : NQ * 8192 / (DH * (int)sizeof(T));
   typedef Tile<T, DH, NQ, KW> Tl;
   constexpr int CPR = Tl::CPR, NIN = Tl::BYTES / 4096;   // wave instructions per wave for K, and for V
   constexpr int KPI = 64 / CPR > 0 ? 64 / CPR : 1;        // keys of an instruction
@@ -536,7 +537,7 @@ __global__ void __launch_bounds__(256, 2) tree_attn_tile_kernel(TreeAttnArgs a) 
   const int i_first = (active ? first : s.nq - 1) / a.G;
   bool bad = false;
   MaskWords words[NQ];
-  auto load_words = [&](int64_t k0) {
+  auto load_words = [&](int k0) {
     if (a.mask && k0 + KW > s.ctx) {
 #pragma unroll
       for (int n = 0; n < NQ; ++n) words[n].load(a.mask + t.qrow[n] * a.words, a.words, k0 - s.ctx);
@@ -545,11 +546,11 @@ __global__ void __launch_bounds__(256, 2) tree_attn_tile_kernel(TreeAttnArgs a) 
   load_words(s.kbeg);
 
   int stage = 0;
-  for (int64_t k0 = s.kbeg; k0 < s.kend; k0 += KW, stage ^= 1) {
+  for (int k0 = s.kbeg; k0 < s.kend; k0 += KW, stage ^= 1) {
     const uint64_t there = rows.there;
     char* ks = lds + stage * 2 * Tl::BYTES;
     char* vs = ks + Tl::BYTES;
-    const int64_t j0 = k0 - s.ctx;
+    const int j0 = k0 - s.ctx;
     const bool full = there == Tl::ALL && (j0 + KW <= 0 || (!a.mask && j0 + KW <= i_first + 1));
     uint64_t bits[NQ];
     if (!full) {
@@ -595,16 +596,17 @@ __global__ void __launch_bounds__(256, 2) tree_attn_tile_kernel(TreeAttnArgs a) 
     for (int d = 0; d < Tl::NDB; ++d) t.put(a, s, n, d, t.o[n][d], t.m[n], t.lsum[n]);
 }
 
-// Joins the parts of requests whose keys were split: DH / 4 lanes per row and head.
-// The lanes first take a split's maximum and sum each, then all of them its dims.
+// Joins the parts of requests whose keys were split, a workgroup per row and head: all
+// threads take the splits' maxima and sums, then groups of DH / 4 of them the splits in
+// turn, four dims a thread.  Bound by the latency of those loads: with one such group
+// per row, 61 parts of 4 users' 32 rows took 29 us.
 template <class T, int DH>
 __global__ void __launch_bounds__(256) tree_attn_join_kernel(TreeAttnArgs a) {
-  constexpr int LPR = DH / 4;
-  const int64_t idx = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
-  const int lane = threadIdx.x % LPR, h = (int)(idx % a.H);
-  const int64_t bi = idx / a.H;
-  const int b = (int)(bi / a.max_new), i = (int)(bi % a.max_new);
-  if (b >= a.B) return;
+  constexpr int LPR = DH / 4, GROUPS = 256 / LPR;
+  __shared__ f32x4_t xs[GROUPS][LPR];
+  __shared__ float red[2][4];
+  const int tid = threadIdx.x, lane = tid % LPR, grp = tid / LPR;
+  const int h = blockIdx.x % a.H, bi = blockIdx.x / a.H, b = bi / a.max_new, i = bi % a.max_new;
   const int r0 = a.row_off[b], count = a.row_off[b + 1] - r0;
   if (i >= min(count, a.n_rows - r0)) return;
   Share s;
@@ -612,27 +614,30 @@ __global__ void __launch_bounds__(256) tree_attn_join_kernel(TreeAttnArgs a) {
   if (n <= 1) return;
   const int64_t row = ((int64_t)r0 + i) * a.H + h, step = (int64_t)a.n_rows * a.H;
   float mm = -INFINITY, ll = 0.f;
-  f32x4_t x = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  for (int s0 = 0; s0 < n; s0 += LPR) {
-    const int here = min(LPR, n - s0);
-    const float2 ml = lane < here ? a.part_ml[(s0 + lane) * step + row] : float2{-INFINITY, 0.f};
-    float mx = ml.x;
+  for (int k = tid; k < n; k += 256) mm = fmaxf(mm, a.part_ml[k * step + row].x);
 #pragma unroll
-    for (int w = 1; w < LPR; w <<= 1) mx = fmaxf(mx, __shfl_xor(mx, w));
-    const float mnew = fmaxf(mm, mx);
-    const float alpha = mm == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mm - mnew);
-    mm = mnew;
-    const float wt = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - mm);
-    float sum = ml.y * wt;
-#pragma unroll
-    for (int w = 1; w < LPR; w <<= 1) sum += __shfl_xor(sum, w);
-    ll = ll * alpha + sum;
-    x *= alpha;
-    const float* p = a.part + (s0 * step + row) * DH + lane * 4;
-    const int l0 = (threadIdx.x & 63) / LPR * LPR;
-#pragma unroll 8
-    for (int k = 0; k < here; ++k) x += *reinterpret_cast<const f32x4_t*>(p + k * step * DH) * __shfl(wt, l0 + k);
+  for (int w = 1; w < 64; w <<= 1) mm = fmaxf(mm, __shfl_xor(mm, w));
+  if ((tid & 63) == 0) red[0][tid >> 6] = mm;
+  __syncthreads();
+  mm = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+  auto weight = [&](float m) { return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mm); };
+  for (int k = tid; k < n; k += 256) {
+    const float2 ml = a.part_ml[k * step + row];
+    ll += ml.y * weight(ml.x);
   }
+#pragma unroll
+  for (int w = 1; w < 64; w <<= 1) ll += __shfl_xor(ll, w);
+  if ((tid & 63) == 0) red[1][tid >> 6] = ll;
+  f32x4_t x = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int k = grp; k < n; k += GROUPS)
+    x += *reinterpret_cast<const f32x4_t*>(a.part + (k * step + row) * DH + lane * 4) * weight(a.part_ml[k * step + row].x);
+  xs[grp][lane] = x;
+  __syncthreads();
+  if (grp > 0) return;
+#pragma unroll
+  for (int k = 1; k < GROUPS; ++k) x += xs[k][lane];
+  ll = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
   const bool some = ll > 0.f || ll != ll;
   x *= some ? 1.f / ll : 0.f;
   T* out = reinterpret_cast<T*>(a.out + ((int64_t)r0 + i) * a.o_row + h * a.o_head) + lane * 4;
@@ -653,6 +658,7 @@ static atspeed_status check_attention(const atspeed_tree_attention_args* args) {
   if (a.max_pages < 1) return fail(ATSPEED_E_INVALID, "max_pages must be >= 1");
   if (!std::isfinite(a.scale)) return fail(ATSPEED_E_INVALID, "scale must be finite");
   if (a.mask && a.mask_words < 1) return fail(ATSPEED_E_INVALID, "mask_words must be >= 1");
+  if (a.n_rows >= (1 << 30)) return fail(ATSPEED_E_SHAPE, "n_rows must be below 2^30");
   if ((long long)a.n_rows * a.n_heads >= (1LL << 31)) return fail(ATSPEED_E_SHAPE, "n_rows x n_heads must be below 2^31");
   return ATSPEED_OK;
 }
@@ -666,8 +672,7 @@ namespace {
 // Launch of one call: queries per workgroup, and how the keys are split.
 struct AttnPlan {
   int tile;          // queries of a workgroup
-  int qtiles, splits;
-  int64_t chunk;
+  int qtiles, splits, cap, chunk;
   size_t part_bytes, bytes;
 };
 
@@ -677,8 +682,8 @@ AttnPlan plan_attention(const atspeed_tree_attention_args& a) {
   const bool bf = a.dtype == ATSPEED_BF16;
   p.tile = nq <= 16 ? 16 : nq <= 32 && bf ? 32 : nq <= 64 || !bf ? 64 : 128;
   p.qtiles = (int)((nq + p.tile - 1) / p.tile);
-  const int64_t cap = (int64_t)a.max_pages * a.page_size;
-  const int64_t keys = std::max<int64_t>(1, std::min<int64_t>((int64_t)a.max_ctx + a.max_new, cap));
+  p.cap = (int)std::min<int64_t>((int64_t)a.max_pages * a.page_size, 1 << 30);
+  const int64_t keys = std::max<int64_t>(1, std::min<int64_t>((int64_t)a.max_ctx + a.max_new, p.cap));
   const int64_t base = (int64_t)a.B * a.n_kv_heads * p.qtiles;
   // Keys are split until the launch has 8 workgroups for each of the 256 CUs, 32 of the
   // short ones of few queries: the bounds count every context as the longest, and what
@@ -687,7 +692,7 @@ AttnPlan plan_attention(const atspeed_tree_attention_args& a) {
   // over up to 65,536 keys: 171 us with 1,024, 158 with 2,048, 199 with 4,096, where the
   // join of the pieces costs more than the spread gains).
   const int64_t want = std::max<int64_t>(1, (p.tile <= 32 ? 8192 : 2048) / base);
-  p.chunk = std::max<int64_t>(256, ((keys + want - 1) / want + 127) / 128 * 128);
+  p.chunk = (int)std::max<int64_t>(256, ((keys + want - 1) / want + 127) / 128 * 128);
   p.splits = (int)((keys + p.chunk - 1) / p.chunk);
   const size_t rows = (size_t)p.splits * a.n_rows * a.n_heads;
   p.part_bytes = p.splits > 1 ? rows * a.d_head * sizeof(float) : 0;
@@ -702,8 +707,9 @@ atspeed_status launch_attention(const TreeAttnArgs& p, F kernel, hipStream_t st)
   hipLaunchKernelGGL(kernel, dim3((unsigned)n), dim3(256), 0, st, p);
   HIP_TRY(hipGetLastError());
   if (p.splits > 1) {
-    const long long rows = (long long)p.B * p.max_new * p.H, per = 256 / (DH / 4);
-    hipLaunchKernelGGL((tree_attn_join_kernel<T, DH>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, st, p);
+    // few: splits come only with few query tiles
+    const long long rows = (long long)p.B * p.max_new * p.H;
+    hipLaunchKernelGGL((tree_attn_join_kernel<T, DH>), dim3((unsigned)rows), dim3(256), 0, st, p);
     HIP_TRY(hipGetLastError());
   }
   return ATSPEED_OK;
@@ -770,7 +776,7 @@ atspeed_status atspeed_tree_attention(const atspeed_tree_attention_args* args, v
   p.B = a.B; p.n_rows = a.n_rows; p.H = a.n_heads; p.KH = a.n_kv_heads; p.G = a.n_heads / a.n_kv_heads;
   p.max_pages = a.max_pages; p.n_pool = a.n_pool; p.max_new = std::min(a.max_new, a.n_rows); p.words = a.mask_words;
   p.shift = log2_of(a.page_size); p.tail = a.page_size - 1;
-  p.qtiles = plan.qtiles; p.splits = plan.splits; p.chunk = plan.chunk;
+  p.qtiles = plan.qtiles; p.splits = plan.splits; p.cap = plan.cap; p.chunk = plan.chunk;
   // the queries carry the scale's sign, so that the largest product is the largest score
   p.q_flip = a.scale < 0.f ? (es == 2 ? 0x80008000u : 0x80000000u) : 0u;
   p.scale = std::max(std::fabs(a.scale) * 1.4426950408889634f, 1e-37f);

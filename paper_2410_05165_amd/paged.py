@@ -28,53 +28,53 @@ def _library():
     return _lib
 
 
-def _check(status: int):
+def _call(fn, args, device, *more):
+    """fn(args, *more, stream) on the current stream of GPU `device` (its index)."""
+    if device == torch.cuda.current_device():
+        status = fn(args, *more, torch._C._cuda_getCurrentRawStream(device))
+    else:
+        with torch.cuda.device(device):
+            status = fn(args, *more, torch._C._cuda_getCurrentRawStream(device))
     if status != 0:
         raise AtspeedError(status, _lib.atspeed_last_error().decode())
 
 
-def _call(fn, args, device, *more):
-    """fn(args, *more, stream) on the current stream of the tensors' GPU."""
-    index = device.index
-    if index == torch.cuda.current_device():
-        _check(fn(args, *more, torch.cuda.current_stream(index).cuda_stream))
-    else:
-        with torch.cuda.device(index):
-            _check(fn(args, *more, torch.cuda.current_stream(index).cuda_stream))
-
-
 def _want(t, name, dtype, shape, device):
-    """The address of a contiguous tensor of this type, shape and device (None: 0)."""
+    """The address of a contiguous tensor of this type and shape on GPU `device` (None: none)."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{name}: want a contiguous {dtype} tensor on {device}, got {t.dtype} on {t.device}")
-    if t.shape != shape:
-        raise ValueError(f"{name}: want shape {tuple(shape)}, got {tuple(t.shape)}")
-    return t.data_ptr()
+    if t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name}: want a contiguous {dtype} {tuple(shape)} on GPU {device}, got {t.dtype} "
+                     f"{tuple(t.shape)} on {t.device}")
 
 
 def _gpu(t, name):
-    if t.device.type != "cuda":
+    """The index of the tensor's GPU."""
+    if not t.is_cuda:
         raise ValueError(f"{name} is on {t.device}: the operators run on the GPU alone")
-    return t.device
+    return t.get_device()
 
 
 def _rows(t, name, shape, dtype, device):
-    """[rows, heads, d_head] with any row and head strides."""
-    if t.dtype is not dtype or t.device != device or t.shape != shape or (shape[2] > 1 and t.stride(2) != 1):
-        raise ValueError(f"{name}: want {dtype} {tuple(shape)} on {device}, the last dimension contiguous")
-    return t
+    """(address, row stride, head stride) of [rows, heads, d_head] with any row and head strides."""
+    if t.shape == shape and t.dtype is dtype and t.get_device() == device:
+        row, head, one = t.stride()
+        if one == 1:
+            return t.data_ptr(), row, head
+    raise ValueError(f"{name}: want {dtype} {tuple(shape)} on GPU {device}, the last dimension contiguous")
 
 
 def _caches(k_cache, v_cache):
-    if k_cache.dim() != 4 or k_cache.dtype not in DTYPES:
+    """(GPU, address and strides of the keys, address and strides of the values)."""
+    device, shape, dtype = _gpu(k_cache, "k_cache"), k_cache.shape, k_cache.dtype
+    if len(shape) != 4 or dtype not in DTYPES:
         raise ValueError("k_cache: want float32 or bfloat16 [pages, page_size, kv_heads, d_head]")
-    device = _gpu(k_cache, "k_cache")
-    for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
-        if t.shape != k_cache.shape or t.dtype is not k_cache.dtype or t.device != device or t.stride(3) != 1:
-            raise ValueError(f"{name}: the caches want one type, shape and device, the last dimension contiguous")
-    return device
+    *ks, k1 = k_cache.stride()
+    *vs, v1 = v_cache.stride()
+    if v_cache.shape != shape or v_cache.dtype is not dtype or v_cache.get_device() != device or k1 != 1 or v1 != 1:
+        raise ValueError("the caches want one type, shape and device, the last dimension contiguous")
+    return device, (k_cache.data_ptr(), *ks), (v_cache.data_ptr(), *vs)
 
 
 class StepPlan(NamedTuple):
@@ -98,8 +98,7 @@ def atspeed_page_plan(held, keep, add, block_table, free_pages, n_free, page_siz
     held, keep, add [B], n_free [1]: int32; parent [B, max_nodes] int32 or None (chains).
     The returned n_free and length are the next step's n_free and held.
     """
-    dev = _gpu(block_table, "block_table")
-    i32 = torch.int32
+    dev, where, i32 = _gpu(block_table, "block_table"), block_table.device, torch.int32
     if block_table.dim() != 2:
         raise ValueError("block_table: want [B, max_pages]")
     B, most = block_table.shape
@@ -110,9 +109,9 @@ def atspeed_page_plan(held, keep, add, block_table, free_pages, n_free, page_siz
         if parent.dim() != 2:
             raise ValueError("parent: want [B, max_nodes]")
         nodes = parent.shape[1]
-    buf = torch.empty(1 + 4 * B + 1 + 4 * max_rows, dtype=i32, device=dev)
-    out = torch.split(buf, [1, B, B, B, B + 1, max_rows, max_rows, max_rows, max_rows])
-    mask = torch.empty((max_rows, (nodes + 63) // 64), dtype=torch.int64, device=dev) if parent is not None else None
+    buf = torch.empty(4 * (B + max_rows) + 2, dtype=i32, device=where)
+    out = buf.split_with_sizes([1, B, B, B, B + 1, max_rows, max_rows, max_rows, max_rows])
+    mask = torch.empty((max_rows, (nodes + 63) // 64), dtype=torch.int64, device=where) if parent is not None else None
     at = buf.data_ptr()
     row = at + 4 * (4 * B + 2)
     args = PagePlanArgs(B, page_size, most, free_pages.numel(), max_rows, nodes,
@@ -133,14 +132,14 @@ def atspeed_kv_append(k, v, k_cache, v_cache, slot):
 
     Caches [pages, page_size, kv_heads, d_head]; all four may be strided, the last dimension contiguous.
     """
-    dev = _caches(k_cache, v_cache)
+    dev, kc, vc = _caches(k_cache, v_cache)
     pool, page, heads, dh = k_cache.shape
-    shape = (slot.numel(), heads, dh)
-    _rows(k, "k", shape, k_cache.dtype, dev)
-    _rows(v, "v", shape, k_cache.dtype, dev)
-    args = KvAppendArgs(DTYPES[k_cache.dtype], shape[0], heads, dh, page, pool, k.data_ptr(), v.data_ptr(),
-                        *k.stride()[:2], *v.stride()[:2], k_cache.data_ptr(), *k_cache.stride()[:3],
-                        v_cache.data_ptr(), *v_cache.stride()[:3], _want(slot, "slot", torch.int32, shape[:1], dev))
+    dtype, n = k_cache.dtype, slot.numel()
+    shape = (n, heads, dh)
+    k_at, k_row, k_head = _rows(k, "k", shape, dtype, dev)
+    v_at, v_row, v_head = _rows(v, "v", shape, dtype, dev)
+    args = KvAppendArgs(DTYPES[dtype], n, heads, dh, page, pool, k_at, v_at, k_row, k_head, v_row, v_head, *kc, *vc,
+                        _want(slot, "slot", torch.int32, (n,), dev))
     _call(_library().atspeed_kv_append, args, dev)
 
 
@@ -153,34 +152,31 @@ def atspeed_tree_attention(q, k_cache, v_cache, block_table, row_off, ctx, max_c
     a request's row count stay within.  scale: 1 / sqrt(d_head) by default.  Returns out (given or new, of q's
     type), or (out, lse [rows, heads] fp32).
     """
-    dev = _caches(k_cache, v_cache)
+    dev, kc, vc = _caches(k_cache, v_cache)
     pool, page, kv_heads, dh = k_cache.shape
     if q.dim() != 3 or block_table.dim() != 2:
         raise ValueError("want q [rows, heads, d_head] and block_table [B, max_pages]")
+    dtype, i32 = k_cache.dtype, torch.int32
     rows, heads, _ = q.shape
     shape = (rows, heads, dh)
-    _rows(q, "q", shape, k_cache.dtype, dev)
+    q_at = _rows(q, "q", shape, dtype, dev)
     if out is None:
-        out = torch.empty(shape, dtype=q.dtype, device=dev)
-    else:
-        _rows(out, "out", shape, q.dtype, dev)
-    lse = torch.empty((rows, heads), dtype=torch.float32, device=dev) if return_lse else None
+        out = torch.empty(shape, dtype=dtype, device=q.device)
+    o_at = _rows(out, "out", shape, dtype, dev)
+    lse = torch.empty((rows, heads), dtype=torch.float32, device=q.device) if return_lse else None
     B, most = block_table.shape
-    words = 0
-    if mask is not None:
-        words = mask.shape[-1]
-    i32 = torch.int32
-    args = TreeAttentionArgs(DTYPES[q.dtype], B, rows, heads, kv_heads, dh, page, most, pool, max_ctx, max_new, words,
-                             1.0 / math.sqrt(dh) if scale is None else scale, q.data_ptr(), *q.stride()[:2],
-                             k_cache.data_ptr(), *k_cache.stride()[:3], v_cache.data_ptr(), *v_cache.stride()[:3],
+    words = 0 if mask is None else mask.shape[-1]
+    args = TreeAttentionArgs(DTYPES[dtype], B, rows, heads, kv_heads, dh, page, most, pool, max_ctx, max_new, words,
+                             1.0 / math.sqrt(dh) if scale is None else scale, *q_at, *kc, *vc,
                              _want(block_table, "block_table", i32, (B, most), dev),
                              _want(row_off, "row_off", i32, (B + 1,), dev), _want(ctx, "ctx", i32, (B,), dev),
-                             _want(mask, "mask", torch.int64, (rows, words), dev), out.data_ptr(), *out.stride()[:2],
-                             lse.data_ptr() if lse is not None else None)
-    lib = _library()
-    need = C.c_size_t(0)
-    _check(lib.atspeed_tree_attention_workspace_bytes(args, need))
-    ws = torch.empty(need.value, dtype=torch.uint8, device=dev) if need.value else None
+                             _want(mask, "mask", torch.int64, (rows, words), dev), *o_at,
+                             lse.data_ptr() if return_lse else None)
+    lib, need = _library(), C.c_size_t(0)
+    status = lib.atspeed_tree_attention_workspace_bytes(args, need)
+    if status != 0:
+        raise AtspeedError(status, lib.atspeed_last_error().decode())
+    ws = torch.empty(need.value, dtype=torch.uint8, device=q.device) if need.value else None
     _call(lib.atspeed_tree_attention, args, dev, ws.data_ptr() if ws is not None else None, need.value)
     return (out, lse) if return_lse else out
 
@@ -197,14 +193,14 @@ def atspeed_logit_rules(logits, row_off, token_base: int = 0, history=None, hist
     """
     if logits.dim() != 2 or logits.dtype not in DTYPES or (logits.shape[1] > 1 and logits.stride(1) != 1):
         raise ValueError("logits: want float32 or bfloat16 [rows, cols], rows contiguous")
-    dev = _gpu(logits, "logits")
+    dev, where = _gpu(logits, "logits"), logits.device
     rows, cols = logits.shape
     f32, i32 = torch.float32, torch.int32
     if out is None:
         if out_row is not None:
             raise ValueError("out_row scatters to a given out")
-        out = torch.empty((rows, cols), dtype=f32, device=dev)
-    elif out.dtype is not f32 or out.device != dev or out.shape[-1] != cols or (cols > 1 and out.stride(-1) != 1):
+        out = torch.empty((rows, cols), dtype=f32, device=where)
+    elif out.dtype is not f32 or out.get_device() != dev or out.shape[-1] != cols or (cols > 1 and out.stride(-1) != 1):
         raise ValueError("out: want float32 [.., cols] on the logits' device, rows contiguous")
     flat = out if out.dim() == 2 else out.view(-1, cols)
     if out_row is None and flat.shape[0] != rows:
@@ -216,7 +212,7 @@ def atspeed_logit_rules(logits, row_off, token_base: int = 0, history=None, hist
     words = 0 if mask is None else mask.shape[-1]
     n_bias = 0 if bias is None else bias.shape[0]
     states = 0 if allowed is None else allowed.shape[0]
-    if bias is not None and (bias.dtype is not f32 or bias.device != dev or bias.shape != (n_bias, cols) or
+    if bias is not None and (bias.dtype is not f32 or bias.get_device() != dev or bias.shape != (n_bias, cols) or
                              (cols > 1 and bias.stride(1) != 1)):
         raise ValueError("bias: want float32 [n, cols] on the logits' device, rows contiguous")
     args = LogitRulesArgs(DTYPES[logits.dtype], B, rows, cols, token_base, hist, nodes, words, n_bias, states,
