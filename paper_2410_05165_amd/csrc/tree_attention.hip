@@ -194,9 +194,11 @@ struct Tile {
     }
   }
 
-  // bits: the keys each query sees, if not `full` (all of them).
+  // bits: the keys each query sees, if not `full` (all of them).  between(k) runs after
+  // the k-th chunk group of the scores, k = 0 .. NKS - 1.
+  template <class F>
   __device__ __forceinline__ void step(const TreeAttnArgs& a, const char* ks, const char* vs, bool full,
-                                       const uint64_t (&bits)[NQ]) {
+                                       const uint64_t (&bits)[NQ], F&& between) {
     f32x4_t sc[NQ][NKB];
 #pragma unroll
     for (int n = 0; n < NQ; ++n)
@@ -220,6 +222,7 @@ struct Tile {
           }
         }
       }
+      between(k);
     }
     if (!full) {
 #pragma unroll
@@ -463,7 +466,7 @@ __global__ void __launch_bounds__(256, 2) tree_attn_stream_kernel(TreeAttnArgs a
         }
       }
     }
-    t.step(a, ks, vs, full, bits);
+    t.step(a, ks, vs, full, bits, [](int) {});
   }
 
   if (__syncthreads_or(bad) && wave == 0) t.add_not_finite(a, s);
@@ -515,19 +518,29 @@ __global__ void __launch_bounds__(256, 2) tree_attn_tile_kernel(TreeAttnArgs a) 
   const bool active = first < s.nq;
   int pg = s.page(a, s.kbeg, KW);
   TileRows rows;
-  auto dma = [&](const char* p, char* dst) {
+  // Wave instruction c of a tile's K (c < NIN) or V.  No memory clobber: what reads these
+  // bytes stands behind the loop's wait and barrier, and the compiler is free to move the
+  // present tile's reads past this.
+  auto dma = [&](int c, int stage) {
+    const bool v = c >= NIN;
+    const int in = (v ? c - NIN : c) * 4 + wave, key = in * KPI + lane / CPR, j = lane % CPR;
+    const char* p = (v ? a.v + s.kvh * a.v_head : a.k + s.kvh * a.k_head) +
+                    (j ^ (v ? Tl::vswz(key) : Tl::kswz(key))) * 16 + (uint64_t)__shfl(v ? rows.v : rows.k, key) * a.unit;
+    char* dst = lds + (stage * 2 + (v ? 1 : 0)) * Tl::BYTES + in * 1024;
     const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void_t*)dst);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(p) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(p) : "m0");
+  };
+  // A CU takes one such instruction in 16 clocks: issued all at once behind the barrier,
+  // they hold up the four waves for 500, so they go between the matrix instructions.
+  constexpr int PER = (2 * NIN + Tl::NKS - 1) / Tl::NKS;
+  auto some_dma = [&](int k, int stage) {
+#pragma unroll
+    for (int c = k * PER; c < (k + 1) * PER; ++c)
+      if (c < 2 * NIN) dma(c, stage);
   };
   auto fetch = [&](int stage) {
-    char* ks = lds + stage * 2 * Tl::BYTES;
 #pragma unroll
-    for (int c = 0; c < NIN; ++c) {
-      const int in = c * 4 + wave, key = in * KPI + lane / CPR, j = lane % CPR;
-      dma(a.k + s.kvh * a.k_head + (j ^ Tl::kswz(key)) * 16 + (uint64_t)__shfl(rows.k, key) * a.unit, ks + in * 1024);
-      dma(a.v + s.kvh * a.v_head + (j ^ Tl::vswz(key)) * 16 + (uint64_t)__shfl(rows.v, key) * a.unit,
-          ks + Tl::BYTES + in * 1024);
-    }
+    for (int k = 0; k < Tl::NKS; ++k) some_dma(k, stage);
   };
   rows.set(a, s.kbeg, pg);
   if (s.kbeg < s.kend) fetch(0);
@@ -560,10 +573,10 @@ __global__ void __launch_bounds__(256, 2) tree_attn_tile_kernel(TreeAttnArgs a) 
     // this tile has landed, and the other stage has been read
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (k0 + KW < s.kend) {
+    const bool more = k0 + KW < s.kend;
+    if (more) {
       rows.set(a, k0 + KW, pg);
       load_words(k0 + KW);
-      fetch(stage ^ 1);
       pg = s.page(a, k0 + 2 * KW, KW);
     }
     if (there != Tl::ALL || k0 + KW > s.clear) {
@@ -585,8 +598,15 @@ __global__ void __launch_bounds__(256, 2) tree_attn_tile_kernel(TreeAttnArgs a) 
       for (int n = 0; n < NQ; ++n) any |= bits[n];
       some = __any(any != 0);
     }
-    if (active && some) t.step(a, ks, vs, full, bits);   // no query of the wave sees the tile: nothing to add
+    if (!active || !some) {   // no query of the wave sees the tile
+      if (more) fetch(stage ^ 1);
+    } else {
+      // the last tile asks for itself again: without a branch here the matrix
+      // instructions stay in one block (causal chunks 117 us with it, 107 without)
+      t.step(a, ks, vs, full, bits, [&](int k) { some_dma(k, stage ^ 1); });
+    }
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing is written to LDS behind the workgroup's end
   if (__syncthreads_or(bad)) t.add_not_finite(a, s);
   t.sum_lanes();
   if (!active) return;
