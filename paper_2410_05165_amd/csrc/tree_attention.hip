@@ -698,21 +698,36 @@ struct AttnPlan {
 
 AttnPlan plan_attention(const atspeed_tree_attention_args& a) {
   AttnPlan p{};
-  const int64_t nq = (int64_t)std::min(a.max_new, a.n_rows) * (a.n_heads / a.n_kv_heads);
   const bool bf = a.dtype == ATSPEED_BF16;
-  p.tile = nq <= 16 ? 16 : nq <= 32 && bf ? 32 : nq <= 64 || !bf ? 64 : 128;
-  p.qtiles = (int)((nq + p.tile - 1) / p.tile);
+  const int64_t nq = (int64_t)std::min(a.max_new, a.n_rows) * (a.n_heads / a.n_kv_heads);
+  const int64_t pairs = (int64_t)a.B * a.n_kv_heads;
   p.cap = (int)std::min<int64_t>((int64_t)a.max_pages * a.page_size, 1 << 30);
   const int64_t keys = std::max<int64_t>(1, std::min<int64_t>((int64_t)a.max_ctx + a.max_new, p.cap));
-  const int64_t base = (int64_t)a.B * a.n_kv_heads * p.qtiles;
+  // Queries of a workgroup: the smallest tile that holds them (fp32 has tiles of 16 and
+  // 64).  Launches that do not fill the CUs are bound by the steps each workgroup takes
+  // one after the other; over up to 1,024 keys they take the tiles of few queries, whose
+  // waves share the steps out, though these read the keys once for each (30 rows over 110
+  // keys of d_head 32: 7.2 us in tiles of 64, 5.0 in tiles of 16; 27 rows over 526 keys 21
+  // and 13; but 102 rows x 29 users over 128 keys, 464 workgroups of 32, 11.1 and 13.1).
+  const int few = bf ? 32 : 16;
+  p.tile = nq <= 16 ? 16 : nq <= few ? few : nq <= 64 || !bf ? 64 : 128;
+  if (p.tile > few && keys <= 1024 && pairs * ((nq + few - 1) / few) <= 256) p.tile = few;
+  p.qtiles = (int)((nq + p.tile - 1) / p.tile);
   // Keys are split until the launch has 8 workgroups for each of the 256 CUs, 32 of the
   // short ones of few queries: the bounds count every context as the longest, and what
   // ragged contexts leave over is spread evenly only if the pieces are many (64 single
   // tokens over up to 8,192 keys: 208 us with 2,048, 175 with 4,096, 155 with 8,192; trees
   // over up to 65,536 keys: 171 us with 1,024, 158 with 2,048, 199 with 4,096, where the
-  // join of the pieces costs more than the spread gains).
-  const int64_t want = std::max<int64_t>(1, (p.tile <= 32 ? 8192 : 2048) / base);
-  p.chunk = (int)std::max<int64_t>(256, ((keys + want - 1) / want + 127) / 128 * 128);
+  // join of the pieces costs more than the spread gains).  Pieces of under 256 keys lose
+  // to their join (78 rows x 7 users over 1,970 keys: 27 us with 256, 31 with 128), and
+  // so does any split of up to 10 steps (4 rows x 8 users over 600 keys: 10.2 us in
+  // pieces, 8.3 whole; 256 rows x 8 users over 310 keys 31 and 14; but 12 rows x 2 users
+  // over 2,012 keys, 32 steps, 16.5 and 51).
+  const int64_t base = pairs * p.qtiles, want = std::max<int64_t>(1, (p.tile <= 32 ? 8192 : 2048) / base);
+  const int step = p.tile <= 32 ? (bf ? 128 : 64) : std::min(64, (p.tile / 64) * 8192 / (a.d_head * (bf ? 2 : 4)));
+  int64_t chunk = std::max<int64_t>(256, ((keys + want - 1) / want + 127) / 128 * 128);
+  if (keys <= 10 * step) chunk = keys;
+  p.chunk = (int)chunk;
   p.splits = (int)((keys + p.chunk - 1) / p.chunk);
   const size_t rows = (size_t)p.splits * a.n_rows * a.n_heads;
   p.part_bytes = p.splits > 1 ? rows * a.d_head * sizeof(float) : 0;
