@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Dict, Optional
 
 import numpy as np
@@ -78,10 +79,22 @@ class AlignArgs(C.Structure):
 
 
 def _struct(name, spec):
-    """A ctypes structure from "type: name name ..." groups in the header's field order."""
-    kinds = {"i": C.c_int32, "l": C.c_int64, "f": C.c_float, "p": C.c_void_p}
-    fields = [(n, kinds[part.split(":")[0].strip()]) for part in spec.split(";") for n in part.split(":")[1].split()]
-    return type(name, (C.Structure,), {"_fields_": fields})
+    """A ctypes structure from "type: name name ..." groups in the header's field order.
+
+    ``pack(*values)`` gives its bytes (pointers as integers, 0 for null) in a quarter of the time that an
+    instance takes to fill: these calls come once a layer.
+    """
+    kinds = {"i": (C.c_int32, "i"), "l": (C.c_int64, "q"), "f": (C.c_float, "f"), "p": (C.c_void_p, "P")}
+    parts = [(n, kinds[part.split(":")[0].strip()]) for part in spec.split(";") for n in part.split(":")[1].split()]
+    layout = struct.Struct("@" + "".join(code for _, (_, code) in parts))
+
+    def pack(*values):
+        try:
+            return layout.pack(*values)
+        except struct.error as e:
+            raise ValueError(f"{name}: {e}") from None
+
+    return type(name, (C.Structure,), {"_fields_": [(n, kind) for n, (kind, _) in parts], "pack": staticmethod(pack)})
 
 
 # Arguments of the context-free calls (atspeed_pages members are spelled out).
@@ -138,11 +151,12 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
     lib.atspeed_align_step.argtypes = [vp, C.POINTER(AlignArgs), C.POINTER(C.c_double)]
     lib.atspeed_target_search.argtypes = [vp, i32, i32, pi32, pi32, pf, pi32, pi32, pi32, pi32]
     lib.atspeed_mixed_search.argtypes = [vp, C.c_float, i32, i32, pi32, pi32, pf, pi32, pi32, pi32, pi32]
-    lib.atspeed_page_plan.argtypes = [C.POINTER(PagePlanArgs), vp]
-    lib.atspeed_kv_append.argtypes = [C.POINTER(KvAppendArgs), vp]
-    lib.atspeed_tree_attention_workspace_bytes.argtypes = [C.POINTER(TreeAttentionArgs), C.POINTER(C.c_size_t)]
-    lib.atspeed_tree_attention.argtypes = [C.POINTER(TreeAttentionArgs), vp, C.c_size_t, vp]
-    lib.atspeed_logit_rules.argtypes = [C.POINTER(LogitRulesArgs), vp]
+    # the argument structures: by reference, or their bytes
+    lib.atspeed_page_plan.argtypes = [vp, vp]
+    lib.atspeed_kv_append.argtypes = [vp, vp]
+    lib.atspeed_tree_attention_workspace_bytes.argtypes = [vp, C.POINTER(C.c_size_t)]
+    lib.atspeed_tree_attention.argtypes = [vp, vp, C.c_size_t, vp]
+    lib.atspeed_logit_rules.argtypes = [vp, vp]
     for name in SYMBOLS:
         fn = getattr(lib, name)
         if fn.restype is C.c_int:  # default

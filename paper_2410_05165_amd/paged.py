@@ -30,7 +30,7 @@ def _library():
 
 def _call(fn, args, device, *more):
     """fn(args, *more, stream) on the current stream of GPU `device` (its index)."""
-    if device == torch.cuda.current_device():
+    if device == torch._C._cuda_getDevice():
         status = fn(args, *more, torch._C._cuda_getCurrentRawStream(device))
     else:
         with torch.cuda.device(device):
@@ -40,9 +40,9 @@ def _call(fn, args, device, *more):
 
 
 def _want(t, name, dtype, shape, device):
-    """The address of a contiguous tensor of this type and shape on GPU `device` (None: none)."""
+    """The address of a contiguous tensor of this type and shape on GPU `device` (None: null)."""
     if t is None:
-        return None
+        return 0
     if t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous():
         return t.data_ptr()
     raise ValueError(f"{name}: want a contiguous {dtype} {tuple(shape)} on GPU {device}, got {t.dtype} "
@@ -60,8 +60,8 @@ def _rows(t, name, shape, dtype, device):
     """(address, row stride, head stride) of [rows, heads, d_head] with any row and head strides."""
     if t.shape == shape and t.dtype is dtype and t.get_device() == device:
         row, head, one = t.stride()
-        if one == 1:
-            return t.data_ptr(), row, head
+        if one == 1:   # the stride of a dimension of one element says nothing
+            return t.data_ptr(), row if shape[0] > 1 else 0, head if shape[1] > 1 else 0
     raise ValueError(f"{name}: want {dtype} {tuple(shape)} on GPU {device}, the last dimension contiguous")
 
 
@@ -72,6 +72,9 @@ def _caches(k_cache, v_cache):
         raise ValueError("k_cache: want float32 or bfloat16 [pages, page_size, kv_heads, d_head]")
     *ks, k1 = k_cache.stride()
     *vs, v1 = v_cache.stride()
+    for i in range(3):
+        if shape[i] == 1:   # the stride of a dimension of one element says nothing
+            ks[i] = vs[i] = 0
     if v_cache.shape != shape or v_cache.dtype is not dtype or v_cache.get_device() != device or k1 != 1 or v1 != 1:
         raise ValueError("the caches want one type, shape and device, the last dimension contiguous")
     return device, (k_cache.data_ptr(), *ks), (v_cache.data_ptr(), *vs)
@@ -110,11 +113,11 @@ def atspeed_page_plan(held, keep, add, block_table, free_pages, n_free, page_siz
             raise ValueError("parent: want [B, max_nodes]")
         nodes = parent.shape[1]
     buf = torch.empty(4 * (B + max_rows) + 2, dtype=i32, device=where)
-    out = buf.split_with_sizes([1, B, B, B, B + 1, max_rows, max_rows, max_rows, max_rows])
+    out = buf.unsafe_split_with_sizes([1, B, B, B, B + 1, max_rows, max_rows, max_rows, max_rows])   # no autograd here
     mask = torch.empty((max_rows, (nodes + 63) // 64), dtype=torch.int64, device=where) if parent is not None else None
     at = buf.data_ptr()
     row = at + 4 * (4 * B + 2)
-    args = PagePlanArgs(B, page_size, most, free_pages.numel(), max_rows, nodes,
+    args = PagePlanArgs.pack(B, page_size, most, free_pages.numel(), max_rows, nodes,
                         _want(held, "held", i32, (B,), dev), _want(keep, "keep", i32, (B,), dev),
                         _want(add, "add", i32, (B,), dev), _want(parent, "parent", i32, (B, nodes), dev),
                         _want(block_table, "block_table", i32, (B, most), dev),
@@ -122,7 +125,7 @@ def atspeed_page_plan(held, keep, add, block_table, free_pages, n_free, page_siz
                         _want(n_free, "n_free", i32, (1,), dev),
                         at, at + 4, at + 4 * (B + 1), at + 4 * (2 * B + 1), at + 4 * (3 * B + 1),
                         row, row + 4 * max_rows, row + 8 * max_rows, row + 12 * max_rows,
-                        mask.data_ptr() if mask is not None else None)
+                        mask.data_ptr() if mask is not None else 0)
     _call(_library().atspeed_page_plan, args, dev)
     return StepPlan(*out, mask)
 
@@ -138,7 +141,7 @@ def atspeed_kv_append(k, v, k_cache, v_cache, slot):
     shape = (n, heads, dh)
     k_at, k_row, k_head = _rows(k, "k", shape, dtype, dev)
     v_at, v_row, v_head = _rows(v, "v", shape, dtype, dev)
-    args = KvAppendArgs(DTYPES[dtype], n, heads, dh, page, pool, k_at, v_at, k_row, k_head, v_row, v_head, *kc, *vc,
+    args = KvAppendArgs.pack(DTYPES[dtype], n, heads, dh, page, pool, k_at, v_at, k_row, k_head, v_row, v_head, *kc, *vc,
                         _want(slot, "slot", torch.int32, (n,), dev))
     _call(_library().atspeed_kv_append, args, dev)
 
@@ -166,12 +169,12 @@ def atspeed_tree_attention(q, k_cache, v_cache, block_table, row_off, ctx, max_c
     lse = torch.empty((rows, heads), dtype=torch.float32, device=q.device) if return_lse else None
     B, most = block_table.shape
     words = 0 if mask is None else mask.shape[-1]
-    args = TreeAttentionArgs(DTYPES[dtype], B, rows, heads, kv_heads, dh, page, most, pool, max_ctx, max_new, words,
+    args = TreeAttentionArgs.pack(DTYPES[dtype], B, rows, heads, kv_heads, dh, page, most, pool, max_ctx, max_new, words,
                              1.0 / math.sqrt(dh) if scale is None else scale, *q_at, *kc, *vc,
                              _want(block_table, "block_table", i32, (B, most), dev),
                              _want(row_off, "row_off", i32, (B + 1,), dev), _want(ctx, "ctx", i32, (B,), dev),
                              _want(mask, "mask", torch.int64, (rows, words), dev), *o_at,
-                             lse.data_ptr() if return_lse else None)
+                             lse.data_ptr() if return_lse else 0)
     lib, need = _library(), C.c_size_t(0)
     status = lib.atspeed_tree_attention_workspace_bytes(args, need)
     if status != 0:
@@ -215,7 +218,7 @@ def atspeed_logit_rules(logits, row_off, token_base: int = 0, history=None, hist
     if bias is not None and (bias.dtype is not f32 or bias.get_device() != dev or bias.shape != (n_bias, cols) or
                              (cols > 1 and bias.stride(1) != 1)):
         raise ValueError("bias: want float32 [n, cols] on the logits' device, rows contiguous")
-    args = LogitRulesArgs(DTYPES[logits.dtype], B, rows, cols, token_base, hist, nodes, words, n_bias, states,
+    args = LogitRulesArgs.pack(DTYPES[logits.dtype], B, rows, cols, token_base, hist, nodes, words, n_bias, states,
                           flat.shape[0], mask_value, logits.data_ptr(), logits.stride(0), flat.data_ptr(),
                           flat.stride(0), _want(out_row, "out_row", i32, (rows,), dev),
                           _want(row_off, "row_off", i32, (B + 1,), dev), _want(history, "history", i32, (B, hist), dev),
@@ -224,7 +227,7 @@ def atspeed_logit_rules(logits, row_off, token_base: int = 0, history=None, hist
                           _want(mask, "mask", torch.int64, (rows, words), dev),
                           _want(repetition, "repetition", f32, vec, dev), _want(frequency, "frequency", f32, vec, dev),
                           _want(presence, "presence", f32, vec, dev), _want(temperature, "temperature", f32, vec, dev),
-                          bias.data_ptr() if bias is not None else None, bias.stride(0) if bias is not None else 0,
+                          bias.data_ptr() if bias is not None else 0, bias.stride(0) if bias is not None else 0,
                           _want(bias_index, "bias_index", i32, vec, dev),
                           _want(allowed, "allowed", i32, (states, (cols + 31) // 32), dev),
                           _want(state, "state", i32, (rows,), dev))

@@ -395,6 +395,59 @@ def test_attention_strides_scale_and_place(dtype, dh):
     assert int(wide[:, :3].count_nonzero()) == 0 and int(wide[:, 9:].count_nonzero()) == 0
 
 
+@pytest.mark.parametrize("dtype,dh", [(BF16, 128), (F32, 32)])
+def test_attention_of_scale_zero_is_the_mean(dtype, dh):
+    c = attention_case(23, [70, 3], [40, 2], 4, 2, dh, 16, dtype, True)
+    close_to_exact(c, *atspeed_tree_attention(**c, scale=0.0, return_lse=True), scale=0.0)
+
+
+@pytest.mark.parametrize("dtype,dh", [(BF16, 128), (F32, 64)])
+@pytest.mark.parametrize("new", [1, 40])
+def test_attention_stays_inside_for_nonsense_lengths(dtype, dh, new):
+    """Row offsets, contexts and pages hold garbage: no access leaves the buffers, rows of sane requests are right."""
+    c = attention_case(24, [100, 50, 3000], [new, new, new], 4, 2, dh, 16, dtype, True)
+    want = atspeed_tree_attention(**c)
+    rng = np.random.default_rng(3)
+    for off in ([0, new, -5, 3 * new], [0, 2 ** 31 - 1, -2 ** 31, 7], [-9, new, 2 * new, 3 * new], [5, 4, 3, 2]):
+        for ctx in (c["ctx"], ints([2 ** 31 - 1, -2 ** 31, 10 ** 9])):
+            bad = dict(c, row_off=ints(off), ctx=ctx, block_table=ints(rng.integers(-2 ** 31, 2 ** 31, c["block_table"].shape)))
+            atspeed_tree_attention(**bad)
+            atspeed_tree_attention(**dict(bad, mask=None))
+    got = atspeed_tree_attention(**dict(c, row_off=ints([0, new, 2 * new, -7])))
+    assert torch.equal(got[:2 * new], want[:2 * new])
+
+
+def test_attention_with_parts_in_a_graph():
+    """A split context in two captured graphs that replay in turn: each equals its eager call."""
+    cases = [attention_case(81 + i, [9000, 40, 2500], [5, 3, 6], 8, 2, 128, 16, BF16, True) for i in range(2)]
+    want = [atspeed_tree_attention(**c, return_lse=True) for c in cases]
+    torch.cuda.synchronize()
+    graphs, got = [torch.cuda.CUDAGraph() for _ in cases], []
+    for g, c in zip(graphs, cases):
+        with torch.cuda.graph(g):
+            got.append(atspeed_tree_attention(**c, return_lse=True))
+    for _ in range(3):
+        for g, x, w in zip(graphs, got, want):
+            for t in x:
+                t.zero_()
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(x[0], w[0]) and torch.equal(x[1], w[1])
+
+
+def test_strides_of_dimensions_of_one_element_do_not_matter():
+    c = attention_case(22, [20], [1], 1, 1, 64, 32, BF16, False)
+    odd = lambda t, *s: torch.as_strided(t, t.shape, s)  # noqa: E731
+    want = atspeed_tree_attention(**c)
+    assert c["k_cache"].shape[2] == 1
+    got = atspeed_tree_attention(**dict(c, q=odd(c["q"], 3, 5, 1), k_cache=odd(c["k_cache"], *c["k_cache"].stride()[:2], 7, 1)))
+    assert torch.equal(got, want)
+    k = torch.randn((1, 1, 64), device=DEV).to(BF16)
+    a, b = (torch.zeros((4, 8, 1, 64), dtype=BF16, device=DEV) for _ in range(2))
+    atspeed_kv_append(odd(k, 1, 3, 1), k, odd(a, 512, 64, 9, 1), b, ints([9]))
+    assert torch.equal(a[1, 1], k[0]) and torch.equal(b, a)
+
+
 def test_attention_leaves_other_rows_alone():
     c = attention_case(8, [40, 9], [7, 5], 4, 2, 128, 16, BF16, True, spare=6)
     out = torch.full_like(c["q"], 3.0)
@@ -624,6 +677,8 @@ def test_refusals_of_tensors():
     for kw in bad:
         with pytest.raises(ValueError):
             atspeed_tree_attention(**dict(c, **kw))
+    with pytest.raises(ValueError):
+        atspeed_tree_attention(**dict(c, max_ctx=2 ** 40))
     r = rules_case(1, 2, [1, 1], 50, F32)
     for kw in (dict(logits=r["logits"].double()), dict(state=r["state"][:1]), dict(bias=r["bias"][:, :49]),
                dict(allowed=r["allowed"][:, :1]), dict(history=r["history"].long()), dict(out_row=ints([0, 1]))):
