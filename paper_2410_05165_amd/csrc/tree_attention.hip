@@ -250,8 +250,12 @@ struct Tile {
 #pragma unroll
         for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (!((mine >> (kb * 16 + i)) & 1)) sc[n][kb][i] = -INFINITY;
+          for (int i = 0; i < 4; ++i) {   // a set bit keeps the score, a clear one makes it -inf
+            const uint32_t half = (uint32_t)(kb < 2 ? mine : mine >> 32);
+            const uint32_t keep = (uint32_t)((int32_t)(half << (31 - (kb & 1) * 16 - i)) >> 31);
+            const uint32_t x = __float_as_uint(sc[n][kb][i]);
+            sc[n][kb][i] = __uint_as_float((x & keep) | (0xff800000u & ~keep));
+          }
       }
     }
     float mx[NQ];
@@ -339,14 +343,21 @@ struct Tile {
   // times such a value is not 0, so in tiles that not every query sees whole they are
   // left out of the product.
   static __device__ __forceinline__ bool finite(u32x4_t& w) {
-    bool bad = false;
+    // an exponent of all ones overflows into the sign's place when one is added to it
+    constexpr uint32_t EXP = BF ? 0x7f807f80u : 0x7f800000u, ONE = BF ? 0x00800080u : 0x00800000u;
+    uint32_t over = 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if constexpr (BF) {
-        if ((w[e] & 0x7f800000u) == 0x7f800000u) { w[e] &= 0x0000ffffu; bad = true; }
-        if ((w[e] & 0x00007f80u) == 0x00007f80u) { w[e] &= 0xffff0000u; bad = true; }
-      } else {
-        if ((w[e] & 0x7f800000u) == 0x7f800000u) { w[e] = 0u; bad = true; }
+    for (int e = 0; e < 4; ++e) over |= (w[e] & EXP) + ONE;
+    const bool bad = (over & ~(EXP | (BF ? 0x007f007fu : 0x007fffffu))) != 0;
+    if (bad) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (BF) {
+          if ((w[e] & 0x7f800000u) == 0x7f800000u) w[e] &= 0x0000ffffu;
+          if ((w[e] & 0x00007f80u) == 0x00007f80u) w[e] &= 0xffff0000u;
+        } else {
+          if ((w[e] & 0x7f800000u) == 0x7f800000u) w[e] = 0u;
+        }
       }
     }
     return bad;
@@ -540,14 +551,17 @@ __global__ void __launch_bounds__(256, 2) tree_attn_tile_kernel(TreeAttnArgs a) 
   // Wave instruction c of a tile's K (c < NIN) or V.  No memory clobber: what reads these
   // bytes stands behind the loop's wait and barrier, and the compiler is free to move the
   // present tile's reads past this.
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void_t*)lds;
+  const int key0 = wave * KPI + lane / CPR;   // key of the lane in instruction 0; the next one's is 4 KPI on
   auto dma = [&](int c, int stage) {
     const bool v = c >= NIN;
-    const int in = (v ? c - NIN : c) * 4 + wave, key = in * KPI + lane / CPR, j = lane % CPR;
+    const int in = v ? c - NIN : c, key = key0 + in * 4 * KPI, j = lane % CPR;
+    const uint32_t row = __builtin_amdgcn_ds_bpermute(key0 * 4 + in * 16 * KPI, v ? rows.v : rows.k);
     const char* p = (v ? a.v + s.kvh * a.v_head : a.k + s.kvh * a.k_head) +
-                    (j ^ (v ? Tl::vswz(key) : Tl::kswz(key))) * 16 + (uint64_t)__shfl(v ? rows.v : rows.k, key) * a.unit;
-    char* dst = lds + (stage * 2 + (v ? 1 : 0)) * Tl::BYTES + in * 1024;
-    const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void_t*)dst);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(p) : "m0");
+                    (j ^ (v ? Tl::vswz(key) : Tl::kswz(key))) * 16 + (uint64_t)row * a.unit;
+    const uint32_t at = lds0 + (stage * 2 + (v ? 1 : 0)) * Tl::BYTES + (in * 4 + wave) * 1024;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                 ::"s"(__builtin_amdgcn_readfirstlane(at)), "v"(p) : "m0");
   };
   // A CU takes one such instruction in 16 clocks: issued all at once behind the barrier,
   // they hold up the four waves for 500, so they go between the matrix instructions.
