@@ -634,11 +634,13 @@ ATSPEED_API atspeed_status atspeed_tree_attention(const atspeed_tree_attention_a
  *     paths of mask [n_rows, mask_words] (nullable).
  *   bias [n_bias, n_cols] fp32, rows bias_stride apart; bias_index [B], none where it is
  *     outside 0 .. n_bias - 1 (null: every request takes row 0).
- *   allowed [n_states, ceil(n_cols / 32)] uint32; state [n_rows]: a negative state
- *     allows every column, one from n_states on none.
+ *   allowed [n_states, ceil(n_cols / 32)] uint32; state [n_rows], or with
+ *     state_by_request [B]: a negative state allows every column, one from n_states on
+ *     none.
  * repetition and temperature must be positive.  B 1..1024, n_cols 1..2^20. */
 typedef struct {
-  int32_t dtype, B, n_rows, n_cols, token_base, max_hist, max_nodes, mask_words, n_bias, n_states, n_out_rows;
+  int32_t dtype, B, n_rows, n_cols, token_base, max_hist, max_nodes, mask_words, n_bias, n_states, n_out_rows,
+      state_by_request;
   float mask_value;
   const void* logits;
   int64_t logits_stride;
@@ -661,6 +663,24 @@ typedef struct {
   const int32_t* state;
 } atspeed_logit_rules_args;
 ATSPEED_API atspeed_status atspeed_logit_rules(const atspeed_logit_rules_args* args, void* stream);
+
+/* Rules on the item logits of a context's own forwards: from the next forward on the
+ * target's and the draft's logits pass atspeed_logit_rules before their log-softmax, so
+ * prefill, draft, verify, tree_logits, decode_topk and the searches rank, accept and
+ * return what the rules leave of them (logits_dev outputs and atspeed_logprobs too).  The
+ * call ends the present batch: a prefill comes next.  The lists of a strict decode are
+ * those of atspeed_target_search under the same rules.  rules (nullable: no rules from
+ * here on) is copied, its buffers stay the caller's and are read by every forward; request
+ * b is user b of the batch, history [max_batch, max_hist] and the other arrays likewise.
+ * Used are history, hist_len, max_hist, repetition, frequency, presence, temperature,
+ * bias, bias_stride, bias_index, n_bias, allowed with state [max_batch], n_states and
+ * mask_value; every other pointer must be null, n_cols L*codebook and token_base the
+ * target's item_base (a column is an item code's token).  mask_value must be finite:
+ * masked codes rank behind all others and are listed only where those run out.
+ * ATSPEED_E_INVALID otherwise; ATSPEED_E_STATE from atspeed_align_data and
+ * atspeed_align_step while rules are set (their gradient is that of the plain logits).
+ * atspeed_accept takes the caller's logits as they are. */
+ATSPEED_API atspeed_status atspeed_set_logit_rules(atspeed_ctx* ctx, const atspeed_logit_rules_args* rules);
 
 #ifdef __cplusplus
 }

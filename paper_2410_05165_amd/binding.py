@@ -26,7 +26,8 @@ SYMBOLS = ("atspeed_workspace_bytes", "atspeed_create", "atspeed_destroy", "atsp
            "atspeed_accept", "atspeed_accept_noalloc", "atspeed_decode_topk", "atspeed_logprobs", "atspeed_get_state", "atspeed_set_state",
            "atspeed_set_timing", "atspeed_get_timing", "atspeed_align_data", "atspeed_align_step",
            "atspeed_target_search", "atspeed_mixed_search", "atspeed_page_plan", "atspeed_kv_append",
-           "atspeed_tree_attention_workspace_bytes", "atspeed_tree_attention", "atspeed_logit_rules")
+           "atspeed_tree_attention_workspace_bytes", "atspeed_tree_attention", "atspeed_logit_rules",
+           "atspeed_set_logit_rules")
 KERNEL_CLASSES = ("qkv", "o", "gu", "down", "lm_head", "attention", "row", "select")
 
 
@@ -109,7 +110,7 @@ TreeAttentionArgs = _struct("TreeAttentionArgs", """i: dtype B n_rows n_heads n_
     p: k_data; l: k_page k_token k_head; p: v_data; l: v_page v_token v_head; p: block_table row_off ctx mask out;
     l: out_row_stride out_head_stride; p: lse""")
 LogitRulesArgs = _struct("LogitRulesArgs", """i: dtype B n_rows n_cols token_base max_hist max_nodes mask_words n_bias
-       n_states n_out_rows; f: mask_value; p: logits; l: logits_stride; p: out; l: out_stride;
+       n_states n_out_rows state_by_request; f: mask_value; p: logits; l: logits_stride; p: out; l: out_stride;
     p: out_row row_off history hist_len node_token mask repetition frequency presence temperature bias;
     l: bias_stride; p: bias_index allowed state""")
 
@@ -157,6 +158,7 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
     lib.atspeed_tree_attention_workspace_bytes.argtypes = [vp, C.POINTER(C.c_size_t)]
     lib.atspeed_tree_attention.argtypes = [vp, vp, C.c_size_t, vp]
     lib.atspeed_logit_rules.argtypes = [vp, vp]
+    lib.atspeed_set_logit_rules.argtypes = [vp, vp]
     for name in SYMBOLS:
         fn = getattr(lib, name)
         if fn.restype is C.c_int:  # default
@@ -320,6 +322,22 @@ class Engine:
         loss = C.c_double(0.0)
         self._check(self.lib.atspeed_align_step(self.ctx, C.byref(args), C.byref(loss)))
         return loss.value
+
+    def atspeed_set_logit_rules(self, **rules):
+        """Rules on the item logits of every forward from here on (none given: no rules).
+
+        history [max_batch, n], hist_len, repetition, frequency, presence, temperature, bias [n, L*codebook] with
+        bias_index, allowed [n, ceil(L*codebook / 32)] with state, as paged.atspeed_logit_rules takes them with
+        max_batch requests; mask_value (default -1e4).  The tensors are held until the next call.
+        """
+        if not rules:
+            self._check(self.lib.atspeed_set_logit_rules(self.ctx, None))
+            self._rules = None
+            return
+        from .paged import pack_rules
+        args = pack_rules(self.n_item, self.w.target.item_base, self.cfg.max_batch, self.device, **rules)
+        self._check(self.lib.atspeed_set_logit_rules(self.ctx, args))
+        self._rules = rules
 
     def atspeed_get_state(self, B: int):
         K, L = self.w.K, self.w.L

@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(kRuleThreads) logit_rules_kernel(atspeed_logit
       for (int e = 0; e < VEC; ++e) x[k][e] = c + e < a.n_cols ? St<T>::ld(in + c + e) : 0.f;
     }
   }
-  const int state = a.allowed ? a.state[r] : -1;
+  int state = a.allowed && !a.state_by_request ? a.state[r] : -1;
   const int orow = a.out_row ? a.out_row[r] : r;
   const bool counting = (a.repetition || a.frequency || a.presence) && (a.history || a.node_token);
   if (counting)
@@ -94,6 +94,7 @@ __global__ void __launch_bounds__(kRuleThreads) logit_rules_kernel(atspeed_logit
   const float temp_inv = a.temperature ? 1.f / a.temperature[b] : 1.f;
   const int bi = a.bias ? (a.bias_index ? a.bias_index[b] : 0) : -1;
   const float* bias = bi >= 0 && bi < a.n_bias ? a.bias + (int64_t)bi * a.bias_stride : nullptr;
+  if (a.allowed && a.state_by_request) state = a.state[b];
   const bool masked = state >= 0;
   const uint32_t* allowed = masked && state < a.n_states ? a.allowed + (int64_t)state * ((a.n_cols + 31) / 32) : nullptr;
   float* out = a.out + (int64_t)orow * a.out_stride;
@@ -156,6 +157,17 @@ static atspeed_status run_rules(const atspeed_logit_rules_args& a, bool vec, hip
   return small ? launch_rules<T, 1, 4>(a, st) : launch_rules<T, 1, 16>(a, st);
 }
 
+// What the rules themselves need: the pointers that go together, and their counts.
+atspeed_status check_rules(const atspeed_logit_rules_args& a) {
+  if ((a.history != nullptr) != (a.hist_len != nullptr)) return fail(ATSPEED_E_INVALID, "history and hist_len go together");
+  if (a.history && a.max_hist < 1) return fail(ATSPEED_E_INVALID, "max_hist must be >= 1");
+  if (a.bias && a.n_bias < 1) return fail(ATSPEED_E_INVALID, "n_bias must be >= 1");
+  if ((a.allowed != nullptr) != (a.state != nullptr)) return fail(ATSPEED_E_INVALID, "allowed and state go together");
+  if (a.allowed && a.n_states < 1) return fail(ATSPEED_E_INVALID, "n_states must be >= 1");
+  if (a.bias && a.bias_stride < a.n_cols) return fail(ATSPEED_E_SHAPE, "a row stride is below n_cols");
+  return ATSPEED_OK;
+}
+
 }  // namespace atspeed
 
 using namespace atspeed;
@@ -169,15 +181,11 @@ extern "C" atspeed_status atspeed_logit_rules(const atspeed_logit_rules_args* ar
   if (a.n_cols < 1 || a.n_cols > (1 << 20)) return fail(ATSPEED_E_INVALID, "n_cols must be 1..2^20");
   if (a.n_rows == 0) return ATSPEED_OK;
   if (!a.logits || !a.out || !a.row_off) return fail(ATSPEED_E_INVALID, "logit rules: null pointer");
-  if ((a.history != nullptr) != (a.hist_len != nullptr)) return fail(ATSPEED_E_INVALID, "history and hist_len go together");
-  if (a.history && a.max_hist < 1) return fail(ATSPEED_E_INVALID, "max_hist must be >= 1");
+  ST_TRY(check_rules(a));
   if (a.node_token && a.max_nodes < 1) return fail(ATSPEED_E_INVALID, "max_nodes must be >= 1");
   if (a.node_token && a.mask && a.mask_words < 1) return fail(ATSPEED_E_INVALID, "mask_words must be >= 1");
-  if (a.bias && a.n_bias < 1) return fail(ATSPEED_E_INVALID, "n_bias must be >= 1");
-  if ((a.allowed != nullptr) != (a.state != nullptr)) return fail(ATSPEED_E_INVALID, "allowed and state go together");
-  if (a.allowed && a.n_states < 1) return fail(ATSPEED_E_INVALID, "n_states must be >= 1");
   if (a.out_row && a.n_out_rows < 1) return fail(ATSPEED_E_INVALID, "n_out_rows must be >= 1");
-  if (a.logits_stride < a.n_cols || a.out_stride < a.n_cols || (a.bias && a.bias_stride < a.n_cols))
+  if (a.logits_stride < a.n_cols || a.out_stride < a.n_cols)
     return fail(ATSPEED_E_SHAPE, "a row stride is below n_cols");
   if ((const void*)a.out == a.logits &&
       (a.dtype != ATSPEED_FP32 || a.out_row || a.out_stride != a.logits_stride))

@@ -140,6 +140,10 @@ struct atspeed_ctx {
   int* fidx = nullptr;             // [B*Tmax] per user, the nodes still to forward
   int* fcnt = nullptr;             // [B]
   int64_t rows_fwd = 0;            // target tree rows forwarded (decode statistics)
+  // rules on the logits of every forward (atspeed_set_logit_rules)
+  bool ruled = false;
+  atspeed_logit_rules_args rules{};
+  int* one_each = nullptr;         // [B + 1] 0, 1, 2, ...: one row a user
   // residual-stream capture of the next target forward (atspeed_capture_hidden)
   float* cap_x = nullptr;        // [2 n_layers + 1][cap_rows][d] fp32
   bf16_t* cap_act = nullptr;     // bf16 inputs of every GEMM and attention (layout at atspeed_capture_hidden)
@@ -430,6 +434,7 @@ void layout(atspeed_ctx& c, const atspeed_config& cfg, int trie_nodes, Arena& a)
   c.root_h = a.take<char>((size_t)B * std::max(cfg.draft.d_model, 1) * es);
   c.align_kslot = a.take<int>((size_t)B * L);
   c.loss_rows = a.take<float>(M);
+  c.one_each = a.take<int>(B + 1);
 }
 
 atspeed_status bind_weights(ModelRt& r, const atspeed_weights* w, const char* who) {
@@ -593,6 +598,12 @@ atspeed_status forward(atspeed_ctx& c, ModelRt& r, bool prefill, int Mmax, int T
   MARK_F(ATSPEED_K_LMHEAD, 2.0 * Mmf * c.nitem * d);
   HIP_TRY(gemm(g, st));
   MARK(ATSPEED_K_ROW);
+  if (c.ruled) {
+    atspeed_logit_rules_args ra = c.rules;
+    ra.B = B; ra.n_rows = Mmf; ra.logits = ra.out = c.logits; ra.logits_stride = ra.out_stride = c.nitem;
+    ra.row_off = prefill ? c.one_each : c.rows.user_off;
+    ST_TRY(atspeed_logit_rules(&ra, st));
+  }
   if (prefill) HIP_TRY(log_softmax_rows(c.logits, c.Mb, B, c.nitem, nullptr, r.root, dbg, st));
   else HIP_TRY(log_softmax_rows(c.logits, c.rows.M, Mmax, c.nitem, c.rows.slot, r.lp, dbg, st));
   MARK(-1);
@@ -745,6 +756,9 @@ atspeed_status atspeed_create(const atspeed_config* cfg, const atspeed_weights* 
   if (e == hipSuccess) e = hipMemsetAsync(c->state.t, 0, sizeof(int) * cfg->max_batch, c->st);
   if (e == hipSuccess) e = hipMemsetAsync(c->state.steps, 0, sizeof(int) * cfg->max_batch, c->st);
   if (e == hipSuccess) e = hipMemsetAsync(c->tree.n_nodes, 0, sizeof(int) * cfg->max_batch, c->st);
+  std::vector<int> one_each(cfg->max_batch + 1);
+  for (int b = 0; b <= cfg->max_batch; ++b) one_each[b] = b;
+  if (e == hipSuccess) e = hipMemcpyAsync(c->one_each, one_each.data(), one_each.size() * 4, hipMemcpyHostToDevice, c->st);
   if (e == hipSuccess) e = hipStreamSynchronize(c->st);
   if (e != hipSuccess) return bail(fail(ATSPEED_E_DEVICE, std::string("create: ") + hipGetErrorString(e)));
   s = upload_rope(*c, c->tgt);
@@ -804,6 +818,27 @@ static atspeed_status prefill_impl(atspeed_ctx* c, int32_t B, int32_t P, const i
   c->drafted = false;
   c->carry_ok = false;
   c->align_ready = false;
+  return ATSPEED_OK;
+}
+
+atspeed_status atspeed_set_logit_rules(atspeed_ctx* c, const atspeed_logit_rules_args* rules) {
+  if (!c) return fail(ATSPEED_E_INVALID, "ctx is null");
+  atspeed_logit_rules_args ra{};
+  if (rules) {
+    ra = *rules;
+    if (ra.logits || ra.out || ra.out_row || ra.row_off || ra.node_token || ra.mask)
+      return fail(ATSPEED_E_INVALID, "logit rules of a context: the logits, rows and tree are the context's own");
+    if (ra.n_cols != c->nitem || ra.token_base != c->cfg.target.item_base)
+      return fail(ATSPEED_E_SHAPE, "logit rules of a context: n_cols is L*codebook and token_base the item_base");
+    if (!std::isfinite(ra.mask_value)) return fail(ATSPEED_E_INVALID, "logit rules of a context: mask_value must be finite");
+    ST_TRY(check_rules(ra));
+    ra.dtype = ATSPEED_FP32;
+    ra.state_by_request = 1;
+  }
+  c->rules = ra;
+  c->ruled = rules != nullptr;
+  // the root log-probs and the trees are of the rules before
+  c->prefilled = c->dft_prefilled = c->drafted = c->carry_ok = c->align_ready = false;
   return ATSPEED_OK;
 }
 
@@ -1153,6 +1188,7 @@ atspeed_status atspeed_align_data(atspeed_ctx* c, int32_t S, const int32_t* item
   if (!a->ctx_weight || !a->label_weight || !a->root_weight || !a->log_pK || !a->lp_target || !a->root_target)
     return fail(ATSPEED_E_INVALID, "align_data: null batch buffer");
   if (S < 1) return fail(ATSPEED_E_SHAPE, "align_data: S must be positive");
+  if (c->ruled) return fail(ATSPEED_E_STATE, "alignment is of the plain logits: logit rules are set");
   if (!c->prefilled || !c->dft_prefilled) return fail(ATSPEED_E_STATE, "align_data needs atspeed_prefill first");
   if (!c->dft.present) return fail(ATSPEED_E_STATE, "context has no draft model");
   const atspeed_config& cf = c->cfg;
@@ -1196,6 +1232,7 @@ atspeed_status atspeed_align_step(atspeed_ctx* c, const atspeed_align_args* a, d
   if (!(a->lr >= 0.f) || !(a->beta1 >= 0.f && a->beta1 < 1.f) || !(a->beta2 >= 0.f && a->beta2 < 1.f) ||
       !(a->eps > 0.f) || !(a->weight_decay >= 0.f))
     return fail(ATSPEED_E_INVALID, "align_step: optimizer hyper-parameter out of range");
+  if (c->ruled) return fail(ATSPEED_E_STATE, "alignment is of the plain logits: logit rules are set");
   if (!c->align_ready) return fail(ATSPEED_E_STATE, "align_step needs atspeed_align_data after the last prefill or draft");
   const atspeed_config& cf = c->cfg;
   ModelRt& r = c->dft;

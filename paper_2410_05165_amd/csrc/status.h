@@ -7,6 +7,8 @@
 namespace atspeed {
 // Records msg for atspeed_last_error and returns s.
 atspeed_status fail(atspeed_status s, const std::string& msg);
+// The arguments of atspeed_logit_rules that are not a call's logits and rows.
+atspeed_status check_rules(const atspeed_logit_rules_args& a);
 }  // namespace atspeed
 
 #define HIP_TRY(expr)                                                                      \

@@ -184,15 +184,43 @@ def atspeed_tree_attention(q, k_cache, v_cache, block_table, row_off, ctx, max_c
     return (out, lse) if return_lse else out
 
 
+def _rule_counts(history, bias, allowed, cols, device):
+    """(max_hist, n_bias, n_states, address and stride of the biases) of the rules."""
+    n_bias = 0 if bias is None else bias.shape[0]
+    if bias is not None and (bias.dtype is not torch.float32 or bias.get_device() != device or
+                             bias.shape != (n_bias, cols) or (cols > 1 and bias.stride(1) != 1)):
+        raise ValueError(f"bias: want float32 [n, {cols}] on GPU {device}, rows contiguous")
+    return (0 if history is None else history.shape[-1], n_bias, 0 if allowed is None else allowed.shape[0],
+            (0, 0) if bias is None else (bias.data_ptr(), bias.stride(0) if n_bias > 1 else cols))
+
+
+def pack_rules(cols: int, token_base: int, B: int, device, history=None, hist_len=None, repetition=None, frequency=None,
+               presence=None, temperature=None, bias=None, bias_index=None, allowed=None, state=None,
+               mask_value: float = -1.0e4):
+    """The arguments of Engine.atspeed_set_logit_rules: rules without logits, rows or trees, state [B]."""
+    dev, f32, i32, vec = device.index or 0, torch.float32, torch.int32, (B,)
+    hist, n_bias, states, biases = _rule_counts(history, bias, allowed, cols, dev)
+    return LogitRulesArgs.pack(FP32, B, 0, cols, token_base, hist, 0, 0, n_bias, states, 0, 1, mask_value, 0, 0, 0, 0, 0, 0,
+                               _want(history, "history", i32, (B, hist), dev), _want(hist_len, "hist_len", i32, vec, dev),
+                               0, 0, _want(repetition, "repetition", f32, vec, dev),
+                               _want(frequency, "frequency", f32, vec, dev), _want(presence, "presence", f32, vec, dev),
+                               _want(temperature, "temperature", f32, vec, dev), *biases,
+                               _want(bias_index, "bias_index", i32, vec, dev),
+                               _want(allowed, "allowed", i32, (states, (cols + 31) // 32), dev),
+                               _want(state, "state", i32, vec, dev))
+
+
 def atspeed_logit_rules(logits, row_off, token_base: int = 0, history=None, hist_len=None, repetition=None,
                         frequency=None, presence=None, temperature=None, bias=None, bias_index=None, allowed=None,
-                        state=None, mask=None, node_token=None, mask_value: float = -math.inf, out=None, out_row=None):
+                        state=None, mask=None, node_token=None, mask_value: float = -math.inf, out=None, out_row=None,
+                        state_by_request: bool = False):
     """Penalties, biases, temperature and grammar masks on logits [rows, cols] (fp32 or bf16), as fp32.
 
     row_off [B + 1]; history [B, max_hist] and hist_len [B]; repetition, frequency, presence, temperature [B] fp32;
-    bias [n, cols] fp32 with bias_index [B]; allowed [states, ceil(cols / 32)] int32 bit words with state [rows];
-    node_token [B, max_nodes] with mask [rows, words] (None: chains).  out: fp32 [rows, cols], or with out_row [rows]
-    any [.., cols] that its rows are scattered to; may be ``logits`` itself.  Parts that are None are left out.
+    bias [n, cols] fp32 with bias_index [B]; allowed [states, ceil(cols / 32)] int32 bit words with state [rows]
+    (state_by_request: [B]); node_token [B, max_nodes] with mask [rows, words] (None: chains).  out: fp32 [rows, cols],
+    or with out_row [rows] any [.., cols] that its rows are scattered to; may be ``logits`` itself.  Parts that are
+    None are left out.
     """
     if logits.dim() != 2 or logits.dtype not in DTYPES or (logits.shape[1] > 1 and logits.stride(1) != 1):
         raise ValueError("logits: want float32 or bfloat16 [rows, cols], rows contiguous")
@@ -206,31 +234,25 @@ def atspeed_logit_rules(logits, row_off, token_base: int = 0, history=None, hist
     elif out.dtype is not f32 or out.get_device() != dev or out.shape[-1] != cols or (cols > 1 and out.stride(-1) != 1):
         raise ValueError("out: want float32 [.., cols] on the logits' device, rows contiguous")
     flat = out if out.dim() == 2 else out.view(-1, cols)
-    if out_row is None and flat.shape[0] != rows:
+    n_out = flat.shape[0]
+    if out_row is None and n_out != rows:
         raise ValueError("out: want as many rows as logits")
     B = row_off.numel() - 1
     vec = (B,)
-    hist = 0 if history is None else history.shape[-1]
     nodes = 0 if node_token is None else node_token.shape[-1]
     words = 0 if mask is None else mask.shape[-1]
-    n_bias = 0 if bias is None else bias.shape[0]
-    states = 0 if allowed is None else allowed.shape[0]
-    if bias is not None and (bias.dtype is not f32 or bias.get_device() != dev or bias.shape != (n_bias, cols) or
-                             (cols > 1 and bias.stride(1) != 1)):
-        raise ValueError("bias: want float32 [n, cols] on the logits' device, rows contiguous")
-    args = LogitRulesArgs.pack(DTYPES[logits.dtype], B, rows, cols, token_base, hist, nodes, words, n_bias, states,
-                          flat.shape[0], mask_value, logits.data_ptr(), logits.stride(0), flat.data_ptr(),
-                          flat.stride(0), _want(out_row, "out_row", i32, (rows,), dev),
-                          _want(row_off, "row_off", i32, (B + 1,), dev), _want(history, "history", i32, (B, hist), dev),
-                          _want(hist_len, "hist_len", i32, vec, dev),
-                          _want(node_token, "node_token", i32, (B, nodes), dev),
-                          _want(mask, "mask", torch.int64, (rows, words), dev),
-                          _want(repetition, "repetition", f32, vec, dev), _want(frequency, "frequency", f32, vec, dev),
-                          _want(presence, "presence", f32, vec, dev), _want(temperature, "temperature", f32, vec, dev),
-                          bias.data_ptr() if bias is not None else 0, bias.stride(0) if bias is not None else 0,
-                          _want(bias_index, "bias_index", i32, vec, dev),
-                          _want(allowed, "allowed", i32, (states, (cols + 31) // 32), dev),
-                          _want(state, "state", i32, (rows,), dev))
+    hist, n_bias, states, biases = _rule_counts(history, bias, allowed, cols, dev)
+    args = LogitRulesArgs.pack(
+        DTYPES[logits.dtype], B, rows, cols, token_base, hist, nodes, words, n_bias, states, n_out,
+        1 if state_by_request else 0, mask_value, logits.data_ptr(), logits.stride(0) if rows > 1 else cols,
+        flat.data_ptr(), flat.stride(0) if n_out > 1 else cols, _want(out_row, "out_row", i32, (rows,), dev),
+        _want(row_off, "row_off", i32, (B + 1,), dev), _want(history, "history", i32, (B, hist), dev),
+        _want(hist_len, "hist_len", i32, vec, dev), _want(node_token, "node_token", i32, (B, nodes), dev),
+        _want(mask, "mask", torch.int64, (rows, words), dev), _want(repetition, "repetition", f32, vec, dev),
+        _want(frequency, "frequency", f32, vec, dev), _want(presence, "presence", f32, vec, dev),
+        _want(temperature, "temperature", f32, vec, dev), *biases, _want(bias_index, "bias_index", i32, vec, dev),
+        _want(allowed, "allowed", i32, (states, (cols + 31) // 32), dev),
+        _want(state, "state", i32, vec if state_by_request else (rows,), dev))
     _call(_library().atspeed_logit_rules, args, dev)
     return out
 

@@ -584,6 +584,28 @@ def test_rules_in_place_strided_and_scattered():
     assert int(wide[:, :11].count_nonzero()) == 0 and int(wide[:, 214:].count_nonzero()) == 0
 
 
+def test_rules_with_a_state_for_each_request():
+    c = rules_case(14, 4, [2, 0, 3, 1], 300, BF16)
+    of = torch.tensor([2, -1, 7, 0], dtype=torch.int32, device=DEV)      # one set, none, one past the end, one set
+    rows = of[torch.tensor([0, 0, 2, 2, 2, 3], device=DEV)].contiguous()
+    want = atspeed_logit_rules(**dict(c, state=rows))
+    assert torch.equal(atspeed_logit_rules(**dict(c, state=of), state_by_request=True), want)
+    assert bool((want[2:5] == -math.inf).all())
+
+
+def test_rules_stay_inside_for_nonsense_indices():
+    c = rules_case(15, 3, [2, 3, 1], 90, F32)
+    rng = np.random.default_rng(1)
+    junk = lambda t: ints(rng.integers(-2 ** 31, 2 ** 31, t.shape))  # noqa: E731
+    names = ("row_off", "history", "hist_len", "bias_index", "state", "node_token")
+    for n in names:
+        atspeed_logit_rules(**dict(c, **{n: junk(c[n])}))
+    out = torch.full((6, 90), 5.0, device=DEV)
+    atspeed_logit_rules(**dict(c, **{n: junk(c[n]) for n in names}), out=out, out_row=junk(c["state"]))
+    assert torch.equal(out, torch.full_like(out, 5.0))
+    check_rules(c)
+
+
 def test_rules_rows_behind_the_last_request_stay():
     c = rules_case(12, 2, [3, 2], 64, F32)
     out = torch.full((5, 64), 9.0, device=DEV)

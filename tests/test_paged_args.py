@@ -22,7 +22,7 @@ def test_structures_follow_the_header(cls, name):
     kinds = {"int32_t": C.c_int32, "int64_t": C.c_int64, "float": C.c_float}
     want = []
     for line in filter(None, (x.strip() for x in body.split(";"))):
-        kind, names = re.match(r"((?:const )?\w+\s*\*?)\s*(.*)", line).groups()
+        kind, names = re.match(r"((?:const )?\w+\s*\*?)\s*(.*)", line, re.S).groups()
         for n in (x.strip() for x in names.split(",")):
             if kind.strip() == "atspeed_pages":
                 s = n.split("_")[0]
@@ -119,6 +119,10 @@ def test_rules_refusals():
            (INVALID, dict(logits=P, out=P, out_row=None, dtype=bd.BF16))]
     refuse("atspeed_logit_rules", bd.LogitRulesArgs, good, bad)
     assert bd.load_library().atspeed_logit_rules(C.byref(fill(bd.LogitRulesArgs, **{**good, "n_rows": 0})), None) == OK
+
+
+def test_rules_of_a_context_need_one():
+    assert bd.load_library().atspeed_set_logit_rules(None, None) == INVALID
 
 
 def test_tensors_that_are_not_on_a_gpu_are_refused():
