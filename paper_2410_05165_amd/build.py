@@ -1,4 +1,4 @@
-"""Builds the gfx950 shared library ``libatspeed.so`` in this directory with hipcc."""
+"""Builds ``libatspeed.so`` (gfx950, hipcc) and ``_marshal.so`` (its calls on PyTorch tensors, g++) in this directory."""
 from __future__ import annotations
 
 import os
@@ -8,6 +8,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libatspeed.so")
+MARSHAL = os.path.join(HERE, "_marshal.so")
 SOURCES = ["runtime.hip", "gemm.hip", "gemm_f32.hip", "attention.hip", "misc.hip", "select.hip", "relaxed.hip", "align.hip",
            "paged.hip", "tree_attention.hip", "rules.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -25,7 +26,30 @@ def build(verbose: bool = False) -> str:
         sys.stderr.write(r.stdout + r.stderr)
         raise RuntimeError("hipcc failed")
     os.replace(LIB + ".tmp", LIB)
+    build_marshal(verbose)
     return LIB
+
+
+def build_marshal(verbose: bool = False) -> str:
+    import sysconfig
+
+    import torch
+    from torch.utils.cpp_extension import include_paths
+
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           *["-I" + p for p in (*include_paths(), sysconfig.get_paths()["include"])],
+           os.path.join(CSRC, "marshal.cpp"), "-o", MARSHAL + ".tmp",
+           "-L" + os.path.join(os.path.dirname(torch.__file__), "lib"), "-lc10", "-ltorch_cpu", "-ltorch_python",
+           "-L" + HERE, "-l:libatspeed.so", "-Wl,-rpath,$ORIGIN"]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        sys.stderr.write(r.stdout + r.stderr)
+        raise RuntimeError(cmd[0] + " failed")
+    os.replace(MARSHAL + ".tmp", MARSHAL)
+    return MARSHAL
 
 
 if __name__ == "__main__":
