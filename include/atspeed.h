@@ -588,6 +588,9 @@ ATSPEED_API atspeed_status atspeed_kv_append(const atspeed_kv_append_args* args,
  *     or 2^30, and keys in pages outside 0 .. n_pool - 1, are not seen.
  *   max_ctx, max_new: what ctx[b] and a request's row count stay within; they size
  *     the launch (a context above max_ctx is still read whole).
+ * Long contexts are cut into pieces by the lengths of all the call's requests, and the
+ * pieces joined in order: the same call gives the same bits, a request among others of
+ * other lengths need not.
  * workspace: 16-byte aligned, at least atspeed_tree_attention_workspace_bytes (may be
  * 0, then it may be null); concurrent calls need one each. */
 typedef struct {

@@ -13,6 +13,7 @@
 // (0.64 PFLOP/s).
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "common.h"
 #include "paged.h"
@@ -34,12 +35,13 @@ struct TreeAttnArgs {
   char* out;
   int64_t o_row, o_head;       // bytes
   float* lse;
-  float* part;                 // [splits][n_rows][H][d_head] unnormalised sums of split requests
-  float2* part_ml;             // [splits][n_rows][H] running maximum and sum
+  int4* split;                 // [B] where a split request's parts are: first unit, parts, tiles
+  float* part;                 // [units][KH][qb][d_head] unnormalised sums
+  float2* part_ml;             // [units][KH][qb] running maximum and sum
   int B, n_rows, H, G, KH, max_pages, n_pool, max_new, words, shift, tail;
-  int qtiles, splits;
+  int qtiles, qb;              // query tiles of a request at most, queries of a tile
+  int units;                   // workgroups a key/value head if requests are split, else 0
   int cap;                     // keys a request can have: max_pages pages, at most 2^30
-  int chunk;                   // keys of a split
   uint32_t q_flip;             // sign bits of the queries' elements (negative scale)
   float scale;                 // |scale| log2(e)
 };
@@ -52,11 +54,6 @@ typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4_t;
 typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
 typedef __attribute__((address_space(3))) void lds_void_t;
 
-// Pieces of a request's keys; the last one takes what a context above max_ctx holds more.
-__device__ __forceinline__ int split_count(const TreeAttnArgs& a, int total) {
-  return total <= a.chunk ? 1 : min((total - 1) / a.chunk + 1, a.splits);
-}
-
 // New rows of request b, from row r0 on; none where its offsets are no rows of the call.
 __device__ __forceinline__ int new_rows(const TreeAttnArgs& a, int b, int& r0) {
   const int begin = a.row_off[b], end = a.row_off[b + 1];
@@ -65,39 +62,129 @@ __device__ __forceinline__ int new_rows(const TreeAttnArgs& a, int b, int& r0) {
   return sane ? end - begin : 0;
 }
 
+// Lane i: the sum of lanes 0 .. i.
+template <class N>
+__device__ __forceinline__ N wave_scan(N x) {
+  const auto from = [&](auto ctrl, auto rows) {
+    return __builtin_bit_cast(N, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), ctrl.value, rows.value, 0xf, false));
+  };
+  typedef std::integral_constant<int, 0xf> All;
+  x += from(std::integral_constant<int, 0x111>{}, All{});   // row_shr: 1, 2, 4, 8 lanes of a row of 16
+  x += from(std::integral_constant<int, 0x112>{}, All{});
+  x += from(std::integral_constant<int, 0x114>{}, All{});
+  x += from(std::integral_constant<int, 0x118>{}, All{});
+  x += from(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});   // row_bcast: 15 to the next row
+  x += from(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});   // 31 to the rows behind
+  return x;
+}
+__device__ __forceinline__ int round_up64(int n) { return (n + 63) & ~63; }
+
 // One workgroup's share: a request, a key/value head, a tile of its queries (row i, head
 // h of the group: query i * G + h), a range of its keys.
 struct Share {
-  int kvh, r0, nq, q0, split, nsplit;
+  int kvh, r0, nq, q0, unit, nsplit;
   int ctx, kbeg, kend;   // context keys; this workgroup's keys
   int clear;             // from this key on some query may not see a key
   const int* table;
 
-  // False where there is nothing to do.  QB queries a tile.
-  __device__ __forceinline__ bool init(const TreeAttnArgs& a, int QB) {
-    // Workgroup L runs on XCD L % 8: the tiles and splits of one pair stay on one
-    // XCD, whose L2 then holds the pair's keys; the pairs are dealt round-robin.
-    const int L = blockIdx.x, Z = a.qtiles * a.splits;
-    const int pair = ((L >> 3) / Z) * 8 + (L & 7), z = (L >> 3) % Z;
-    if (pair >= a.B * a.KH) return false;
-    const int b = pair / a.KH;
-    kvh = pair % a.KH;
-    split = z / a.qtiles;
-    // chains: the tiles with the most keys first
-    const int qt = a.mask ? z % a.qtiles : a.qtiles - 1 - z % a.qtiles;
-    const int count = new_rows(a, b, r0);
-    nq = min(min(count, a.n_rows - r0), a.max_new) * a.G;   // fits: n_rows x heads does
-    q0 = qt * QB;
-    if (count == 0 || q0 >= nq) return false;
-    const int total = keys(a, b, count);
-    nsplit = split_count(a, total);
-    if (split >= nsplit) return false;
-    kbeg = split * a.chunk;
-    kend = split + 1 < nsplit ? kbeg + a.chunk : total;
-    if (!a.mask) kend = min(kend, ctx + (min(q0 + QB, nq) - 1) / a.G + 1);
+  // False where there is nothing to do.
+  __device__ __forceinline__ bool init(const TreeAttnArgs& a) {
+    int b, qt, split, total;
+    if (a.units) {
+      if (!pick(a, b, qt, split, total)) return false;
+    } else {
+      // Workgroup L runs on XCD L % 8: the tiles of one pair stay on one XCD, whose L2
+      // then holds the pair's keys; the pairs are dealt round-robin.
+      const int L = blockIdx.x, pair = ((L >> 3) / a.qtiles) * 8 + (L & 7), z = (L >> 3) % a.qtiles;
+      if (pair >= a.B * a.KH) return false;
+      b = pair / a.KH;
+      kvh = pair % a.KH;
+      qt = a.mask ? z : a.qtiles - 1 - z;   // chains: the tiles with the most keys first
+      split = unit = 0;
+      nsplit = 1;
+      total = request(a, b);
+    }
+    q0 = qt * a.qb;
+    if (q0 >= nq) return false;
+    const int chunk = round_up64((total + nsplit - 1) / nsplit);
+    kbeg = split * chunk;
+    kend = split + 1 < nsplit ? min(kbeg + chunk, total) : total;   // the last pieces may be empty
+    if (!a.mask) kend = min(kend, ctx + (min(q0 + a.qb, nq) - 1) / a.G + 1);
     clear = a.mask ? ctx : ctx + q0 / a.G + 1;
     table = a.table + (int64_t)b * a.max_pages;
     return true;
+  }
+  // Keys of request b; sets r0, nq and ctx.
+  __device__ __forceinline__ int request(const TreeAttnArgs& a, int b) {
+    const int count = new_rows(a, b, r0);
+    nq = min(min(count, a.n_rows - r0), a.max_new) * a.G;   // fits: n_rows x heads does
+    return keys(a, b, count);
+  }
+  // The workgroup's piece where requests are split: all requests into pieces of about c
+  // keys, c such that they are a.units at most for a key/value head.  With S = sum of
+  // tiles x keys and N = sum of tiles the pieces are S / c at least and S / c + N at most,
+  // and a.units >= 2 N: c = S / units is enlarged by eighths until they fit, 2 S / units
+  // at most.  Every wave works it out from the requests' lengths, 64 requests at a time,
+  // and takes the workgroup's place in the list of the pieces.
+  __device__ __forceinline__ bool pick(const TreeAttnArgs& a, int& b, int& qt, int& split, int& total) {
+    const int lane = threadIdx.x & 63;
+    int len, tiles;
+    auto load = [&](int i) {
+      len = tiles = 0;
+      if (i >= a.B) return;
+      len = request(a, i);
+      tiles = (nq + a.qb - 1) / a.qb;
+    };
+    const bool one = a.B <= 64;   // the lengths stay in registers
+    float S = 0;
+    for (int i0 = 0; i0 < a.B; i0 += 64) {
+      load(i0 + lane);
+      S += wave_scan((float)len * tiles);
+    }
+    // sums of 1,024 numbers in fp32: 1e-6 off at most
+    const float c0 = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, S), 63)) * 1.00001f / a.units;
+    float per_key;
+    int all;
+    auto pieces = [&]() { return tiles * (1 + (int)((float)max(len - 1, 0) * per_key)); };
+    for (int e = 8; e <= 16; ++e) {
+      per_key = 1.f / fmaxf(c0 * e * 0.125f, 256.f);
+      int n = 0;
+      for (int i0 = 0; i0 < a.B; i0 += 64) {
+        if (!one) load(i0 + lane);
+        n += wave_scan(pieces());
+      }
+      all = __builtin_amdgcn_readlane(n, 63);
+      if (all <= a.units) break;
+    }
+    // Workgroup L runs on XCD L % 8, which takes neighbours in the list: the tiles of a
+    // piece, which read the same keys.
+    all = min(all, a.units);
+    const int L = blockIdx.x, per = (all * a.KH + 7) / 8, at = (L & 7) * per + (L >> 3);
+    if ((L >> 3) >= per || at >= all * a.KH) return false;
+    kvh = at / all;
+    unit = at % all;
+    int left = unit;
+    for (int i0 = 0; i0 < a.B; i0 += 64) {
+      if (!one) load(i0 + lane);
+      const int n = pieces(), upto = wave_scan(n);
+      const uint64_t past = __ballot(upto > left);
+      if (past) {
+        const int l = __ffsll((unsigned long long)past) - 1, t = __builtin_amdgcn_readlane(tiles, l);
+        b = i0 + l;
+        left -= __builtin_amdgcn_readlane(upto - n, l);
+        total = __builtin_amdgcn_readlane(len, l);
+        r0 = __builtin_amdgcn_readlane(r0, l);
+        nq = __builtin_amdgcn_readlane(nq, l);
+        ctx = __builtin_amdgcn_readlane(ctx, l);
+        nsplit = __builtin_amdgcn_readlane(n, l) / t;
+        split = left / t;
+        qt = left % t;
+        if (left == 0 && kvh == 0 && threadIdx.x == 0) a.split[b] = int4{unit, nsplit, t, 0};
+        return true;
+      }
+      left -= __builtin_amdgcn_readlane(upto, 63);
+    }
+    return false;
   }
   // Keys of request b with `count` new rows (none where ctx is negative); sets ctx.
   __device__ __forceinline__ int keys(const TreeAttnArgs& a, int b, int count) {
@@ -214,13 +301,14 @@ struct Tile {
   }
 
   // bits: the keys each query sees, if not `full` (all of them).  between(k) runs after
-  // the k-th chunk group of the scores, k = 0 .. NKS - 1.
-  template <class F>
+  // the k-th chunk group of the scores, k = 0 .. NKS - 1.  NB: the blocks of queries that
+  // there are.
+  template <int NB, class F>
   __device__ __forceinline__ void step(const TreeAttnArgs& a, const char* ks, const char* vs, bool full,
                                        const uint64_t (&bits)[NQ], F&& between) {
-    f32x4_t sc[NQ][NKB];
+    f32x4_t sc[NB][NKB];
 #pragma unroll
-    for (int n = 0; n < NQ; ++n)
+    for (int n = 0; n < NB; ++n)
 #pragma unroll
       for (int kb = 0; kb < NKB; ++kb) sc[n][kb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -230,7 +318,7 @@ struct Tile {
         const int key = kb * 16 + ql;
         const f32x4_t kf = *reinterpret_cast<const f32x4_t*>(ks + key * ROWB + ((k * 4 + g) ^ kswz(key)) * 16);
 #pragma unroll
-        for (int n = 0; n < NQ; ++n) {
+        for (int n = 0; n < NB; ++n) {
           if constexpr (BF) {
             sc[n][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf),
                                                                  __builtin_bit_cast(bf16x8_t, qf[n][k]), sc[n][kb], 0, 0, 0);
@@ -245,7 +333,7 @@ struct Tile {
     }
     if (!full) {
 #pragma unroll
-      for (int n = 0; n < NQ; ++n) {
+      for (int n = 0; n < NB; ++n) {
         const uint64_t mine = bits[n] >> (g * 4);
 #pragma unroll
         for (int kb = 0; kb < NKB; ++kb)
@@ -258,10 +346,10 @@ struct Tile {
           }
       }
     }
-    float mx[NQ];
+    float mx[NB];
     bool moved = false;
 #pragma unroll
-    for (int n = 0; n < NQ; ++n) {
+    for (int n = 0; n < NB; ++n) {
       float x = sc[n][0][0];
 #pragma unroll
       for (int kb = 0; kb < NKB; ++kb)
@@ -272,7 +360,7 @@ struct Tile {
     }
     if (__any(moved)) {
 #pragma unroll
-      for (int n = 0; n < NQ; ++n) {
+      for (int n = 0; n < NB; ++n) {
         float x = fmaxf(mx[n], __shfl_xor(mx[n], 16));
         x = fmaxf(x, __shfl_xor(x, 32));
         const float mnew = fmaxf(m[n], x);
@@ -284,7 +372,7 @@ struct Tile {
       }
     }
 #pragma unroll
-    for (int n = 0; n < NQ; ++n) {
+    for (int n = 0; n < NB; ++n) {
       const float ref = m[n] != -INFINITY ? m[n] : 0.f;   // a query that has seen nothing yet
       float ps = 0.f;
 #pragma unroll
@@ -300,9 +388,9 @@ struct Tile {
     if constexpr (BF) {
 #pragma unroll
       for (int kk = 0; kk < KW / 32; ++kk) {
-        bf16x8_t pf[NQ];
+        bf16x8_t pf[NB];
 #pragma unroll
-        for (int n = 0; n < NQ; ++n)
+        for (int n = 0; n < NB; ++n)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             pf[n][i] = (__bf16)sc[n][2 * kk][i];
@@ -319,7 +407,7 @@ struct Tile {
           const auto w8 = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
           const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, w8);
 #pragma unroll
-          for (int n = 0; n < NQ; ++n) o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[n], o[n][d], 0, 0, 0);
+          for (int n = 0; n < NB; ++n) o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[n], o[n][d], 0, 0, 0);
         }
       }
     } else {
@@ -333,7 +421,7 @@ struct Tile {
             const int dim = d * 16 + ql;
             const float vf = *reinterpret_cast<const float*>(vs + key * ROWB + (((dim >> 2) ^ vswz(key)) << 4) + (dim & 3) * 4);
 #pragma unroll
-            for (int n = 0; n < NQ; ++n) o[n][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf, sc[n][kb][i], o[n][d], 0, 0, 0);
+            for (int n = 0; n < NB; ++n) o[n][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf, sc[n][kb][i], o[n][d], 0, 0, 0);
           }
         }
     }
@@ -406,7 +494,8 @@ struct Tile {
     if (!qok[n]) return;
     const int64_t at = qrow[n] * a.H + qhead[n];
     if (s.nsplit > 1) {
-      const int64_t pt = s.split * (int64_t)a.n_rows * a.H + at;
+      const int c = qi[n] * a.G + qhead[n] - s.kvh * a.G - s.q0;
+      const int64_t pt = ((int64_t)s.unit * a.KH + s.kvh) * a.qb + c;
       *reinterpret_cast<f32x4_t*>(a.part + pt * DH + d * 16 + g * 4) = x;
       if (d == 0 && g == 0) a.part_ml[pt] = float2{mm, ll};
       return;
@@ -440,7 +529,7 @@ __global__ void __launch_bounds__(256, 2) tree_attn_stream_kernel(TreeAttnArgs a
   __shared__ float2 ml_s[4][16];
   static_assert(4 * NDB * 64 * 16 <= 4 * 2 * Tl::BYTES, "the join fits the tiles");
   Share s;
-  if (!s.init(a, 16 * NQ)) return;
+  if (!s.init(a)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   char* ks = lds + wave * 2 * Tl::BYTES;
   char* vs = ks + Tl::BYTES;
@@ -496,7 +585,7 @@ __global__ void __launch_bounds__(256, 2) tree_attn_stream_kernel(TreeAttnArgs a
         }
       }
     }
-    t.step(a, ks, vs, full, bits, [](int) {});
+    t.template step<NQ>(a, ks, vs, full, bits, [](int) {});
   }
 
   if (__syncthreads_or(bad) && wave == 0) t.add_not_finite(a, s);
@@ -542,9 +631,12 @@ __global__ void __launch_bounds__(256, 2) tree_attn_tile_kernel(TreeAttnArgs a) 
   constexpr int KPI = 64 / CPR > 0 ? 64 / CPR : 1;        // keys of an instruction
   __shared__ __align__(1024) char lds[2 * 2 * Tl::BYTES];
   Share s;
-  if (!s.init(a, 64 * NQ)) return;
+  if (!s.init(a)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int first = s.q0 + wave * 16 * NQ;
+  // A tile of up to 64 queries, a request's last: one block a wave instead of two for the
+  // first waves (300 nodes x 128 users 1.24 -> 1.22 ms).
+  const bool half = NQ == 2 && s.nq - s.q0 <= 64;
+  const int first = s.q0 + wave * (half ? 16 : 16 * NQ);
   const bool active = first < s.nq;
   int pg = s.page(a, s.kbeg, KW);
   TileRows rows;
@@ -582,122 +674,144 @@ __global__ void __launch_bounds__(256, 2) tree_attn_tile_kernel(TreeAttnArgs a) 
   t.init(a, s, active ? first : s.nq - 1);
   const int i_first = (active ? first : s.nq - 1) / a.G;
   bool bad = false;
-  MaskWords words[NQ];
-  auto load_words = [&](int k0) {
-    if (a.mask && k0 + KW > s.ctx) {
+  auto run = [&](auto blocks) {
+    constexpr int NB = decltype(blocks)::value;
+    MaskWords words[NB];
+    auto load_words = [&](int k0) {
+      if (a.mask && k0 + KW > s.ctx) {
 #pragma unroll
-      for (int n = 0; n < NQ; ++n) words[n].load(a.mask + t.qrow[n] * a.words, a.words, k0 - s.ctx);
+        for (int n = 0; n < NB; ++n) words[n].load(a.mask + t.qrow[n] * a.words, a.words, k0 - s.ctx);
+      }
+    };
+    load_words(s.kbeg);
+
+    int stage = 0;
+    for (int k0 = s.kbeg; k0 < s.kend; k0 += KW, stage ^= 1) {
+      const uint64_t there = rows.there;
+      char* ks = lds + stage * 2 * Tl::BYTES;
+      char* vs = ks + Tl::BYTES;
+      const int j0 = k0 - s.ctx;
+      const bool full = there == Tl::ALL && (j0 + KW <= 0 || (!a.mask && j0 + KW <= i_first + 1));
+      uint64_t bits[NQ];
+      if (!full) {
+#pragma unroll
+        for (int n = 0; n < NB; ++n) bits[n] = there & (a.mask ? words[n].bits(j0) : chain_bits(t.qi[n], j0));
+      }
+      // this tile has landed, and the other stage has been read
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      const bool more = k0 + KW < s.kend;
+      if (more) {
+        rows.set(a, k0 + KW, pg);
+        load_words(k0 + KW);
+        pg = s.page(a, k0 + 2 * KW, KW);
+      }
+      if (there != Tl::ALL || k0 + KW > s.clear) {
+#pragma unroll
+        for (int c = 0; c < NIN; ++c) {
+          u32x4_t* p = reinterpret_cast<u32x4_t*>(vs) + c * 256 + threadIdx.x;
+          u32x4_t w = *p;
+          if (Tl::finite(w)) {
+            *p = w;
+            bad = true;
+          }
+        }
+        __syncthreads();
+      }
+      bool some = full;
+      if (!full) {
+        uint64_t any = 0;
+#pragma unroll
+        for (int n = 0; n < NB; ++n) any |= bits[n];
+        some = __any(any != 0);
+      }
+      if (!active || !some) {   // no query of the wave sees the tile
+        if (more) fetch(stage ^ 1);
+      } else {
+        // the last tile asks for itself again: without a branch here the matrix
+        // instructions stay in one block (causal chunks 117 us with it, 107 without)
+        t.template step<NB>(a, ks, vs, full, bits, [&](int k) { some_dma(k, stage ^ 1); });
+      }
     }
   };
-  load_words(s.kbeg);
-
-  int stage = 0;
-  for (int k0 = s.kbeg; k0 < s.kend; k0 += KW, stage ^= 1) {
-    const uint64_t there = rows.there;
-    char* ks = lds + stage * 2 * Tl::BYTES;
-    char* vs = ks + Tl::BYTES;
-    const int j0 = k0 - s.ctx;
-    const bool full = there == Tl::ALL && (j0 + KW <= 0 || (!a.mask && j0 + KW <= i_first + 1));
-    uint64_t bits[NQ];
-    if (!full) {
-#pragma unroll
-      for (int n = 0; n < NQ; ++n) bits[n] = there & (a.mask ? words[n].bits(j0) : chain_bits(t.qi[n], j0));
-    }
-    // this tile has landed, and the other stage has been read
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    const bool more = k0 + KW < s.kend;
-    if (more) {
-      rows.set(a, k0 + KW, pg);
-      load_words(k0 + KW);
-      pg = s.page(a, k0 + 2 * KW, KW);
-    }
-    if (there != Tl::ALL || k0 + KW > s.clear) {
-#pragma unroll
-      for (int c = 0; c < NIN; ++c) {
-        u32x4_t* p = reinterpret_cast<u32x4_t*>(vs) + c * 256 + threadIdx.x;
-        u32x4_t w = *p;
-        if (Tl::finite(w)) {
-          *p = w;
-          bad = true;
-        }
-      }
-      __syncthreads();
-    }
-    bool some = full;
-    if (!full) {
-      uint64_t any = 0;
-#pragma unroll
-      for (int n = 0; n < NQ; ++n) any |= bits[n];
-      some = __any(any != 0);
-    }
-    if (!active || !some) {   // no query of the wave sees the tile
-      if (more) fetch(stage ^ 1);
-    } else {
-      // the last tile asks for itself again: without a branch here the matrix
-      // instructions stay in one block (causal chunks 117 us with it, 107 without)
-      t.step(a, ks, vs, full, bits, [&](int k) { some_dma(k, stage ^ 1); });
-    }
-  }
+  if (half) run(std::integral_constant<int, 1>{});
+  else run(std::integral_constant<int, NQ>{});
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing is written to LDS behind the workgroup's end
   if (__syncthreads_or(bad)) t.add_not_finite(a, s);
   t.sum_lanes();
   if (!active) return;
 #pragma unroll
   for (int n = 0; n < NQ; ++n)
+    if (n == 0 || !half)
 #pragma unroll
-    for (int d = 0; d < Tl::NDB; ++d) t.put(a, s, n, d, t.o[n][d], t.m[n], t.lsum[n]);
+      for (int d = 0; d < Tl::NDB; ++d) t.put(a, s, n, d, t.o[n][d], t.m[n], t.lsum[n]);
 }
 
-// Joins the parts of requests whose keys were split, a workgroup per row and head: all
-// threads take the splits' maxima and sums, then groups of DH / 4 of them the splits in
-// turn, four dims a thread.  Bound by the latency of those loads: with one such group
-// per row, 61 parts of 4 users' 32 rows took 29 us.
-template <class T, int DH>
+// Joins the parts of requests whose keys were split.  DH / 4 threads, a group, hold a
+// row and head, four dims each.  Bound by the latency of the loads, so many parts (MANY)
+// get a workgroup per row and head: all threads take the parts' maxima and sums, then its
+// groups the parts in turn (61 parts of 4 users' 32 rows: 29 us with a group for each
+// row, 14 so).  Few parts get a group.
+template <class T, int DH, bool MANY>
 __global__ void __launch_bounds__(256) tree_attn_join_kernel(TreeAttnArgs a) {
   constexpr int LPR = DH / 4, GROUPS = 256 / LPR;
-  __shared__ f32x4_t xs[GROUPS][LPR];
-  __shared__ float red[2][4];
   const int tid = threadIdx.x, lane = tid % LPR, grp = tid / LPR;
-  const int h = blockIdx.x % a.H, bi = blockIdx.x / a.H, b = bi / a.max_new, i = bi % a.max_new;
+  const int at = MANY ? blockIdx.x : blockIdx.x * GROUPS + grp;
+  const int h = at % a.H, bi = at / a.H, b = bi / a.max_new, i = bi % a.max_new;
+  if (b >= a.B) return;
   int r0;
   const int count = new_rows(a, b, r0);
   if (i >= min(count, a.n_rows - r0)) return;
-  Share s;
-  const int n = split_count(a, s.keys(a, b, count));
+  const int4 where = a.split[b];   // first unit, parts, tiles
+  const int n = where.y, q = i * a.G + h % a.G;
   if (n <= 1) return;
-  const int64_t row = ((int64_t)r0 + i) * a.H + h, step = (int64_t)a.n_rows * a.H;
+  const int64_t out_row = (int64_t)r0 + i, row = ((int64_t)(where.x + q / a.qb) * a.KH + h / a.G) * a.qb + q % a.qb,
+                step = (int64_t)where.z * a.KH * a.qb;
+  const f32x4_t* part = reinterpret_cast<const f32x4_t*>(a.part + row * DH) + lane;
   float mm = -INFINITY, ll = 0.f;
-  for (int k = tid; k < n; k += 256) mm = fmaxf(mm, a.part_ml[k * step + row].x);
-#pragma unroll
-  for (int w = 1; w < 64; w <<= 1) mm = fmaxf(mm, __shfl_xor(mm, w));
-  if ((tid & 63) == 0) red[0][tid >> 6] = mm;
-  __syncthreads();
-  mm = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
   auto weight = [&](float m) { return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mm); };
-  for (int k = tid; k < n; k += 256) {
-    const float2 ml = a.part_ml[k * step + row];
-    ll += ml.y * weight(ml.x);
-  }
-#pragma unroll
-  for (int w = 1; w < 64; w <<= 1) ll += __shfl_xor(ll, w);
-  if ((tid & 63) == 0) red[1][tid >> 6] = ll;
   f32x4_t x = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int k = grp; k < n; k += GROUPS)
-    x += *reinterpret_cast<const f32x4_t*>(a.part + (k * step + row) * DH + lane * 4) * weight(a.part_ml[k * step + row].x);
-  xs[grp][lane] = x;
-  __syncthreads();
-  if (grp > 0) return;
+  if constexpr (MANY) {
+    __shared__ f32x4_t xs[GROUPS][LPR];
+    __shared__ float red[2][4];
+    for (int k = tid; k < n; k += 256) mm = fmaxf(mm, a.part_ml[k * step + row].x);
 #pragma unroll
-  for (int k = 1; k < GROUPS; ++k) x += xs[k][lane];
-  ll = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
+    for (int w = 1; w < 64; w <<= 1) mm = fmaxf(mm, __shfl_xor(mm, w));
+    if ((tid & 63) == 0) red[0][tid >> 6] = mm;
+    __syncthreads();
+    mm = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+    for (int k = tid; k < n; k += 256) {
+      const float2 ml = a.part_ml[k * step + row];
+      ll += ml.y * weight(ml.x);
+    }
+#pragma unroll
+    for (int w = 1; w < 64; w <<= 1) ll += __shfl_xor(ll, w);
+    if ((tid & 63) == 0) red[1][tid >> 6] = ll;
+#pragma unroll 4
+    for (int k = grp; k < n; k += GROUPS) x += part[k * step * LPR] * weight(a.part_ml[k * step + row].x);
+    xs[grp][lane] = x;
+    __syncthreads();
+    if (grp > 0) return;
+#pragma unroll
+    for (int k = 1; k < GROUPS; ++k) x += xs[k][lane];
+    ll = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
+  } else {
+#pragma unroll 4
+    for (int k = 0; k < n; ++k) mm = fmaxf(mm, a.part_ml[k * step + row].x);
+#pragma unroll 4
+    for (int k = 0; k < n; ++k) {
+      const float2 ml = a.part_ml[k * step + row];
+      const float w = weight(ml.x);
+      x += part[k * step * LPR] * w;
+      ll += ml.y * w;
+    }
+  }
   const bool some = ll > 0.f || ll != ll;
   x *= some ? 1.f / ll : 0.f;
-  T* out = reinterpret_cast<T*>(a.out + ((int64_t)r0 + i) * a.o_row + h * a.o_head) + lane * 4;
+  T* out = reinterpret_cast<T*>(a.out + out_row * a.o_row + h * a.o_head) + lane * 4;
 #pragma unroll
   for (int e = 0; e < 4; ++e) St<T>::st(out + e, x[e]);
-  if (a.lse && lane == 0) a.lse[row] = some ? (mm + __log2f(ll)) * kLn2 : -INFINITY;
+  if (a.lse && lane == 0) a.lse[out_row * a.H + h] = some ? (mm + __log2f(ll)) * kLn2 : -INFINITY;
 }
 
 static atspeed_status check_attention(const atspeed_tree_attention_args* args) {
@@ -726,8 +840,8 @@ namespace {
 // Launch of one call: queries per workgroup, and how the keys are split.
 struct AttnPlan {
   int tile;          // queries of a workgroup
-  int qtiles, splits, cap, chunk;
-  size_t part_bytes, bytes;
+  int qtiles, units, cap;
+  size_t part_at, ml_at, bytes;   // of the workspace
 };
 
 AttnPlan plan_attention(const atspeed_tree_attention_args& a) {
@@ -747,38 +861,45 @@ AttnPlan plan_attention(const atspeed_tree_attention_args& a) {
   p.tile = nq <= 16 ? 16 : nq <= few ? few : nq <= 64 || !bf ? 64 : 128;
   if (p.tile > few && keys <= 1024 && pairs * ((nq + few - 1) / few) <= 256) p.tile = few;
   p.qtiles = (int)((nq + p.tile - 1) / p.tile);
-  // Keys are split until the launch has 8 workgroups for each of the 256 CUs, 32 of the
-  // short ones of few queries: the bounds count every context as the longest, and what
-  // ragged contexts leave over is spread evenly only if the pieces are many (64 single
-  // tokens over up to 8,192 keys: 208 us with 2,048, 175 with 4,096, 155 with 8,192; trees
-  // over up to 65,536 keys: 171 us with 1,024, 158 with 2,048, 199 with 4,096, where the
-  // join of the pieces costs more than the spread gains).  Pieces of under 256 keys lose
-  // to their join (78 rows x 7 users over 1,970 keys: 27 us with 256, 31 with 128), and
-  // so does any split of up to 10 steps (4 rows x 8 users over 600 keys: 10.2 us in
-  // pieces, 8.3 whole; 256 rows x 8 users over 310 keys 31 and 14; but 12 rows x 2 users
-  // over 2,012 keys, 32 steps, 16.5 and 51).
-  const int64_t base = pairs * p.qtiles, want = std::max<int64_t>(1, (p.tile <= 32 ? 8192 : 2048) / base);
+  // Requests are split where the launch has at least two pieces a tile of queries: into
+  // 512 workgroups, two for each of the 256 CUs, or as few times that as it takes, all of
+  // the same length as far as the contexts allow, since the kernel has them (Share::pick).
+  // Pieces of one length as the host alone could cut them, for the longest context, took
+  // (us; so): trees of 4 users over up to 65,536 keys 144 (136); of one over 65,536 102
+  // (71); one prompt chunk of 1,024 rows over 4,096 keys 137 (114), 300 rows over 30,000,
+  // 2 heads, 211 (80); 64 single tokens over up to 8,192 keys 148 (145).  1,024 workgroups
+  // for the second and third take 90 and 130: each piece pays its start and its part.
+  // Pieces of under 256 keys lose to their join, and so does any split of up to 10 steps
+  // (4 rows x 8 users over 600 keys: 10.2 us in pieces, 8.3 whole; 256 rows x 8 users over
+  // 310 keys 31 and 14).
   const int step = p.tile <= 32 ? (bf ? 128 : 64) : std::min(64, (p.tile / 64) * 8192 / (a.d_head * (bf ? 2 : 4)));
-  int64_t chunk = std::max<int64_t>(256, ((keys + want - 1) / want + 127) / 128 * 128);
-  if (keys <= 10 * step) chunk = keys;
-  p.chunk = (int)chunk;
-  p.splits = (int)((keys + p.chunk - 1) / p.chunk);
-  const size_t rows = (size_t)p.splits * a.n_rows * a.n_heads;
-  p.part_bytes = p.splits > 1 ? rows * a.d_head * sizeof(float) : 0;
-  p.bytes = p.splits > 1 ? p.part_bytes + rows * sizeof(float2) : 0;
+  const int64_t tiles = (int64_t)a.B * p.qtiles;
+  int64_t units = std::max(1, 512 / a.n_kv_heads);
+  while (units < 2 * tiles && units * 2 * a.n_kv_heads <= 2048) units *= 2;
+  if (keys > 10 * step && units >= 2 * tiles) {
+    p.units = (int)units;
+    const size_t rows = (size_t)units * a.n_kv_heads * p.tile;
+    p.part_at = (size_t)a.B * sizeof(int4);
+    p.ml_at = p.part_at + rows * a.d_head * sizeof(float);
+    p.bytes = p.ml_at + rows * sizeof(float2);
+  }
   return p;
 }
 
 template <class T, int DH, class F>
 atspeed_status launch_attention(const TreeAttnArgs& p, F kernel, hipStream_t st) {
-  const long long pairs = (long long)p.B * p.KH, n = (pairs + 7) / 8 * 8 * p.qtiles * p.splits;
+  const long long pairs = (long long)p.B * p.KH;
+  const long long n = p.units ? (p.units * p.KH + 7) / 8 * 8 : (pairs + 7) / 8 * 8 * p.qtiles;
   if (n >= (1LL << 31)) return fail(ATSPEED_E_SHAPE, "tree attention: too many query tiles");
   hipLaunchKernelGGL(kernel, dim3((unsigned)n), dim3(256), 0, st, p);
   HIP_TRY(hipGetLastError());
-  if (p.splits > 1) {
-    // few: splits come only with few query tiles
-    const long long rows = (long long)p.B * p.max_new * p.H;
-    hipLaunchKernelGGL((tree_attn_join_kernel<T, DH>), dim3((unsigned)rows), dim3(256), 0, st, p);
+  if (p.units) {
+    // few: units come only with few query tiles
+    const unsigned rows = (unsigned)((long long)p.B * p.max_new * p.H), groups = 1024 / DH;
+    if (p.units <= 16 * p.B * p.qtiles)
+      hipLaunchKernelGGL((tree_attn_join_kernel<T, DH, false>), dim3((rows + groups - 1) / groups), dim3(256), 0, st, p);
+    else
+      hipLaunchKernelGGL((tree_attn_join_kernel<T, DH, true>), dim3(rows), dim3(256), 0, st, p);
     HIP_TRY(hipGetLastError());
   }
   return ATSPEED_OK;
@@ -841,11 +962,12 @@ atspeed_status atspeed_tree_attention(const atspeed_tree_attention_args* args, v
   p.table = a.block_table; p.row_off = a.row_off; p.ctx = a.ctx; p.mask = a.mask;
   p.out = (char*)a.out; p.o_row = a.out_row_stride * es; p.o_head = a.out_head_stride * es;
   p.lse = a.lse;
-  p.part = (float*)workspace; p.part_ml = (float2*)((char*)workspace + plan.part_bytes);
+  p.split = (int4*)workspace;
+  p.part = (float*)((char*)workspace + plan.part_at); p.part_ml = (float2*)((char*)workspace + plan.ml_at);
   p.B = a.B; p.n_rows = a.n_rows; p.H = a.n_heads; p.KH = a.n_kv_heads; p.G = a.n_heads / a.n_kv_heads;
   p.max_pages = a.max_pages; p.n_pool = a.n_pool; p.max_new = std::min(a.max_new, a.n_rows); p.words = a.mask_words;
   p.shift = log2_of(a.page_size); p.tail = a.page_size - 1;
-  p.qtiles = plan.qtiles; p.splits = plan.splits; p.cap = plan.cap; p.chunk = plan.chunk;
+  p.qtiles = plan.qtiles; p.qb = plan.tile; p.units = plan.units; p.cap = plan.cap;
   // the queries carry the scale's sign, so that the largest product is the largest score
   p.q_flip = a.scale < 0.f ? (es == 2 ? 0x80008000u : 0x80000000u) : 0u;
   p.scale = std::max(std::fabs(a.scale) * 1.4426950408889634f, 1e-37f);

@@ -477,11 +477,22 @@ def test_attention_context_above_its_bound_is_read_whole():
 
 
 @pytest.mark.parametrize("dtype,dh", [(BF16, 128), (F32, 64)])
-def test_attention_is_repeatable_and_independent_of_other_requests(dtype, dh):
-    """The same bits twice, and for a request alone where the launch has the same shape."""
+def test_attention_is_repeatable(dtype, dh):
     c = attention_case(51, [4000, 700, 4000], [3, 3, 3], 8, 2, dh, 16, dtype, True)
     a, b = atspeed_tree_attention(**c), atspeed_tree_attention(**c)
     assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype,dh", [(BF16, 128), (BF16, 64), (F32, 32)])
+@pytest.mark.parametrize("B,most", [(5, 40), (64, 1), (70, 1), (70, 9), (130, 80)])
+@pytest.mark.parametrize("tree", [True, False])
+def test_attention_cuts_ragged_batches_into_even_pieces(dtype, dh, B, most, tree):
+    """Long and short contexts and requests without rows, in batches of more requests than a wave has lanes."""
+    rng = np.random.default_rng(B + most)
+    ctx, new = rng.integers(0, 3000, B), rng.integers(0, most + 1, B)
+    ctx[1], ctx[-1], new[0], new[-1] = 0, 3000, 0, most
+    c = attention_case(61, ctx, new, 2, 1, dh, 16, dtype, tree)
+    close_to_exact(c, *atspeed_tree_attention(**c, return_lse=True))
 
 
 # ---------------------------------------------------------------- logit rules

@@ -105,6 +105,18 @@ def test_attention_refusals():
         assert lib.atspeed_tree_attention(C.byref(fill(bd.TreeAttentionArgs, **{**ATTN, **kw})), None, 0, None) == OK
 
 
+@pytest.mark.parametrize("kv_heads", [1, 3, 8, 511, 513, 1024])
+@pytest.mark.parametrize("max_new", [1, 16, 40, 200])
+def test_attention_workspace_of_long_contexts(kv_heads, max_new):
+    """Parts of at most 2,048 workgroups of 128 queries (fp32 sums of 128 dims, two numbers a query)."""
+    n = C.c_size_t(1)
+    kw = dict(n_kv_heads=kv_heads, n_heads=kv_heads, max_pages=10 ** 6, max_ctx=10 ** 6, max_new=max_new, n_rows=400)
+    assert bd.load_library().atspeed_tree_attention_workspace_bytes(C.byref(fill(bd.TreeAttentionArgs, **{**ATTN, **kw})), C.byref(n)) == OK
+    assert n.value <= 2048 * 128 * (128 * 4 + 8) + 32
+    # two requests: two pieces of each of their tiles
+    assert (n.value > 0) == (kv_heads * 4 * -(-max_new // 128) <= 2048)
+
+
 def test_rules_refusals():
     good = dict(dtype=bd.FP32, B=2, n_rows=5, n_cols=100, max_hist=10, max_nodes=4, mask_words=1, n_bias=2, n_states=3,
                 n_out_rows=5, logits_stride=100, out_stride=100, bias_stride=100)
