@@ -87,11 +87,15 @@ struct Share {
   int clear;             // from this key on some query may not see a key
   const int* table;
 
-  // False where there is nothing to do.
+  // False where there is nothing to do.  CUT: the requests are cut into pieces (kernels of
+  // their own: the registers of pick() cost the others 2 to 12%).
+  template <bool CUT>
   __device__ __forceinline__ bool init(const TreeAttnArgs& a) {
     int b, qt, split, total;
-    if (a.units) {
+    if constexpr (CUT) {
       if (!pick(a, b, qt, split, total)) return false;
+      // one value a wave, as the compiler cannot tell
+      for (int* x : {&b, &qt, &split, &total, &kvh, &unit, &nsplit, &r0, &nq, &ctx}) *x = __builtin_amdgcn_readfirstlane(*x);
     } else {
       // Workgroup L runs on XCD L % 8: the tiles of one pair stay on one XCD, whose L2
       // then holds the pair's keys; the pairs are dealt round-robin.
@@ -520,7 +524,7 @@ struct Tile {
 // key tiles of their own in turn, staged through registers into a part of LDS that only
 // they use, so there is no barrier until the four results are joined.  Bound by the reads
 // of the cache: two workgroups of a CU hold 128 KB of rows in flight.
-template <class T, int DH, int NQ>
+template <class T, int DH, int NQ, bool CUT>
 __global__ void __launch_bounds__(256, 2) tree_attn_stream_kernel(TreeAttnArgs a) {
   constexpr int KW = sizeof(T) == 2 ? 32 : 16;
   typedef Tile<T, DH, NQ, KW> Tl;
@@ -529,7 +533,7 @@ __global__ void __launch_bounds__(256, 2) tree_attn_stream_kernel(TreeAttnArgs a
   __shared__ float2 ml_s[4][16];
   static_assert(4 * NDB * 64 * 16 <= 4 * 2 * Tl::BYTES, "the join fits the tiles");
   Share s;
-  if (!s.init(a)) return;
+  if (!s.init<CUT>(a)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   char* ks = lds + wave * 2 * Tl::BYTES;
   char* vs = ks + Tl::BYTES;
@@ -623,7 +627,7 @@ __global__ void __launch_bounds__(256, 2) tree_attn_stream_kernel(TreeAttnArgs a
 // instruction: the swizzle is in which chunk a lane asks for), two stages, the next tile
 // in flight during the present one's matrix work.  The loads are written so that the
 // compiler does not count them; the wait for them is explicit.
-template <class T, int DH, int NQ>
+template <class T, int DH, int NQ, bool CUT>
 __global__ void __launch_bounds__(256, 2) tree_attn_tile_kernel(TreeAttnArgs a) {
   constexpr int KW = NQ * 8192 / (DH * (int)sizeof(T)) > 64 ? 64 : NQ * 8192 / (DH * (int)sizeof(T));
   typedef Tile<T, DH, NQ, KW> Tl;
@@ -631,7 +635,7 @@ __global__ void __launch_bounds__(256, 2) tree_attn_tile_kernel(TreeAttnArgs a) 
   constexpr int KPI = 64 / CPR > 0 ? 64 / CPR : 1;        // keys of an instruction
   __shared__ __align__(1024) char lds[2 * 2 * Tl::BYTES];
   Share s;
-  if (!s.init(a)) return;
+  if (!s.init<CUT>(a)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // A tile of up to 64 queries, a request's last: one block a wave instead of two for the
   // first waves (300 nodes x 128 users 1.24 -> 1.22 ms).
@@ -905,15 +909,20 @@ atspeed_status launch_attention(const TreeAttnArgs& p, F kernel, hipStream_t st)
   return ATSPEED_OK;
 }
 
-template <class T, int DH>
-atspeed_status run_attention(const TreeAttnArgs& p, int tile, hipStream_t st) {
-  if (tile == 16) return launch_attention<T, DH>(p, tree_attn_stream_kernel<T, DH, 1>, st);
-  if (tile == 64) return launch_attention<T, DH>(p, tree_attn_tile_kernel<T, DH, 1>, st);
+template <class T, int DH, bool CUT>
+atspeed_status run_attention(const TreeAttnArgs& p, hipStream_t st) {
+  if (p.qb == 16) return launch_attention<T, DH>(p, tree_attn_stream_kernel<T, DH, 1, CUT>, st);
+  if (p.qb == 64) return launch_attention<T, DH>(p, tree_attn_tile_kernel<T, DH, 1, CUT>, st);
   if constexpr (sizeof(T) == 2) {
-    if (tile == 32) return launch_attention<T, DH>(p, tree_attn_stream_kernel<T, DH, 2>, st);
-    return launch_attention<T, DH>(p, tree_attn_tile_kernel<T, DH, 2>, st);
+    if (p.qb == 32) return launch_attention<T, DH>(p, tree_attn_stream_kernel<T, DH, 2, CUT>, st);
+    return launch_attention<T, DH>(p, tree_attn_tile_kernel<T, DH, 2, CUT>, st);
   }
   return fail(ATSPEED_E_DEVICE, "tree attention: no such tile");
+}
+
+template <class T, int DH>
+atspeed_status run_attention(const TreeAttnArgs& p, hipStream_t st) {
+  return p.units ? run_attention<T, DH, true>(p, st) : run_attention<T, DH, false>(p, st);
 }
 
 }  // namespace
@@ -972,10 +981,10 @@ atspeed_status atspeed_tree_attention(const atspeed_tree_attention_args* args, v
   p.q_flip = a.scale < 0.f ? (es == 2 ? 0x80008000u : 0x80000000u) : 0u;
   p.scale = std::max(std::fabs(a.scale) * 1.4426950408889634f, 1e-37f);
   hipStream_t st = (hipStream_t)stream;
-  if (es == 2) return a.d_head == 64 ? run_attention<bf16_t, 64>(p, plan.tile, st) : run_attention<bf16_t, 128>(p, plan.tile, st);
-  if (a.d_head == 32) return run_attention<float, 32>(p, plan.tile, st);
-  if (a.d_head == 64) return run_attention<float, 64>(p, plan.tile, st);
-  return run_attention<float, 128>(p, plan.tile, st);
+  if (es == 2) return a.d_head == 64 ? run_attention<bf16_t, 64>(p, st) : run_attention<bf16_t, 128>(p, st);
+  if (a.d_head == 32) return run_attention<float, 32>(p, st);
+  if (a.d_head == 64) return run_attention<float, 64>(p, st);
+  return run_attention<float, 128>(p, st);
 }
 
 }  // extern "C"
