@@ -4,13 +4,12 @@
 // query heads of one key/value head are the queries of a matrix tile, so grouped heads
 // read the cache once for the group.  Two kernels: up to 32 queries (single tokens,
 // small trees), bound by the reads of the cache, and more, bound by the matrix and
-// vector instructions and the latencies between them; long contexts are split over
-// workgroups and their parts joined.  Measured (us; share of a 4.95 TB/s copy or of a
-// 1,214 TFLOP/s product): 64 single tokens over up to 8,192 keys, 8 of 32 heads, 151
-// (95% of the copy); 60 nodes x 32 users over 144 keys, 32 heads, 29 (97%); trees of 4
-// users over up to 65,536 keys 144 (82%); 300 nodes x 128 users over 1,024 keys 1,260
-// (0.51 PFLOP/s of what the rows see); causal chunks of up to 1,024 x 16 users 108
-// (0.64 PFLOP/s).
+// vector instructions and the latencies between them; long contexts are cut into pieces
+// and their parts joined.  Measured (us; share of a 4.95 TB/s copy or of a 1,214 TFLOP/s
+// product): 64 single tokens over up to 8,192 keys, 8 of 32 heads, 145 (99% of the copy);
+// 60 nodes x 32 users over 144 keys, 32 heads, 33.5 (84%); trees of 4 users over up to
+// 65,536 keys 134 (89%); 300 nodes x 128 users over 1,024 keys 1,230 (0.52 PFLOP/s of
+// what the rows see); causal chunks of up to 1,024 x 16 users 108 (0.64 PFLOP/s).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
