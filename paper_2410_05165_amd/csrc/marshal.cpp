@@ -41,6 +41,15 @@ void check(atspeed_status s) {
   throw Raised{};
 }
 
+// A launch waits where the stream's queue is full: other threads run meanwhile.
+template <class F>
+void enqueue(F&& call) {
+  PyThreadState* state = PyEval_SaveThread();
+  const atspeed_status s = call();
+  PyEval_RestoreThread(state);
+  check(s);
+}
+
 std::string shown(c10::IntArrayRef s) {
   std::string r = "(";
   for (size_t i = 0; i < s.size(); ++i) r += (i ? ", " : "") + std::to_string(s[i]);
@@ -235,7 +244,8 @@ PyObject* page_plan(PyObject*, PyObject* const* o, Py_ssize_t n) {
     a.row_pos = p + R;
     a.slot = p + 2 * R;
     a.tree_slot = p + 3 * R;
-    check(atspeed_page_plan(&a, stream_of(o[9])));
+    void* const st = stream_of(o[9]);
+    enqueue([&] { return atspeed_page_plan(&a, st); });
     Ref r(PyTuple_New(10));
     const int64_t sizes[9] = {1, B, B, B, B + 1, R, R, R, R};
     int64_t begin = 0;
@@ -271,7 +281,8 @@ PyObject* kv_append(PyObject*, PyObject* const* o, Py_ssize_t n) {
     a.k_pages = c.k;
     a.v_pages = c.v;
     a.slot = want_i32(o[4], "slot", {rows}, c.dev);
-    check(atspeed_kv_append(&a, stream_of(o[5])));
+    void* const st = stream_of(o[5]);
+    enqueue([&] { return atspeed_kv_append(&a, st); });
     Py_RETURN_NONE;
   });
 }
@@ -325,7 +336,8 @@ PyObject* tree_attention(PyObject*, PyObject* const* o, Py_ssize_t n) {
     size_t need = 0;
     check(atspeed_tree_attention_workspace_bytes(&a, &need));
     if (need) ws = fresh({(int64_t)need}, c10::ScalarType::Byte, c.dev);
-    check(atspeed_tree_attention(&a, need ? address<void>(ws) : nullptr, need, stream_of(o[12])));
+    void *const st = stream_of(o[12]), *const at = need ? address<void>(ws) : nullptr;
+    enqueue([&] { return atspeed_tree_attention(&a, at, need, st); });
     Ref result(given_or_new(o[10], out));
     if (!with_lse) return result.release();
     Ref sums(THPVariable_Wrap(lse));
@@ -403,7 +415,8 @@ PyObject* logit_rules(PyObject*, PyObject* const* o, Py_ssize_t n) {
     }
     a.state_by_request = flag(o[18]);
     a.state = a.state_by_request ? want_i32(o[12], "state", {B}, dev) : want_i32(o[12], "state", {rows}, dev);
-    check(atspeed_logit_rules(&a, stream_of(o[19])));
+    void* const st = stream_of(o[19]);
+    enqueue([&] { return atspeed_logit_rules(&a, st); });
     return given_or_new(o[16], out);
   });
 }

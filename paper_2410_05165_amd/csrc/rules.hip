@@ -82,7 +82,7 @@ __global__ void __launch_bounds__(kRuleThreads) logit_rules_kernel(atspeed_logit
     if (a.node_token) {
       const int* tok = a.node_token + (int64_t)b * a.max_nodes;
       const uint64_t* m = a.mask ? a.mask + (int64_t)r * a.mask_words : nullptr;
-      const int n = min(a.max_nodes, m ? a.mask_words * 64 : r - a.row_off[b] + 1);
+      const int n = (int)min((int64_t)a.max_nodes, m ? (int64_t)a.mask_words * 64 : r - (int64_t)a.row_off[b] + 1);
       for (int j = tid; j < n; j += kRuleThreads)
         if (!m || ((m[j >> 6] >> (j & 63)) & 1)) see(tok[j]);
     }

@@ -1,6 +1,8 @@
 """The paged operators (step plan, cache append, tree attention, logit rules) against
 plain implementations in Python integers and 64 bits."""
 import math
+import sys
+import threading
 
 import numpy as np
 import pytest
@@ -698,6 +700,53 @@ def test_two_calls_at_once_on_two_streams():
     torch.cuda.synchronize()
     for i in range(2):
         assert all(torch.equal(x, want[i]) for x in got[i])
+
+
+def test_calls_from_two_threads():
+    cases = [attention_case(64 + i, [5000, 300], [2, 30], 8, 2, 128, 16, BF16, True) for i in range(2)]
+    want = [atspeed_tree_attention(**c, return_lse=True) for c in cases]
+    torch.cuda.synchronize()
+    got = [[], []]
+
+    def work(i):
+        with torch.cuda.stream(torch.cuda.Stream(device=DEV)):
+            for _ in range(20):
+                got[i].append(atspeed_tree_attention(**cases[i], return_lse=True))
+            torch.cuda.current_stream().synchronize()
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for i in range(2):
+        assert len(got[i]) == 20 and all(torch.equal(x, y) for r in got[i] for x, y in zip(r, want[i]))
+
+
+def test_calls_keep_no_reference():
+    c = attention_case(66, [5000, 30], [2, 3], 8, 2, 128, 16, BF16, True)
+    r = rules_case(2, 2, [1, 1], 50, F32)
+    out, z = torch.empty_like(c["q"]), torch.empty((2, 50), device=DEV)
+    held = [*c.values(), *r.values(), out, z]
+    refused = dict(c, ctx=c["ctx"].long())
+
+    def calls():
+        for _ in range(5):
+            assert atspeed_tree_attention(**c, out=out) is out and atspeed_logit_rules(**r, out=z) is z
+            atspeed_tree_attention(**c, return_lse=True)
+            try:
+                atspeed_tree_attention(**refused)
+                raise AssertionError("not refused")
+            except ValueError:
+                pass
+
+    calls()
+    before = [sys.getrefcount(t) for t in held if isinstance(t, torch.Tensor)]
+    torch.cuda.synchronize()
+    used = torch.cuda.memory_allocated()
+    calls()
+    assert [sys.getrefcount(t) for t in held if isinstance(t, torch.Tensor)] == before
+    assert torch.cuda.memory_allocated() == used
 
 
 # ---------------------------------------------------------------- refusals that reach the tensors
