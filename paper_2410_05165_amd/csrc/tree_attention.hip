@@ -854,14 +854,19 @@ AttnPlan plan_attention(const atspeed_tree_attention_args& a) {
   const int64_t pairs = (int64_t)a.B * a.n_kv_heads;
   p.cap = (int)std::min<int64_t>((int64_t)a.max_pages * a.page_size, 1 << 30);
   const int64_t keys = std::max<int64_t>(1, std::min<int64_t>((int64_t)a.max_ctx + a.max_new, p.cap));
-  // Queries of a workgroup: the smallest tile that holds them (fp32 has tiles of 16 and
-  // 64).  Launches that do not fill the CUs are bound by the steps each workgroup takes
-  // one after the other; over up to 1,024 keys they take the tiles of few queries, whose
-  // waves share the steps out, though these read the keys once for each (30 rows over 110
-  // keys of d_head 32: 7.2 us in tiles of 64, 5.0 in tiles of 16; 27 rows over 526 keys 21
-  // and 13; but 102 rows x 29 users over 128 keys, 464 workgroups of 32, 11.1 and 13.1).
+  // Queries of a workgroup: the smallest tile that holds them.  fp32 has tiles of 16, 32
+  // and 64; those of 32 take the registers of d_head 128 and, with d_head 64, half of the
+  // waves of a CU, which pays below 256 workgroups (fp32 in tiles of 64 and of 32, us: 24
+  // rows x 40 users over 300 keys, 12 heads of 32, 15.7 and 10.4; 4 rows x 2 users over
+  // 6,000 keys, 32 heads of 64 on 4, 21.8 and 16.6; but 18 rows x 30 users over 150 keys, 32
+  // heads of 64, 15.6 and 19.1).
+  // Launches that do not fill the CUs are bound by the steps each workgroup takes one
+  // after the other; over up to 1,024 keys they take the tiles of few queries, whose waves
+  // share the steps out, though these read the keys once for each (30 rows over 110 keys
+  // of d_head 32: 7.2 us in tiles of 64, 5.0 in tiles of 16; 27 rows over 526 keys 21 and
+  // 13; but 102 rows x 29 users over 128 keys, 464 workgroups of 32, 11.1 and 13.1).
   const int few = bf ? 32 : 16;
-  p.tile = nq <= 16 ? 16 : nq <= few ? few : nq <= 64 || !bf ? 64 : 128;
+  p.tile = nq <= 16 ? 16 : nq <= 32 && (bf || a.d_head == 32 || (a.d_head == 64 && pairs <= 256)) ? 32 : nq <= 64 || !bf ? 64 : 128;
   if (p.tile > few && keys <= 1024 && pairs * ((nq + few - 1) / few) <= 256) p.tile = few;
   p.qtiles = (int)((nq + p.tile - 1) / p.tile);
   // Requests are split where the launch has at least two pieces a tile of queries: into
@@ -912,8 +917,10 @@ template <class T, int DH, bool CUT>
 atspeed_status run_attention(const TreeAttnArgs& p, hipStream_t st) {
   if (p.qb == 16) return launch_attention<T, DH>(p, tree_attn_stream_kernel<T, DH, 1, CUT>, st);
   if (p.qb == 64) return launch_attention<T, DH>(p, tree_attn_tile_kernel<T, DH, 1, CUT>, st);
-  if constexpr (sizeof(T) == 2) {
+  if constexpr (sizeof(T) == 2 || DH <= 64) {
     if (p.qb == 32) return launch_attention<T, DH>(p, tree_attn_stream_kernel<T, DH, 2, CUT>, st);
+  }
+  if constexpr (sizeof(T) == 2) {
     return launch_attention<T, DH>(p, tree_attn_tile_kernel<T, DH, 2, CUT>, st);
   }
   return fail(ATSPEED_E_DEVICE, "tree attention: no such tile");

@@ -485,7 +485,15 @@ def test_attention_is_repeatable(dtype, dh):
     assert torch.equal(a, b)
 
 
-@pytest.mark.parametrize("dtype,dh", [(BF16, 128), (BF16, 64), (F32, 32)])
+@pytest.mark.parametrize("dtype,dh", TYPES)
+@pytest.mark.parametrize("most", [1, 20, 40])
+def test_attention_of_many_short_requests(dtype, dh, most):
+    rng = np.random.default_rng(most)
+    c = attention_case(62, rng.integers(0, 200, 40), rng.integers(0, most + 1, 40), 8, 8, dh, 16, dtype, True)
+    close_to_exact(c, *atspeed_tree_attention(**c, return_lse=True))
+
+
+@pytest.mark.parametrize("dtype,dh", [(BF16, 128), (BF16, 64), (F32, 32), (F32, 64)])
 @pytest.mark.parametrize("B,most", [(5, 40), (64, 1), (70, 1), (70, 9), (130, 80)])
 @pytest.mark.parametrize("tree", [True, False])
 def test_attention_cuts_ragged_batches_into_even_pieces(dtype, dh, B, most, tree):
