@@ -150,11 +150,14 @@ static atspeed_status launch_rules(const atspeed_logit_rules_args& a, hipStream_
   return ATSPEED_OK;
 }
 
-// Rows of up to 1,024 columns are one workgroup each; longer ones go in chunks of
-// 4,096, so that a history is read once per 4,096 columns.
+// Chunks of 1,024 columns where that makes up to 2,048 workgroups, 8 a CU, which then
+// share out what one would do in turn; beyond, chunks of 4,096, so that a history is read
+// once per 4,096 columns (chunks of 4,096 and of 1,024, us: 16 rows of 33,024 bf16 columns
+// 6.5 and 4.6; 2 rows of 17,051 fp32 8.6 and 5.2; 64 rows of 33,024 7.1 and 7.0; but 120
+// rows 10.2 and 11.3, 400 rows of 16,487 16.3 and 20.1).
 template <class T>
 static atspeed_status run_rules(const atspeed_logit_rules_args& a, bool vec, hipStream_t st) {
-  const bool small = a.n_cols <= 1024;
+  const bool small = a.n_cols <= 1024 || (long long)a.n_rows * ((a.n_cols + 1023) / 1024) <= 2048;
   if (vec) return small ? launch_rules<T, 4, 1>(a, st) : launch_rules<T, 4, 4>(a, st);
   return small ? launch_rules<T, 1, 4>(a, st) : launch_rules<T, 1, 16>(a, st);
 }

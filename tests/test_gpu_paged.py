@@ -566,6 +566,12 @@ def test_rules_long_histories_and_many_requests():
     check_rules(rules_case(7, 1024, 1, 33, F32, False, hist=2))
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("cols", [8001, 8192])
+def test_rules_many_long_rows(dtype, cols):
+    check_rules(rules_case(6, 300, [1] * 300, cols, dtype, False))
+
+
 def test_rules_wide_trees():
     check_rules(rules_case(8, 2, [130, 70], 200, F32))
 
