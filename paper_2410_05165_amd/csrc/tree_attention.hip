@@ -864,10 +864,13 @@ AttnPlan plan_attention(const atspeed_tree_attention_args& a) {
   // after the other; over up to 1,024 keys they take the tiles of few queries, whose waves
   // share the steps out, though these read the keys once for each (30 rows over 110 keys
   // of d_head 32: 7.2 us in tiles of 64, 5.0 in tiles of 16; 27 rows over 526 keys 21 and
-  // 13; but 102 rows x 29 users over 128 keys, 464 workgroups of 32, 11.1 and 13.1).
-  const int few = bf ? 32 : 16;
+  // 13; but 102 rows x 29 users over 128 keys, 464 workgroups of 32, 11.1 and 13.1).  fp32,
+  // whose matrix instructions are the slower part, up to two workgroups a CU (50 rows x 30
+  // users over 300 keys, 480 of 32, 8 heads of 64, 20.4 and 16.1; at 960, 60 rows x 56
+  // users over 502 keys, 25.9 and 30.5), if the keys are steps enough to share.
+  const int few = bf || (a.d_head <= 64 && pairs * ((nq + 15) / 16) > 256) ? 32 : 16;
   p.tile = nq <= 16 ? 16 : nq <= 32 && (bf || a.d_head == 32 || (a.d_head == 64 && pairs <= 256)) ? 32 : nq <= 64 || !bf ? 64 : 128;
-  if (p.tile > few && keys <= 1024 && pairs * ((nq + few - 1) / few) <= 256) p.tile = few;
+  if (p.tile > few && keys <= 1024 && pairs * ((nq + few - 1) / few) <= (bf || keys <= 64 ? 256 : 512)) p.tile = few;
   p.qtiles = (int)((nq + p.tile - 1) / p.tile);
   // Requests are split where the launch has at least two pieces a tile of queries: into
   // 512 workgroups, two for each of the 256 CUs, or as few times that as it takes, all of
