@@ -861,16 +861,21 @@ AttnPlan plan_attention(const atspeed_tree_attention_args& a) {
   // 6,000 keys, 32 heads of 64 on 4, 21.8 and 16.6; but 18 rows x 30 users over 150 keys, 32
   // heads of 64, 15.6 and 19.1).
   // Launches that do not fill the CUs are bound by the steps each workgroup takes one
-  // after the other; over up to 1,024 keys they take the tiles of few queries, whose waves
-  // share the steps out, though these read the keys once for each (30 rows over 110 keys
-  // of d_head 32: 7.2 us in tiles of 64, 5.0 in tiles of 16; 27 rows over 526 keys 21 and
-  // 13; but 102 rows x 29 users over 128 keys, 464 workgroups of 32, 11.1 and 13.1).  fp32,
-  // whose matrix instructions are the slower part, up to two workgroups a CU (50 rows x 30
-  // users over 300 keys, 480 of 32, 8 heads of 64, 20.4 and 16.1; at 960, 60 rows x 56
-  // users over 502 keys, 25.9 and 30.5), if the keys are steps enough to share.
-  const int few = bf || (a.d_head <= 64 && pairs * ((nq + 15) / 16) > 256) ? 32 : 16;
+  // after the other; over up to 1,024 keys they take the tiles of few queries, whose four
+  // waves share the steps out, though these read the keys once for each: up to 256 of
+  // them, and up to 1,024 where the larger tiles are 256 at most (fp32, whose matrix
+  // instructions are slower, 384) and the keys more than a step (us, larger tiles and
+  // few: 30 rows over 110 keys, fp32, d_head 32, 7.2 and 5.0; 100 rows x 20 users over 600
+  // keys, 8 heads of 64, 17.0 and 9.3; 900 rows x 4 users over 1,000, 23.8 and 12.0; 50
+  // rows x 30 users over 300 keys, fp32, 20.4 and 16.1; but 12 rows x 50 users over 600
+  // keys, 32 heads on 8, 400 larger tiles, 21.9 and 25.7; 60 rows x 56 users over 502
+  // keys, fp32, 448 larger ones, 25.9 and 30.5; 50 rows x 32 users over 80 keys 8.0 and 9.9).
+  const int few = bf || (a.d_head <= 64 && pairs * ((nq + 15) / 16) > 256) ? 32 : 16, few_step = bf ? 128 : 64;
   p.tile = nq <= 16 ? 16 : nq <= 32 && (bf || a.d_head == 32 || (a.d_head == 64 && pairs <= 256)) ? 32 : nq <= 64 || !bf ? 64 : 128;
-  if (p.tile > few && keys <= 1024 && pairs * ((nq + few - 1) / few) <= (bf || keys <= 64 ? 256 : 512)) p.tile = few;
+  const int64_t in_few = pairs * ((nq + few - 1) / few), in_tiles = pairs * ((nq + p.tile - 1) / p.tile);
+  if (p.tile > few && keys <= 1024 &&
+      (in_few <= 256 || (keys > few_step && in_few <= 1024 && in_tiles <= (bf ? 256 : 384))))
+    p.tile = few;
   p.qtiles = (int)((nq + p.tile - 1) / p.tile);
   // Requests are split where the launch has at least two pieces a tile of queries: into
   // 512 workgroups, two for each of the 256 CUs, or as few times that as it takes, all of
@@ -883,7 +888,7 @@ AttnPlan plan_attention(const atspeed_tree_attention_args& a) {
   // Pieces of under 256 keys lose to their join, and so does any split of up to 10 steps
   // (4 rows x 8 users over 600 keys: 10.2 us in pieces, 8.3 whole; 256 rows x 8 users over
   // 310 keys 31 and 14).
-  const int step = p.tile <= 32 ? (bf ? 128 : 64) : std::min(64, (p.tile / 64) * 8192 / (a.d_head * (bf ? 2 : 4)));
+  const int step = p.tile <= 32 ? few_step : std::min(64, (p.tile / 64) * 8192 / (a.d_head * (bf ? 2 : 4)));
   const int64_t tiles = (int64_t)a.B * p.qtiles;
   int64_t units = std::max(1, 512 / a.n_kv_heads);
   while (units < 2 * tiles && units * 2 * a.n_kv_heads <= 2048) units *= 2;

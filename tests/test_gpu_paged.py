@@ -493,6 +493,18 @@ def test_attention_of_many_short_requests(dtype, dh, most):
     close_to_exact(c, *atspeed_tree_attention(**c, return_lse=True))
 
 
+@pytest.mark.parametrize("dtype,dh", TYPES)
+@pytest.mark.parametrize("most", [60, 200])
+@pytest.mark.parametrize("tree", [True, False])
+def test_attention_of_many_requests_with_many_rows(dtype, dh, most, tree):
+    """Launches that fill the GPU with tiles of 64 and 128 queries, last tiles of every size."""
+    rng = np.random.default_rng(most)
+    ctx, new = rng.integers(0, 90, 50), rng.integers(0, most + 1, 50)
+    new[:4] = most, min(most, 129), min(most, 192), min(most, 65)
+    c = attention_case(63, ctx, new, 8, 8, dh, 16, dtype, tree)
+    close_to_exact(c, *atspeed_tree_attention(**c, return_lse=True))
+
+
 @pytest.mark.parametrize("dtype,dh", [(BF16, 128), (BF16, 64), (F32, 32), (F32, 64)])
 @pytest.mark.parametrize("B,most", [(5, 40), (64, 1), (70, 1), (70, 9), (130, 80)])
 @pytest.mark.parametrize("tree", [True, False])
