@@ -4,6 +4,8 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -12,19 +14,26 @@ MARSHAL = os.path.join(HERE, "_marshal.so")
 SOURCES = ["runtime.hip", "gemm.hip", "gemm_f32.hip", "attention.hip", "misc.hip", "select.hip", "relaxed.hip", "align.hip",
            "paged.hip", "tree_attention.hip", "rules.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wno-unused-result", "-fvisibility=hidden"]
 
 
-def build(verbose: bool = False) -> str:
-    cmd = [HIPCC, *FLAGS, *[os.path.join(CSRC, s) for s in SOURCES], "-o", LIB + ".tmp"]
+def _run(cmd, verbose: bool) -> None:
     if verbose:
         print(" ".join(cmd), flush=True)
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         sys.stderr.write(r.stdout + r.stderr)
-        raise RuntimeError("hipcc failed")
+        raise RuntimeError(os.path.basename(cmd[0]) + " failed")
+
+
+def build(verbose: bool = False) -> str:
+    with tempfile.TemporaryDirectory() as tmp, ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
+        objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
+        list(pool.map(lambda so: _run([HIPCC, *FLAGS, "-c", os.path.join(CSRC, so[0]), "-o", so[1]], verbose),
+                      zip(SOURCES, objects)))
+        _run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", *objects, "-o", LIB + ".tmp"], verbose)
     os.replace(LIB + ".tmp", LIB)
     build_marshal(verbose)
     return LIB
@@ -42,12 +51,7 @@ def build_marshal(verbose: bool = False) -> str:
            os.path.join(CSRC, "marshal.cpp"), "-o", MARSHAL + ".tmp",
            "-L" + os.path.join(os.path.dirname(torch.__file__), "lib"), "-lc10", "-ltorch_cpu", "-ltorch_python",
            "-L" + HERE, "-l:libatspeed.so", "-Wl,-rpath,$ORIGIN"]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        sys.stderr.write(r.stdout + r.stderr)
-        raise RuntimeError(cmd[0] + " failed")
+    _run(cmd, verbose)
     os.replace(MARSHAL + ".tmp", MARSHAL)
     return MARSHAL
 
