@@ -8,7 +8,6 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-import struct
 from typing import Dict, Optional
 
 import numpy as np
@@ -80,22 +79,10 @@ class AlignArgs(C.Structure):
 
 
 def _struct(name, spec):
-    """A ctypes structure from "type: name name ..." groups in the header's field order.
-
-    ``pack(*values)`` gives its bytes (pointers as integers, 0 for null) in a quarter of the time that an
-    instance takes to fill: these calls come once a layer.
-    """
-    kinds = {"i": (C.c_int32, "i"), "l": (C.c_int64, "q"), "f": (C.c_float, "f"), "p": (C.c_void_p, "P")}
-    parts = [(n, kinds[part.split(":")[0].strip()]) for part in spec.split(";") for n in part.split(":")[1].split()]
-    layout = struct.Struct("@" + "".join(code for _, (_, code) in parts))
-
-    def pack(*values):
-        try:
-            return layout.pack(*values)
-        except struct.error as e:
-            raise ValueError(f"{name}: {e}") from None
-
-    return type(name, (C.Structure,), {"_fields_": [(n, kind) for n, (kind, _) in parts], "pack": staticmethod(pack)})
+    """A ctypes structure from "type: name name ..." groups in the header's field order."""
+    kinds = {"i": C.c_int32, "l": C.c_int64, "f": C.c_float, "p": C.c_void_p}
+    fields = [(n, kinds[part.split(":")[0].strip()]) for part in spec.split(";") for n in part.split(":")[1].split()]
+    return type(name, (C.Structure,), {"_fields_": fields})
 
 
 # Arguments of the context-free calls (atspeed_pages members are spelled out).
@@ -152,7 +139,6 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
     lib.atspeed_align_step.argtypes = [vp, C.POINTER(AlignArgs), C.POINTER(C.c_double)]
     lib.atspeed_target_search.argtypes = [vp, i32, i32, pi32, pi32, pf, pi32, pi32, pi32, pi32]
     lib.atspeed_mixed_search.argtypes = [vp, C.c_float, i32, i32, pi32, pi32, pf, pi32, pi32, pi32, pi32]
-    # the argument structures: by reference, or their bytes
     lib.atspeed_page_plan.argtypes = [vp, vp]
     lib.atspeed_kv_append.argtypes = [vp, vp]
     lib.atspeed_tree_attention_workspace_bytes.argtypes = [vp, C.POINTER(C.c_size_t)]
@@ -336,7 +322,7 @@ class Engine:
             return
         from .paged import pack_rules
         args = pack_rules(self.n_item, self.w.target.item_base, self.cfg.max_batch, self.device, **rules)
-        self._check(self.lib.atspeed_set_logit_rules(self.ctx, args))
+        self._check(self.lib.atspeed_set_logit_rules(self.ctx, C.byref(args)))
         self._rules = rules
 
     def atspeed_get_state(self, B: int):

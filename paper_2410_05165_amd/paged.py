@@ -102,14 +102,14 @@ def pack_rules(cols: int, token_base: int, B: int, device, history=None, hist_le
         raise ValueError(f"bias: want float32 [n, {cols}] on GPU {dev}, rows contiguous")
     biases = (0, 0) if bias is None else (bias.data_ptr(), bias.stride(0) if n_bias > 1 else cols)
     hist, states = 0 if history is None else history.shape[-1], 0 if allowed is None else allowed.shape[0]
-    return LogitRulesArgs.pack(FP32, B, 0, cols, token_base, hist, 0, 0, n_bias, states, 0, 1, mask_value, 0, 0, 0, 0, 0, 0,
-                               _want(history, "history", i32, (B, hist), dev), _want(hist_len, "hist_len", i32, vec, dev),
-                               0, 0, _want(repetition, "repetition", f32, vec, dev),
-                               _want(frequency, "frequency", f32, vec, dev), _want(presence, "presence", f32, vec, dev),
-                               _want(temperature, "temperature", f32, vec, dev), *biases,
-                               _want(bias_index, "bias_index", i32, vec, dev),
-                               _want(allowed, "allowed", i32, (states, (cols + 31) // 32), dev),
-                               _want(state, "state", i32, vec, dev))
+    return LogitRulesArgs(FP32, B, 0, cols, token_base, hist, 0, 0, n_bias, states, 0, 1, mask_value, 0, 0, 0, 0, 0, 0,
+                          _want(history, "history", i32, (B, hist), dev), _want(hist_len, "hist_len", i32, vec, dev),
+                          0, 0, _want(repetition, "repetition", f32, vec, dev),
+                          _want(frequency, "frequency", f32, vec, dev), _want(presence, "presence", f32, vec, dev),
+                          _want(temperature, "temperature", f32, vec, dev), *biases,
+                          _want(bias_index, "bias_index", i32, vec, dev),
+                          _want(allowed, "allowed", i32, (states, (cols + 31) // 32), dev),
+                          _want(state, "state", i32, vec, dev))
 
 
 def atspeed_logit_rules(logits, row_off, token_base: int = 0, history=None, hist_len=None, repetition=None,

@@ -30,10 +30,6 @@ def test_structures_follow_the_header(cls, name):
             else:
                 want.append((n, C.c_void_p if "*" in kind else kinds[kind.strip()]))
     assert want == [(n, t) for n, t in cls._fields_]
-    # the packed bytes are the structure's
-    values = [2.5 if t is C.c_float else i + 1 for i, (_, t) in enumerate(want)]
-    data = cls.pack(*values)
-    assert data == bytes(cls(*values))[:len(data)] and C.sizeof(cls) - len(data) < 8
 
 
 def fill(cls, **kw):
