@@ -508,11 +508,12 @@ ATSPEED_API atspeed_status atspeed_get_timing(atspeed_ctx* ctx, atspeed_kernel_t
  *                 i-th row of a chain, keep + depth - 1 in a tree); slot the cache
  *                 slot block_table[b][(keep + i) / page_size] * page_size +
  *                 (keep + i) % page_size; tree_slot b * max_nodes + i (the row of a
- *                 padded [B, max_nodes] array such as atspeed_accept's logits; i for
- *                 chains).  All four are -1 past the last row; row_pos and slot are
- *                 -1 for the rows of refused requests; row_pos is -1 for rows whose
- *                 path holds a bad parent, and slot is -1 where the page is not
- *                 in 0 .. n_pool - 1.
+ *                 padded [B, max_nodes] array such as atspeed_accept's logits, -1
+ *                 for the rows from max_nodes on of a request that is refused for
+ *                 them; i for chains).  All four are -1 past the last row; row_pos
+ *                 and slot are -1 for the rows of refused requests; row_pos is -1
+ *                 for rows whose path holds a bad parent, and slot is -1 where the
+ *                 page is not in 0 .. n_pool - 1.
  *   mask [max_rows, ceil(max_nodes / 64)]: bit j % 64 of word j / 64 of a row is set
  *                 for its j-th sibling row where that is the row itself or an
  *                 ancestor; zero past the last row, for refused requests and for

@@ -165,7 +165,8 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(PlanArgs p) {
       b = owner(row_off, B, r);
       user = b;
       i = r - row_off[b];
-      ts = a.parent ? b * a.max_nodes + i : i;
+      // a request of more rows than nodes (refused) has no place for the others: they would be the next one's
+      ts = !a.parent ? i : i < a.max_nodes ? b * a.max_nodes + i : -1;
       if (keep_s[b] >= 0) {
         const int at_pos = keep_s[b] + i, pg = at_pos >> shift;
         // pages the request had are in its table, the others where the table entries come from

@@ -45,7 +45,8 @@ def plan(held, keep, add, table, free, n_free, page, max_rows, parent=None):
         for r in range(off[b], min(off[b + 1], max_rows)):
             i = r - off[b]
             rows["row_user"][r] = b
-            rows["tree_slot"][r] = i if parent is None else b * len(parent[0]) + i
+            if parent is None or i < len(parent[0]):      # rows past a request's nodes are no rows of [B, max_nodes]
+                rows["tree_slot"][r] = i if parent is None else b * len(parent[0]) + i
             if refused[b]:
                 continue
             p = keep[b] + i
