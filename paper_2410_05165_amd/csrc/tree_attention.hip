@@ -216,6 +216,28 @@ struct TileRows {
   }
 };
 
+// The keys of a wave's or workgroup's tiles in which values were left out (Tile::finite).
+struct Holes {
+  int begin = 1 << 30, end = 0;
+  __device__ __forceinline__ void add(bool any_of_wave, int k0, int keys) {
+    if (!any_of_wave) return;
+    begin = min(begin, k0);
+    end = k0 + keys;
+  }
+  // Those of the four waves (waits for them).
+  __device__ __forceinline__ bool join(int2 (&all)[4], int wave) {
+    if (!__syncthreads_or(end != 0)) return false;
+    if ((threadIdx.x & 63) == 0) all[wave] = int2{begin, end};
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      begin = min(begin, all[w].x);
+      end = max(end, all[w].y);
+    }
+    return true;
+  }
+};
+
 // The mask words that hold bits j0 .. j0 + 63 of a row, and those bits.  Context keys
 // (j < 0) are always seen, bits past the words never.
 struct MaskWords {
@@ -454,32 +476,36 @@ struct Tile {
     return bad;
   }
   // ... and here they reach the rows that see them: p is positive there, so they are
-  // what they add.
-  __device__ __forceinline__ void add_not_finite(const TreeAttnArgs& a, const Share& s) {
-    for (int key = s.kbeg; key < s.kend; ++key) {
+  // what they add.  Dims (d0 + i * dstep) * 16 + 4g .. + 3 of query block n, from
+  // the keys of `holes` alone, which has all that were left out.
+  template <int ND>
+  __device__ __forceinline__ void add_not_finite(const TreeAttnArgs& a, const Share& s, const Holes& holes, int n, int d0,
+                                                 int dstep, f32x4_t (&x)[ND]) const {
+    const int end = min(holes.end, s.kend);
+    for (int key = holes.begin; key < end; ++key) {
       const int page = s.table[key >> a.shift];
       if ((unsigned)page >= (unsigned)a.n_pool) continue;
+      const int j0 = key - s.ctx;
+      uint64_t bits;
+      if (a.mask) {
+        MaskWords w;
+        w.load(a.mask + qrow[n] * a.words, a.words, j0);
+        bits = w.bits(j0);
+      } else {
+        bits = chain_bits(qi[n], j0);
+      }
+      if (!(bits & 1)) continue;
       const uint32_t row = page * a.v_page + (key & a.tail) * a.v_token;
       const T* vp = reinterpret_cast<const T*>(a.v + (uint64_t)row * a.unit + s.kvh * a.v_head);
 #pragma unroll
-      for (int n = 0; n < NQ; ++n) {
-        const int j0 = key - s.ctx;
-        uint64_t bits;
-        if (a.mask) {
-          MaskWords w;
-          w.load(a.mask + qrow[n] * a.words, a.words, j0);
-          bits = w.bits(j0);
-        } else {
-          bits = chain_bits(qi[n], j0);
+      for (int i = 0; i < ND; ++i) {
+        const int d = d0 + i * dstep;
+        if (d >= NDB) break;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float v = St<T>::ld(vp + d * 16 + g * 4 + e);
+          if (!(fabsf(v) < INFINITY)) x[i][e] += v;
         }
-        if (!(bits & 1)) continue;
-#pragma unroll
-        for (int d = 0; d < NDB; ++d)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float v = St<T>::ld(vp + d * 16 + g * 4 + e);
-            if (!(fabsf(v) < INFINITY)) o[n][d][e] += v;
-          }
       }
     }
   }
@@ -530,6 +556,7 @@ __global__ void __launch_bounds__(256, 2) tree_attn_stream_kernel(TreeAttnArgs a
   constexpr int CPR = Tl::CPR, ROWB = Tl::ROWB, NDB = Tl::NDB, NCH = KW * CPR / 64;
   __shared__ __align__(16) char lds[4 * 2 * Tl::BYTES];
   __shared__ float2 ml_s[4][16];
+  __shared__ int2 holes_s[4];
   static_assert(4 * NDB * 64 * 16 <= 4 * 2 * Tl::BYTES, "the join fits the tiles");
   Share s;
   if (!s.init<CUT>(a)) return;
@@ -554,13 +581,15 @@ __global__ void __launch_bounds__(256, 2) tree_attn_stream_kernel(TreeAttnArgs a
   Tl t;
   t.init(a, s, s.q0);
   const int i_first = s.q0 / a.G;
-  bool bad = false;
+  Holes holes;
 
   for (int k0 = first; k0 < s.kend; k0 += 4 * KW) {
     const uint64_t there = rows.there;
     if (there != Tl::ALL || k0 + KW > s.clear) {
+      bool bad = false;
 #pragma unroll
       for (int c = 0; c < NCH; ++c) bad |= Tl::finite(vreg[c]);
+      holes.add(__any(bad), k0, KW);
     }
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
@@ -591,9 +620,11 @@ __global__ void __launch_bounds__(256, 2) tree_attn_stream_kernel(TreeAttnArgs a
     t.template step<NQ>(a, ks, vs, full, bits, [](int) {});
   }
 
-  if (__syncthreads_or(bad) && wave == 0) t.add_not_finite(a, s);
+  const bool missing = holes.join(holes_s, wave);
   t.sum_lanes();
-  // join of the four waves, 16 queries at a time; each wave writes a share of the dims
+  // join of the four waves, 16 queries at a time; each wave writes a share of the dims, to
+  // which it adds what was left out of them: behind the join, since the weight of a wave
+  // that saw no key of a query is 0
   f32x4_t* ob = reinterpret_cast<f32x4_t*>(lds);
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
@@ -611,12 +642,20 @@ __global__ void __launch_bounds__(256, 2) tree_attn_stream_kernel(TreeAttnArgs a
       w[k] = x.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x.x - mm);
       ll += x.y * w[k];
     }
-    for (int d = wave; d < NDB; d += 4) {
-      f32x4_t x = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    constexpr int ND = (NDB + 3) / 4;
+    f32x4_t x[ND];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) x += ob[(k * NDB + d) * 64 + lane] * w[k];
-      t.put(a, s, n, d, x, mm, ll);
+    for (int i = 0; i < ND; ++i) {
+      x[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      const int d = wave + i * 4;
+      if (d < NDB)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[i] += ob[(k * NDB + d) * 64 + lane] * w[k];
     }
+    if (missing) t.add_not_finite(a, s, holes, n, wave, 4, x);
+#pragma unroll
+    for (int i = 0; i < ND; ++i)
+      if (wave + i * 4 < NDB) t.put(a, s, n, wave + i * 4, x[i], mm, ll);
   }
 }
 
@@ -633,6 +672,7 @@ __global__ void __launch_bounds__(256, 2) tree_attn_tile_kernel(TreeAttnArgs a) 
   constexpr int CPR = Tl::CPR, NIN = Tl::BYTES / 4096;   // wave instructions per wave for K, and for V
   constexpr int KPI = 64 / CPR > 0 ? 64 / CPR : 1;        // keys of an instruction
   __shared__ __align__(1024) char lds[2 * 2 * Tl::BYTES];
+  __shared__ int2 holes_s[4];
   Share s;
   if (!s.init<CUT>(a)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -676,7 +716,7 @@ __global__ void __launch_bounds__(256, 2) tree_attn_tile_kernel(TreeAttnArgs a) 
   Tl t;
   t.init(a, s, active ? first : s.nq - 1);
   const int i_first = (active ? first : s.nq - 1) / a.G;
-  bool bad = false;
+  Holes holes;
   auto run = [&](auto blocks) {
     constexpr int NB = decltype(blocks)::value;
     MaskWords words[NB];
@@ -710,6 +750,7 @@ __global__ void __launch_bounds__(256, 2) tree_attn_tile_kernel(TreeAttnArgs a) 
         pg = s.page(a, k0 + 2 * KW, KW);
       }
       if (there != Tl::ALL || k0 + KW > s.clear) {
+        bool bad = false;
 #pragma unroll
         for (int c = 0; c < NIN; ++c) {
           u32x4_t* p = reinterpret_cast<u32x4_t*>(vs) + c * 256 + threadIdx.x;
@@ -719,6 +760,7 @@ __global__ void __launch_bounds__(256, 2) tree_attn_tile_kernel(TreeAttnArgs a) 
             bad = true;
           }
         }
+        holes.add(__any(bad), k0, KW);
         __syncthreads();
       }
       bool some = full;
@@ -740,9 +782,14 @@ __global__ void __launch_bounds__(256, 2) tree_attn_tile_kernel(TreeAttnArgs a) 
   if (half) run(std::integral_constant<int, 1>{});
   else run(std::integral_constant<int, NQ>{});
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing is written to LDS behind the workgroup's end
-  if (__syncthreads_or(bad)) t.add_not_finite(a, s);
+  const bool missing = holes.join(holes_s, wave);
   t.sum_lanes();
   if (!active) return;
+  if (missing) {
+#pragma unroll
+    for (int n = 0; n < NQ; ++n)
+      if (n == 0 || !half) t.add_not_finite(a, s, holes, n, 0, 1, t.o[n]);
+  }
 #pragma unroll
   for (int n = 0; n < NQ; ++n)
     if (n == 0 || !half)

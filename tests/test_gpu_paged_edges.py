@@ -1,4 +1,6 @@
-"""Edges of the paged operators: malformed requests."""
+"""Edges of the paged operators: malformed requests, rows whose only key is not finite."""
+import math
+
 import numpy as np
 import pytest
 
@@ -6,8 +8,8 @@ pytestmark = pytest.mark.gpu
 
 torch = pytest.importorskip("torch")
 
-from test_gpu_paged import DEV, ints  # noqa: E402
-from paper_2410_05165_amd.paged import atspeed_logit_rules, atspeed_page_plan  # noqa: E402
+from test_gpu_paged import BF16, DEV, F32, TYPES, attention_case, ints  # noqa: E402
+from paper_2410_05165_amd.paged import atspeed_logit_rules, atspeed_page_plan, atspeed_tree_attention  # noqa: E402
 
 
 # ---------------------------------------------------------------- step plan
@@ -40,3 +42,54 @@ def test_a_malformed_request_leaves_its_neighbours_rows(add):
     for b in range(3):
         n = min(6, off[b + 1] - off[b])
         assert torch.equal(out[b, :n], logits[off[b]:off[b] + n]) and bool((out[b, n:] == 7.0).all()), b
+
+
+# ---------------------------------------------------------------- attention
+
+def roots(c, n):
+    """Every new row sees the context and itself alone."""
+    rows = torch.arange(n, device=DEV)
+    c["mask"] = torch.zeros((n, -(-n // 64)), dtype=torch.int64, device=DEV)
+    c["mask"][rows, rows // 64] = torch.ones((), dtype=torch.int64, device=DEV) << (rows % 64)
+    return c
+
+
+def key_row(c, b, p):
+    """Where key p of request b lies: page, token."""
+    page = c["k_cache"].shape[1]
+    return int(c["block_table"][b, p // page]), p % page
+
+
+@pytest.mark.parametrize("dtype,dh", TYPES)
+@pytest.mark.parametrize("ctx", [0, 5])
+@pytest.mark.parametrize("n", [5, 40, 90, 150])
+def test_a_row_whose_own_value_is_infinite(dtype, dh, ctx, n):
+    """Rows that see their own key (and a few of the context) get the infinity of its value, whichever wave it falls to."""
+    c = roots(attention_case(n + ctx, [ctx], [n], 4, 2, dh, 16, dtype, True), n)
+    clean = atspeed_tree_attention(**c)
+    for r in range(0, n, max(1, n // 12)):
+        page, token = key_row(c, 0, ctx + r)
+        kept = c["v_cache"][page, token, 0, 5].clone()
+        for poison in (math.inf, -math.inf):
+            c["v_cache"][page, token, 0, 5] = poison
+            got = atspeed_tree_attention(**c)
+            assert bool((got[r, :2, 5] == poison).all()), (r, got[r, :2, 5])
+            got[r, :2, 5] = clean[r, :2, 5]
+            assert torch.equal(got, clean)
+        c["v_cache"][page, token, 0, 5] = kept
+
+
+@pytest.mark.parametrize("dtype,dh", [(BF16, 128), (F32, 64)])
+@pytest.mark.parametrize("n", [20, 70])
+def test_infinite_values_in_pieces_that_begin_among_the_new_keys(dtype, dh, n):
+    for ctx in range(4970, 5070, 17):
+        c = roots(attention_case(ctx, [ctx, 9], [n, 0], 4, 2, dh, 16, dtype, True), n)
+        clean = atspeed_tree_attention(**c)
+        at = list(range(1, n, 6))
+        for r in at:
+            page, token = key_row(c, 0, ctx + r)
+            c["v_cache"][page, token, 1, 3] = math.inf
+        got = atspeed_tree_attention(**c)
+        assert bool((got[at, 2:, 3] == math.inf).all()), ctx
+        got[at, 2:, 3] = clean[at, 2:, 3]
+        assert torch.equal(got, clean), ctx
