@@ -203,16 +203,25 @@ struct Share {
   }
 };
 
-// Rows of keys and values of one tile: lane i holds key i's.
+// Rows of keys and values of one tile: lane i holds key i's.  Where a key is not there, it
+// holds the first key's that is (page 0's where none is): what lies elsewhere in the cache
+// is not the request's, and values that are not finite there would cost it a search.
 struct TileRows {
-  uint32_t k, v;     // units; a readable row where the key is not there
+  uint32_t k, v;     // units
   uint64_t there;    // bit i: key i is there
-  __device__ __forceinline__ void set(const TreeAttnArgs& a, int k0, int page) {
+  // all: the bits of a whole tile.
+  __device__ __forceinline__ void set(const TreeAttnArgs& a, int k0, int page, uint64_t all) {
     const bool ok = (unsigned)page < (unsigned)a.n_pool;
     const uint32_t pg = ok ? page : 0, tok = (k0 + (threadIdx.x & 63)) & a.tail;
     k = pg * a.k_page + tok * a.k_token;
     v = pg * a.v_page + tok * a.v_token;
     there = __ballot(ok);
+    if (there != 0 && there != all) {
+      const int first = __ffsll((unsigned long long)there) - 1;
+      const uint32_t k1 = __builtin_amdgcn_readlane(k, first), v1 = __builtin_amdgcn_readlane(v, first);
+      k = ok ? k : k1;
+      v = ok ? v : v1;
+    }
   }
 };
 
@@ -575,7 +584,7 @@ __global__ void __launch_bounds__(256, 2) tree_attn_stream_kernel(TreeAttnArgs a
       vreg[c] = *reinterpret_cast<const u32x4_t*>(a.v + s.kvh * a.v_head + j * 16 + (uint64_t)__shfl(rows.v, key) * a.unit);
     }
   };
-  rows.set(a, first, pg);
+  rows.set(a, first, pg, Tl::ALL);
   if (first < s.kend) fetch();
   pg = s.page(a, first + 4 * KW, KW);
   Tl t;
@@ -589,7 +598,7 @@ __global__ void __launch_bounds__(256, 2) tree_attn_stream_kernel(TreeAttnArgs a
       bool bad = false;
 #pragma unroll
       for (int c = 0; c < NCH; ++c) bad |= Tl::finite(vreg[c]);
-      holes.add(__any(bad), k0, KW);
+      holes.add(there != 0 && __any(bad), k0, KW);
     }
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
@@ -598,7 +607,7 @@ __global__ void __launch_bounds__(256, 2) tree_attn_stream_kernel(TreeAttnArgs a
       *reinterpret_cast<u32x4_t*>(vs + key * ROWB + (j ^ Tl::vswz(key)) * 16) = vreg[c];
     }
     if (k0 + 4 * KW < s.kend) {
-      rows.set(a, k0 + 4 * KW, pg);
+      rows.set(a, k0 + 4 * KW, pg, Tl::ALL);
       fetch();
       pg = s.page(a, k0 + 8 * KW, KW);
     }
@@ -710,7 +719,7 @@ __global__ void __launch_bounds__(256, 2) tree_attn_tile_kernel(TreeAttnArgs a) 
 #pragma unroll
     for (int k = 0; k < Tl::NKS; ++k) some_dma(k, stage);
   };
-  rows.set(a, s.kbeg, pg);
+  rows.set(a, s.kbeg, pg, Tl::ALL);
   if (s.kbeg < s.kend) fetch(0);
   pg = s.page(a, s.kbeg + KW, KW);
   Tl t;
@@ -745,7 +754,7 @@ __global__ void __launch_bounds__(256, 2) tree_attn_tile_kernel(TreeAttnArgs a) 
       __syncthreads();
       const bool more = k0 + KW < s.kend;
       if (more) {
-        rows.set(a, k0 + KW, pg);
+        rows.set(a, k0 + KW, pg, Tl::ALL);
         load_words(k0 + KW);
         pg = s.page(a, k0 + 2 * KW, KW);
       }
@@ -760,7 +769,7 @@ __global__ void __launch_bounds__(256, 2) tree_attn_tile_kernel(TreeAttnArgs a) 
             bad = true;
           }
         }
-        holes.add(__any(bad), k0, KW);
+        holes.add(there != 0 && __any(bad), k0, KW);
         __syncthreads();
       }
       bool some = full;
