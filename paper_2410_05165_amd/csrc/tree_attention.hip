@@ -397,7 +397,8 @@ struct Tile {
       for (int n = 0; n < NB; ++n) {
         float x = fmaxf(mx[n], __shfl_xor(mx[n], 16));
         x = fmaxf(x, __shfl_xor(x, 32));
-        const float mnew = fmaxf(m[n], x);
+        // a query's own scores alone move its maximum, and with it its roundings
+        const float mnew = x > m[n] + kSlack ? x : m[n];
         const float alpha = m[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[n] - mnew);
         m[n] = mnew;
         lsum[n] *= alpha;

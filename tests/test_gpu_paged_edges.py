@@ -1,5 +1,5 @@
 """Edges of the paged operators: malformed requests, rows whose only key is not finite, keys
-that are not there."""
+that are not there, and keys of other branches."""
 import math
 
 import numpy as np
@@ -124,3 +124,21 @@ def test_values_of_pages_that_are_not_a_requests_own_cost_it_nothing(dtype, dh, 
     after = time_of(lambda: atspeed_tree_attention(**c))
     # the same bits by the same instructions; a search of every key made it 12 to 22 times as long
     assert after < 2.5 * before, f"{before * 1e3:.1f} us with page 0 clean, {after * 1e3:.1f} with NaN in it"
+
+
+@pytest.mark.parametrize("dtype,dh", TYPES)
+@pytest.mark.parametrize("ctx,n", [(0, 30), (40, 3), (100, 60), (100, 150), (5000, 12), (5000, 70)])
+def test_finite_keys_of_other_branches_do_not_move_a_row(dtype, dh, ctx, n):
+    """A key that only its own row sees, however large, changes no bit of the others."""
+    c = roots(attention_case(ctx + n, [ctx, 3], [n, 2], 4, 2, dh, 16, dtype, True, scale_q=4.0), n + 2)
+    c["mask"][n:, 0] = torch.tensor([1, 3], device=DEV)
+    clean, clean_lse = atspeed_tree_attention(**c, return_lse=True)
+    for r in (0, n // 2, n - 1):
+        page, token = key_row(c, 0, ctx + r)
+        kept = c["k_cache"][page, token].clone()
+        # along the row's own query: its score, and by chance others', rise by hundreds
+        c["k_cache"][page, token] = (c["q"][r].view(2, 2, dh).sum(1).float() * 40).to(dtype)
+        got, lse = atspeed_tree_attention(**c, return_lse=True)
+        rest = [i for i in range(n + 2) if i != r]
+        assert torch.equal(got[rest], clean[rest]) and torch.equal(lse[rest], clean_lse[rest]), r
+        c["k_cache"][page, token] = kept
