@@ -76,6 +76,13 @@ __device__ __forceinline__ N wave_scan(N x) {
   x += from(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});   // 31 to the rows behind
   return x;
 }
+// Orders a wave's LDS accesses before and behind it, in the compiler's eyes too: what its
+// lanes wrote is there for the others (the hardware keeps a wave's LDS accesses in order).
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 __device__ __forceinline__ int round_up64(int n) { return (n + 63) & ~63; }
 
 // One workgroup's share: a request, a key/value head, a tile of its queries (row i, head
@@ -601,12 +608,14 @@ __global__ void __launch_bounds__(256, 2) tree_attn_stream_kernel(TreeAttnArgs a
       for (int c = 0; c < NCH; ++c) bad |= Tl::finite(vreg[c]);
       holes.add(there != 0 && __any(bad), k0, KW);
     }
+    wave_sync();   // the lanes have read the tile before
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
       const int key = (c * 64 + lane) / CPR, j = (c * 64 + lane) % CPR;
       *reinterpret_cast<u32x4_t*>(ks + key * ROWB + (j ^ Tl::kswz(key)) * 16) = kreg[c];
       *reinterpret_cast<u32x4_t*>(vs + key * ROWB + (j ^ Tl::vswz(key)) * 16) = vreg[c];
     }
+    wave_sync();   // the tile is written
     if (k0 + 4 * KW < s.kend) {
       rows.set(a, k0 + 4 * KW, pg, Tl::ALL);
       fetch();
