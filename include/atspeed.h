@@ -578,8 +578,8 @@ ATSPEED_API atspeed_status atspeed_kv_append(const atspeed_kv_append_args* args,
  * and lse -inf.  What a key or value holds that a row does not see does not reach that
  * row, NaN included.
  *   dtype ATSPEED_BF16: d_head 64 or 128; ATSPEED_FP32: d_head 32, 64 or 128; of q,
- *     out and both caches.  Scores, softmax and sums are fp32; bf16 probabilities
- *     meet the values as bf16.
+ *     out and both caches.  Scores, softmax and sums are fp32; over bf16 caches the
+ *     probabilities meet the values as pairs of bf16 numbers (off by 2^-15 at most).
  *   q row r, head h starts at q + r * q_row_stride + h * q_head_stride (out
  *     likewise; elements), multiples of 16 bytes.  out may be q itself with q's strides.
  *   row_off [B + 1], ctx [B], mask [n_rows, mask_words] as atspeed_page_plan writes

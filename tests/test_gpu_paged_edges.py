@@ -1,5 +1,5 @@
-"""Edges of the paged operators: malformed requests, rows whose only key is not finite, keys
-that are not there, and keys of other branches."""
+"""Edges of the paged operators: malformed requests, rows whose only key is not finite, keys that are
+not there, keys of other branches, and what probabilities keep of their 32 bits."""
 import math
 
 import numpy as np
@@ -9,6 +9,7 @@ pytestmark = pytest.mark.gpu
 
 torch = pytest.importorskip("torch")
 
+import _paged_reference as ref  # noqa: E402
 from test_gpu_paged import BF16, DEV, F32, TYPES, attention_case, ints  # noqa: E402
 from paper_2410_05165_amd.paged import atspeed_logit_rules, atspeed_page_plan, atspeed_tree_attention  # noqa: E402
 
@@ -142,3 +143,20 @@ def test_finite_keys_of_other_branches_do_not_move_a_row(dtype, dh, ctx, n):
         rest = [i for i in range(n + 2) if i != r]
         assert torch.equal(got[rest], clean[rest]) and torch.equal(lse[rest], clean_lse[rest]), r
         c["k_cache"][page, token] = kept
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("ctx,new,tree", [([50, 200], [1, 9], True), ([0, 300], [33, 20], True), ([300, 90], [257, 200], True),
+                                          ([200, 10], [300, 150], False), ([9000, 700], [1, 1], False), ([7000, 300], [40, 60], True)])
+def test_probabilities_keep_their_bits(dh, ctx, new, tree):
+    """bf16: probabilities meet the values as their upper 16 bits, which leave less than 2^-7 of them, and what is
+    left, rounded by at most 2^-8 of it: off by 2^-15.  The rest as in fp32 (scores, exponentials and sums: the
+    bound of test_gpu_paged.close_to_exact), the output rounded once, 2^-8."""
+    c = attention_case(sum(ctx) + sum(new), ctx, new, 8, 2, dh, 16, BF16, tree)
+    got, lse = atspeed_tree_attention(**c, return_lse=True)
+    out, want_lse, spread, reach = ref.attention(c["q"], c["k_cache"], c["v_cache"], c["block_table"], c["row_off"],
+                                                 c["ctx"], c["mask"])
+    e = (dh + 3) * 2.0 ** -24 * reach + 2.0 ** -21 * reach + 2.0 ** -22 + (c["max_ctx"] + c["max_new"] + 8) * 2.0 ** -24
+    tol = 2.0 ** -8 * out.abs() + (2.0 ** -15 + 3 * e)[..., None] * spread
+    off = (got.cpu().double() - out).abs()
+    assert bool((off <= tol).all()), f"{int((off > tol).sum())} of {off.numel()}, worst {float((off / tol).max()):.2f} of the tolerance"
