@@ -679,8 +679,11 @@ ATSPEED_API atspeed_status atspeed_logit_rules(const atspeed_logit_rules_args* a
  * Used are history, hist_len, max_hist, repetition, frequency, presence, temperature,
  * bias, bias_stride, bias_index, n_bias, allowed with state [max_batch], n_states and
  * mask_value; every other pointer must be null, n_cols L*codebook and token_base the
- * target's item_base (a column is an item code's token).  mask_value must be finite:
- * masked codes rank behind all others and are listed only where those run out.
+ * target's item_base (a column is an item code's token).  Masked codes rank behind all
+ * others, however low the rules leave those, and are listed only where the others among
+ * a step's candidates run out, in the order of their codes: their log-probs
+ * (atspeed_logprobs and scores too) are -1e20 each, those of the others at least -1e18.  mask_value, which must be finite, is
+ * what logits_dev outputs hold for them.
  * ATSPEED_E_INVALID otherwise; ATSPEED_E_STATE from atspeed_align_data and
  * atspeed_align_step while rules are set (their gradient is that of the plain logits).
  * atspeed_accept takes the caller's logits as they are. */

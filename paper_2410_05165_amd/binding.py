@@ -314,7 +314,8 @@ class Engine:
 
         history [max_batch, n], hist_len, repetition, frequency, presence, temperature, bias [n, L*codebook] with
         bias_index, allowed [n, ceil(L*codebook / 32)] with state, as paged.atspeed_logit_rules takes them with
-        max_batch requests; mask_value (default -1e4).  The tensors are held until the next call.
+        max_batch requests; mask_value (default -1e4) is what returned logits hold for masked codes, which rank behind
+        all others whatever it is.  The tensors are held until the next call.
         """
         if not rules:
             self._check(self.lib.atspeed_set_logit_rules(self.ctx, None))

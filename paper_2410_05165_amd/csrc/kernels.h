@@ -51,8 +51,13 @@ hipError_t embed_norm(bool bf16, const void* emb, const Rows& rows, int Mmax, in
 // the sum is written back to x when row_index is null.
 hipError_t rmsnorm(bool bf16, float* x, const float* add, const int* Mdev, int Mmax, int d, const float* g, void* out,
                    const int* row_index, hipStream_t st);
+// What a logit of -infinity that no mask asks for is until its log-softmax, so that
+// -infinity means masked.
+constexpr float kLowestLogit = -3.402823466e+38f;
+// mask_value (host, may be null: no column is masked): columns of -infinity are banned
+// and rank behind every other, the copy of the logits holds *mask_value for them.
 hipError_t log_softmax_rows(const float* logits, const int* Mdev, int Mmax, int n, const int* dst_index,
-                            float* lp, float* logits_copy, hipStream_t st);
+                            float* lp, float* logits_copy, hipStream_t st, const float* mask_value = nullptr);
 
 // Draft alignment (AtSpeed-S / AtSpeed-R training of the draft's item head).
 struct AlignRows {

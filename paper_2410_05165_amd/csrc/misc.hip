@@ -213,11 +213,16 @@ hipError_t embed_norm(bool bf16, const void* emb, const Rows& rows, int Mmax, in
 
 // lp[dst[r]] = z[r] - logsumexp(z[r]) over the n item-token columns (fp32).  A
 // workgroup per row, which is read once and held in registers (n is at most 4 x 256:
-// the item tokens of four levels).
+// the item tokens of four levels).  MASKED: columns of -infinity are banned and get
+// kMaskedLp, the others at least kLeastLp, so that whatever adds up log-probs along a
+// path of up to four codes ranks every path with a banned code behind all others; the
+// copy of the logits holds mask_value for them.
 constexpr int kLsmCols = 4;
+constexpr float kMaskedLp = -1e20f, kLeastLp = -1e18f;
+template <bool MASKED>
 __global__ void __launch_bounds__(256)
 log_softmax_kernel(const float* __restrict__ z, const int* __restrict__ Mdev, int n, const int* __restrict__ dst,
-                   float* __restrict__ lp, float* __restrict__ zcopy) {
+                   float* __restrict__ lp, float* __restrict__ zcopy, float mask_value) {
   __shared__ float red[4];
   const int M = *Mdev;
   for (int r = blockIdx.x; r < M; r += gridDim.x) {
@@ -238,23 +243,38 @@ log_softmax_kernel(const float* __restrict__ z, const int* __restrict__ Mdev, in
     for (int k = 0; k < kLsmCols; ++k)
       if (threadIdx.x + k * 256 < n) s += expf(v[k] - mx);
     s = block_sum256(s, red);
-    const float lse = mx + logf(s);
+    const float lse = mx + logf(s);   // nothing allowed: NaN, of which nothing is used
 #pragma unroll
     for (int k = 0; k < kLsmCols; ++k) {
       const int c = threadIdx.x + k * 256;
       if (c < n) {
-        lp[o + c] = v[k] - lse;
-        if (zcopy) zcopy[o + c] = v[k];
+        float l = v[k] - lse, x = v[k];
+        if constexpr (MASKED) {
+          if (x == -INFINITY) {
+            l = kMaskedLp;
+            x = mask_value;
+          } else {
+            if (l < kLeastLp) l = kLeastLp;
+            if (x == kLowestLogit) x = -INFINITY;
+          }
+        }
+        lp[o + c] = l;
+        if (zcopy) zcopy[o + c] = x;
       }
     }
   }
 }
 
 hipError_t log_softmax_rows(const float* logits, const int* Mdev, int Mmax, int n, const int* dst_index,
-                            float* lp, float* logits_copy, hipStream_t st) {
+                            float* lp, float* logits_copy, hipStream_t st, const float* mask_value) {
   if (n > 256 * kLsmCols) return hipErrorInvalidValue;   // L <= 4 levels of at most 256 codes
   int blocks = std::max(1, std::min(Mmax, 8192));
-  hipLaunchKernelGGL(log_softmax_kernel, dim3(blocks), dim3(256), 0, st, logits, Mdev, n, dst_index, lp, logits_copy);
+  if (mask_value)
+    hipLaunchKernelGGL(log_softmax_kernel<true>, dim3(blocks), dim3(256), 0, st, logits, Mdev, n, dst_index, lp,
+                       logits_copy, *mask_value);
+  else
+    hipLaunchKernelGGL(log_softmax_kernel<false>, dim3(blocks), dim3(256), 0, st, logits, Mdev, n, dst_index, lp,
+                       logits_copy, 0.f);
   return hipGetLastError();
 }
 

@@ -409,7 +409,13 @@ verify_relaxed_kernel(StateDev s, TreeDev tr, TrieDev trie, const float* lpt, co
       for (int i = tid; i < nd; i += blockDim.x) {
         const int ci = cand_of[i];
         float a = -INFINITY;
-        if (ci >= 0) a = (cb.sp[ci] / ra.tau - zp) - (tr.q_score[tb + d0 + i] / ra.tau - zq);
+        if (ci >= 0) {
+          const float lp = cb.sp[ci] / ra.tau - zp;
+          // Banned codes are drafted where the allowed ones run out.  Where the target has
+          // allowed ones they have no probability (log-probs of -1e20), under either model,
+          // and are not accepted on the quotient of the two.
+          if (lp > -1e15f) a = lp - (tr.q_score[tb + d0 + i] / ra.tau - zq);
+        }
         const bool acc = logf(philox_u(ra, u, step, lvl, i, 0, 1)) <= a;
         acc_flag[i] = acc;
         if (acc) atomicAdd(&nacc_s, 1);

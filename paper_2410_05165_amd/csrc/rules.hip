@@ -38,7 +38,7 @@ template <class T> struct LogitVec<T, 1> {
 };
 
 template <class T, int VEC, int ITER>
-__global__ void __launch_bounds__(kRuleThreads) logit_rules_kernel(atspeed_logit_rules_args a, int chunks) {
+__global__ void __launch_bounds__(kRuleThreads) logit_rules_kernel(atspeed_logit_rules_args a, int chunks, float lowest) {
   constexpr int CH = kRuleThreads * VEC * ITER;
   __shared__ int count[CH];
   __shared__ int s_user;
@@ -128,6 +128,7 @@ __global__ void __launch_bounds__(kRuleThreads) logit_rules_kernel(atspeed_logit
       }
       if (bias) y += bv[e];
       y *= temp_inv;
+      if (y < lowest) y = lowest;
       x[k][e] = (word >> e) & 1u ? y : a.mask_value;
     }
     if (VEC == 4 && whole) {
@@ -141,11 +142,12 @@ __global__ void __launch_bounds__(kRuleThreads) logit_rules_kernel(atspeed_logit
 }
 
 template <class T, int VEC, int ITER>
-static atspeed_status launch_rules(const atspeed_logit_rules_args& a, hipStream_t st) {
+static atspeed_status launch_rules(const atspeed_logit_rules_args& a, float lowest, hipStream_t st) {
   const int ch = kRuleThreads * VEC * ITER, chunks = (a.n_cols + ch - 1) / ch;
   const long long n = (long long)chunks * a.n_rows;
   if (n >= (1LL << 31)) return fail(ATSPEED_E_SHAPE, "logit rules: too many rows x columns");
-  hipLaunchKernelGGL((logit_rules_kernel<T, VEC, ITER>), dim3((unsigned)n), dim3(kRuleThreads), 0, st, a, chunks);
+  hipLaunchKernelGGL((logit_rules_kernel<T, VEC, ITER>), dim3((unsigned)n), dim3(kRuleThreads), 0, st, a, chunks,
+                     lowest);
   HIP_TRY(hipGetLastError());
   return ATSPEED_OK;
 }
@@ -156,10 +158,10 @@ static atspeed_status launch_rules(const atspeed_logit_rules_args& a, hipStream_
 // 6.5 and 4.6; 2 rows of 17,051 fp32 8.6 and 5.2; 64 rows of 33,024 7.1 and 7.0; but 120
 // rows 10.2 and 11.3, 400 rows of 16,487 16.3 and 20.1).
 template <class T>
-static atspeed_status run_rules(const atspeed_logit_rules_args& a, bool vec, hipStream_t st) {
+static atspeed_status run_rules(const atspeed_logit_rules_args& a, bool vec, float lowest, hipStream_t st) {
   const bool small = a.n_cols <= 1024 || (long long)a.n_rows * ((a.n_cols + 1023) / 1024) <= 2048;
-  if (vec) return small ? launch_rules<T, 4, 1>(a, st) : launch_rules<T, 4, 4>(a, st);
-  return small ? launch_rules<T, 1, 4>(a, st) : launch_rules<T, 1, 16>(a, st);
+  if (vec) return small ? launch_rules<T, 4, 1>(a, lowest, st) : launch_rules<T, 4, 4>(a, lowest, st);
+  return small ? launch_rules<T, 1, 4>(a, lowest, st) : launch_rules<T, 1, 16>(a, lowest, st);
 }
 
 // What the rules themselves need: the pointers that go together, and their counts.
@@ -173,13 +175,7 @@ atspeed_status check_rules(const atspeed_logit_rules_args& a) {
   return ATSPEED_OK;
 }
 
-}  // namespace atspeed
-
-using namespace atspeed;
-
-extern "C" atspeed_status atspeed_logit_rules(const atspeed_logit_rules_args* args, void* stream) {
-  if (!args) return fail(ATSPEED_E_INVALID, "args is null");
-  const atspeed_logit_rules_args& a = *args;
+atspeed_status logit_rules(const atspeed_logit_rules_args& a, float lowest, hipStream_t st) {
   if (a.dtype != ATSPEED_FP32 && a.dtype != ATSPEED_BF16) return fail(ATSPEED_E_INVALID, "dtype");
   if (a.B < 1 || a.B > kMaxRequests) return fail(ATSPEED_E_INVALID, "B must be 1..1024");
   if (a.n_rows < 0) return fail(ATSPEED_E_INVALID, "n_rows must be >= 0");
@@ -201,6 +197,12 @@ extern "C" atspeed_status atspeed_logit_rules(const atspeed_logit_rules_args* ar
   };
   const bool vec = fits(a.logits, a.logits_stride, 4 * es) && fits(a.out, a.out_stride, 16) &&
                    (!a.bias || fits(a.bias, a.bias_stride, 16));
-  hipStream_t st = (hipStream_t)stream;
-  return a.dtype == ATSPEED_BF16 ? run_rules<bf16_t>(a, vec, st) : run_rules<float>(a, vec, st);
+  return a.dtype == ATSPEED_BF16 ? run_rules<bf16_t>(a, vec, lowest, st) : run_rules<float>(a, vec, lowest, st);
+}
+
+}  // namespace atspeed
+
+extern "C" atspeed_status atspeed_logit_rules(const atspeed_logit_rules_args* args, void* stream) {
+  if (!args) return atspeed::fail(ATSPEED_E_INVALID, "args is null");
+  return atspeed::logit_rules(*args, -INFINITY, (hipStream_t)stream);
 }

@@ -598,14 +598,18 @@ atspeed_status forward(atspeed_ctx& c, ModelRt& r, bool prefill, int Mmax, int T
   MARK_F(ATSPEED_K_LMHEAD, 2.0 * Mmf * c.nitem * d);
   HIP_TRY(gemm(g, st));
   MARK(ATSPEED_K_ROW);
+  const float* mask_value = nullptr;
   if (c.ruled) {
     atspeed_logit_rules_args ra = c.rules;
     ra.B = B; ra.n_rows = Mmf; ra.logits = ra.out = c.logits; ra.logits_stride = ra.out_stride = c.nitem;
     ra.row_off = prefill ? c.one_each : c.rows.user_off;
-    ST_TRY(atspeed_logit_rules(&ra, st));
+    // -infinity marks the masked codes until the log-softmax, and nothing else
+    mask_value = &c.rules.mask_value;
+    ra.mask_value = -INFINITY;
+    ST_TRY(logit_rules(ra, kLowestLogit, st));
   }
-  if (prefill) HIP_TRY(log_softmax_rows(c.logits, c.Mb, B, c.nitem, nullptr, r.root, dbg, st));
-  else HIP_TRY(log_softmax_rows(c.logits, c.rows.M, Mmax, c.nitem, c.rows.slot, r.lp, dbg, st));
+  if (prefill) HIP_TRY(log_softmax_rows(c.logits, c.Mb, B, c.nitem, nullptr, r.root, dbg, st, mask_value));
+  else HIP_TRY(log_softmax_rows(c.logits, c.rows.M, Mmax, c.nitem, c.rows.slot, r.lp, dbg, st, mask_value));
   MARK(-1);
   // the draft's root hidden states, for recomputing its root log-probs when its
   // item head is trained (atspeed_align_step)

@@ -9,6 +9,8 @@ namespace atspeed {
 atspeed_status fail(atspeed_status s, const std::string& msg);
 // The arguments of atspeed_logit_rules that are not a call's logits and rows.
 atspeed_status check_rules(const atspeed_logit_rules_args& a);
+// atspeed_logit_rules where allowed columns come out at `lowest` at least.
+atspeed_status logit_rules(const atspeed_logit_rules_args& a, float lowest, hipStream_t st);
 }  // namespace atspeed
 
 #define HIP_TRY(expr)                                                                      \

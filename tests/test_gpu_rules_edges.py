@@ -1,0 +1,107 @@
+"""Edges of the logit rules: codes that a context's rules mask beside allowed ones that rules leave very low."""
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+from _gpu_common import env  # noqa: E402
+from test_gpu_logit_rules import decode, gpu  # noqa: E402
+from paper_2410_05165_amd.binding import Engine  # noqa: E402
+
+DEV = "cuda:0"
+
+
+def narrow(w, cat, B, ban):
+    """allowed words that ban a share of the codes of levels 2 and on for every user, of level 1 half of the first codes in use."""
+    rng = np.random.default_rng(4)
+    n, cb = w.n_item_tokens, w.codebook
+    ok = np.ones((n + 31) // 32 * 32, bool)
+    used = np.unique(cat[:, 0])
+    ok[rng.permutation(used)[: int(len(used) * ban)]] = False
+    ok[cb:2 * cb] = rng.random(cb) >= ban
+    words = gpu(np.packbits(ok[None], axis=-1, bitorder="little").view(np.int32), np.int32)
+    return dict(allowed=words, state=gpu(np.zeros(B), np.int32)), ok[:n]
+
+
+def low(w, B, how):
+    """Rules that leave allowed codes far below the mask value."""
+    bias = torch.zeros((1, w.n_item_tokens), device=DEV)
+    if how == "temperature":
+        return dict(temperature=torch.full((B,), 2e-4, device=DEV))
+    g = torch.Generator(device=DEV).manual_seed(3)
+    some = torch.rand(bias.shape, generator=g, device=DEV) < 0.7
+    some[:, : w.codebook] = True                       # every first code, and most of the others
+    bias[some] = {"bias": -2e4, "huge bias": -1e25, "no bias": -math.inf}[how]
+    return dict(bias=bias)
+
+
+@pytest.mark.parametrize("how", ["temperature", "bias", "huge bias", "no bias"])
+@pytest.mark.parametrize("mode,N", [(0, 10), (1, 10), (2, 10), (2, 60)])
+def test_masked_codes_rank_behind_every_allowed_one(how, mode, N):
+    """More allowed items than beams: no banned code is listed, however low the rules leave the allowed ones and
+    however many codes are drafted."""
+    e = env("tiny", batch=4, N=N)
+    w, B = e["w"], 4
+    eng = Engine(w, e["tw"], e["dw"], e["cat"], mode=mode)
+    prefix = torch.from_numpy(e["pre"]).to(DEV)
+    ban, ok = narrow(w, e["cat"], B, 0.5)
+    items_left = [row for row in e["cat"] if all(ok[w.codebook * l + c] for l, c in enumerate(row))]
+    assert len(items_left) > 4 * w.K
+    eng.atspeed_set_logit_rules(**ban, **low(w, B, how))
+    for search in (False, True):
+        items, scores, n = decode(eng, w, prefix, search=search)
+        for u in range(B):
+            assert n[u] > 0
+            banned = [r for r in items[u, :n[u]].tolist() if not all(ok[w.codebook * l + c] for l, c in enumerate(r))]
+            assert not banned, (search, u, banned)
+            assert not np.isnan(scores[u, :n[u]]).any()
+    eng.close()
+
+
+def test_masked_codes_are_listed_where_the_allowed_ones_run_out():
+    """Two allowed first codes with few items: they come first, banned ones fill the list; nothing allowed: a whole list."""
+    e = env("tiny", batch=4)
+    w, B = e["w"], 4
+    eng = Engine(w, e["tw"], e["dw"], e["cat"])
+    prefix = torch.from_numpy(e["pre"]).to(DEV)
+    n, cb = w.n_item_tokens, w.codebook
+    count = np.bincount(e["cat"][:, 0], minlength=cb)
+    few = np.argsort(np.where(count > 0, count, 10 ** 9))[:1]
+    assert 0 < count[few].sum() < w.K
+    ok = np.ones((2, (n + 31) // 32 * 32), bool)
+    ok[0, :cb] = False
+    ok[0, few] = True
+    ok[1] = False
+    words = gpu(np.packbits(ok, axis=-1, bitorder="little").view(np.int32), np.int32)
+    eng.atspeed_set_logit_rules(allowed=words, state=gpu([0, 1, 7, -1], np.int32))
+    got, searched = decode(eng, w, prefix), decode(eng, w, prefix, search=True)
+    for a, b in zip(got, searched):
+        np.testing.assert_array_equal(a, b)
+    items, scores, k = got
+    assert k.tolist() == [w.K] * B and not np.isnan(scores).any()
+    mine = {tuple(r) for r in e["cat"][np.isin(e["cat"][:, 0], few)].tolist()}
+    assert {tuple(r) for r in items[0, :len(mine)].tolist()} == mine
+    for u in range(B):
+        assert len({tuple(r) for r in items[u].tolist()}) == w.K
+    eng.close()
+
+
+@pytest.mark.parametrize("value", [-1e4, -7.5])
+def test_returned_logits_hold_the_mask_value(value):
+    e = env("tiny", batch=4)
+    w, B = e["w"], 4
+    eng = Engine(w, e["tw"], e["dw"], e["cat"])
+    prefix = torch.from_numpy(e["pre"]).to(DEV)
+    ban, ok = narrow(w, e["cat"], B, 0.5)
+    plain, ruled = (torch.zeros((B, w.n_item_tokens), device=DEV) for _ in range(2))
+    eng.atspeed_prefill(prefix, plain)
+    eng.atspeed_set_logit_rules(**ban, mask_value=value)
+    eng.atspeed_prefill(prefix, ruled)
+    torch.cuda.synchronize()
+    ok = torch.from_numpy(ok).to(DEV)
+    assert torch.equal(ruled, torch.where(ok, plain, value))
+    eng.close()
