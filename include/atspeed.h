@@ -623,7 +623,8 @@ ATSPEED_API atspeed_status atspeed_tree_attention(const atspeed_tree_attention_a
  *                                          - (frequency[b] * c_v + presence[b]);
  *   x_v = (x_v + bias[bias_index[b]][v]) / temperature[b];
  *   x_v = mask_value where bit v % 32 of allowed[state[r]][v / 32] is 0.
- * in fp32.  Each part is left out where its pointers are null: history (with
+ * in fp32 (the divisions as products with the rounded reciprocals, half a step more of
+ * rounding).  Each part is left out where its pointers are null: history (with
  * hist_len), node_token, repetition, frequency, presence, bias, temperature, allowed.
  *   logits [n_rows, n_cols] in dtype (ATSPEED_FP32 or ATSPEED_BF16), rows logits_stride
  *     elements apart; out fp32, rows out_stride apart.  out may be logits itself (fp32,

@@ -1,4 +1,5 @@
-"""Edges of the logit rules: codes that a context's rules mask beside allowed ones that rules leave very low."""
+"""Edges of the logit rules: numbers whose reciprocal does not fit fp32, and codes that a context's rules mask
+beside allowed ones that rules leave very low."""
 import math
 
 import numpy as np
@@ -10,9 +11,31 @@ torch = pytest.importorskip("torch")
 
 from _gpu_common import env  # noqa: E402
 from test_gpu_logit_rules import decode, gpu  # noqa: E402
+from test_gpu_paged import BF16, F32, check_rules, rules_case  # noqa: E402
 from paper_2410_05165_amd.binding import Engine  # noqa: E402
+from paper_2410_05165_amd.paged import atspeed_logit_rules  # noqa: E402
 
 DEV = "cuda:0"
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("cols", [64, 99, 5000])
+@pytest.mark.parametrize("number,size", [(1e-39, 1e-4), (2.0 ** -126, 1e-4), (3e38, 1e5), (2.0 ** 126, 1e5), (1.0, 1.0)])
+def test_rules_divide_by_any_positive_number(dtype, cols, number, size):
+    """Temperatures and repetitions near the ends of fp32, zeros among the logits: results in range are right."""
+    for part in ("temperature", "repetition"):
+        c = rules_case(cols, 3, [2, 1, 3], cols, dtype)
+        for name in ("repetition", "frequency", "presence", "temperature", "bias", "bias_index", "allowed", "state"):
+            if name != part:
+                c[name] = None
+        c[part] = torch.full((3,), number, device=DEV)
+        c["logits"] = (c["logits"].float() * size).to(dtype)
+        if part == "repetition":
+            # of both signs only where the product with the repetition stays in range, too
+            c["logits"] = c["logits"].abs()
+        c["logits"][:, ::7] = 0.0
+        got = check_rules(c)
+        assert not bool(got.isnan().any())
 
 
 def narrow(w, cat, B, ban):
