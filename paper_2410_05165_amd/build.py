@@ -1,4 +1,7 @@
-"""Builds ``libatspeed.so`` (gfx950, hipcc) and ``_marshal.so`` (its calls on PyTorch tensors, g++) in this directory."""
+"""Builds ``libatspeed.so`` (gfx950, hipcc) and ``_marshal.so`` (its calls on PyTorch tensors, g++) in this directory.
+
+``python -m paper_2410_05165_amd.build library`` builds the first alone.
+"""
 from __future__ import annotations
 
 import os
@@ -29,13 +32,19 @@ def _run(cmd, verbose: bool) -> None:
 
 
 def build(verbose: bool = False) -> str:
+    build_library(verbose)
+    build_marshal(verbose)
+    return LIB
+
+
+def build_library(verbose: bool = False) -> str:
+    """libatspeed.so alone, all that a caller of include/atspeed.h needs: hipcc, no PyTorch."""
     with tempfile.TemporaryDirectory() as tmp, ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
         objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
         list(pool.map(lambda so: _run([HIPCC, *FLAGS, "-c", os.path.join(CSRC, so[0]), "-o", so[1]], verbose),
                       zip(SOURCES, objects)))
         _run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", *objects, "-o", LIB + ".tmp"], verbose)
     os.replace(LIB + ".tmp", LIB)
-    build_marshal(verbose)
     return LIB
 
 
@@ -57,4 +66,4 @@ def build_marshal(verbose: bool = False) -> str:
 
 
 if __name__ == "__main__":
-    print(build(verbose=True))
+    print(build_library(verbose=True) if sys.argv[1:] == ["library"] else build(verbose=True))

@@ -14,7 +14,7 @@ from typing import NamedTuple, Optional
 
 import torch
 
-from .binding import FP32, AtspeedError, LogitRulesArgs
+from .binding import AtspeedError, pack_rules  # noqa: F401
 
 try:
     from . import _marshal
@@ -33,16 +33,6 @@ def _run(fn, at, *args):
         return fn(*args, torch._C._cuda_getCurrentRawStream(device))
     with torch.cuda.device(device):
         return fn(*args, torch._C._cuda_getCurrentRawStream(device))
-
-
-def _want(t, name, dtype, shape, device):
-    """The address of a contiguous tensor of this type and shape on GPU `device` (None: null)."""
-    if t is None:
-        return 0
-    if t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous():
-        return t.data_ptr()
-    raise ValueError(f"{name}: want a contiguous {dtype} {tuple(shape)} on GPU {device}, got {t.dtype} "
-                     f"{tuple(t.shape)} on {t.device}")
 
 
 class StepPlan(NamedTuple):
@@ -89,27 +79,6 @@ def atspeed_tree_attention(q, k_cache, v_cache, block_table, row_off, ctx, max_c
     """
     return _run(_marshal.tree_attention, k_cache, q, k_cache, v_cache, block_table, row_off, ctx, max_ctx, max_new, mask,
                 scale, out, return_lse)
-
-
-def pack_rules(cols: int, token_base: int, B: int, device, history=None, hist_len=None, repetition=None, frequency=None,
-               presence=None, temperature=None, bias=None, bias_index=None, allowed=None, state=None,
-               mask_value: float = -1.0e4):
-    """The arguments of Engine.atspeed_set_logit_rules: rules without logits, rows or trees, state [B]."""
-    dev, f32, i32, vec = device.index or 0, torch.float32, torch.int32, (B,)
-    n_bias = 0 if bias is None else bias.shape[0]
-    if bias is not None and (bias.dtype is not f32 or bias.get_device() != dev or bias.shape != (n_bias, cols) or
-                             (cols > 1 and bias.stride(1) != 1)):
-        raise ValueError(f"bias: want float32 [n, {cols}] on GPU {dev}, rows contiguous")
-    biases = (0, 0) if bias is None else (bias.data_ptr(), bias.stride(0) if n_bias > 1 else cols)
-    hist, states = 0 if history is None else history.shape[-1], 0 if allowed is None else allowed.shape[0]
-    return LogitRulesArgs(FP32, B, 0, cols, token_base, hist, 0, 0, n_bias, states, 0, 1, mask_value, 0, 0, 0, 0, 0, 0,
-                          _want(history, "history", i32, (B, hist), dev), _want(hist_len, "hist_len", i32, vec, dev),
-                          0, 0, _want(repetition, "repetition", f32, vec, dev),
-                          _want(frequency, "frequency", f32, vec, dev), _want(presence, "presence", f32, vec, dev),
-                          _want(temperature, "temperature", f32, vec, dev), *biases,
-                          _want(bias_index, "bias_index", i32, vec, dev),
-                          _want(allowed, "allowed", i32, (states, (cols + 31) // 32), dev),
-                          _want(state, "state", i32, vec, dev))
 
 
 def atspeed_logit_rules(logits, row_off, token_base: int = 0, history=None, hist_len=None, repetition=None,

@@ -1,6 +1,7 @@
 """Edges of the logit rules: numbers whose reciprocal does not fit fp32, and codes that a context's rules mask
 beside allowed ones that rules leave very low."""
 import math
+import sys
 
 import numpy as np
 import pytest
@@ -127,4 +128,19 @@ def test_returned_logits_hold_the_mask_value(value):
     torch.cuda.synchronize()
     ok = torch.from_numpy(ok).to(DEV)
     assert torch.equal(ruled, torch.where(ok, plain, value))
+    eng.close()
+
+
+def test_rules_of_a_context_do_without_the_tensor_calls(monkeypatch):
+    monkeypatch.setitem(sys.modules, "paper_2410_05165_amd.paged", None)
+    e = env("tiny", batch=4)
+    eng = Engine(e["w"], e["tw"], e["dw"], e["cat"])
+    eng.atspeed_set_logit_rules(temperature=torch.full((4,), 0.5, device=DEV))
+    root = torch.zeros((2, 4, e["w"].n_item_tokens), device=DEV)
+    prefix = torch.from_numpy(e["pre"]).to(DEV)
+    eng.atspeed_prefill(prefix, root[0])
+    eng.atspeed_set_logit_rules()
+    eng.atspeed_prefill(prefix, root[1])
+    torch.cuda.synchronize()
+    assert torch.equal(root[0], root[1] * 2)
     eng.close()
