@@ -72,6 +72,14 @@ T* address(const at::Tensor& t) {
   return static_cast<T*>(const_cast<void*>(t.unsafeGetTensorImpl()->data()));
 }
 
+// A call writes to this tensor (None: none): autograd, which sees nothing of it, refuses a
+// backward pass that saved it before.
+void written(PyObject* o) {
+  if (o == Py_None) return;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 // The address of a contiguous tensor of this type and shape on this GPU (None: null).
 template <class T>
 T* want(PyObject* o, const char* name, c10::ScalarType type, std::initializer_list<int64_t> shape, const at::Device& dev) {
@@ -246,6 +254,8 @@ PyObject* page_plan(PyObject*, PyObject* const* o, Py_ssize_t n) {
     a.tree_slot = p + 3 * R;
     void* const st = stream_of(o[9]);
     enqueue([&] { return atspeed_page_plan(&a, st); });
+    written(o[3]);
+    written(o[4]);
     Ref r(PyTuple_New(10));
     const int64_t sizes[9] = {1, B, B, B, B + 1, R, R, R, R};
     int64_t begin = 0;
@@ -283,6 +293,8 @@ PyObject* kv_append(PyObject*, PyObject* const* o, Py_ssize_t n) {
     a.slot = want_i32(o[4], "slot", {rows}, c.dev);
     void* const st = stream_of(o[5]);
     enqueue([&] { return atspeed_kv_append(&a, st); });
+    written(o[2]);
+    written(o[3]);
     Py_RETURN_NONE;
   });
 }
@@ -338,6 +350,7 @@ PyObject* tree_attention(PyObject*, PyObject* const* o, Py_ssize_t n) {
     if (need) ws = fresh({(int64_t)need}, c10::ScalarType::Byte, c.dev);
     void *const st = stream_of(o[12]), *const at = need ? address<void>(ws) : nullptr;
     enqueue([&] { return atspeed_tree_attention(&a, at, need, st); });
+    written(o[10]);
     Ref result(given_or_new(o[10], out));
     if (!with_lse) return result.release();
     Ref sums(THPVariable_Wrap(lse));
@@ -417,6 +430,7 @@ PyObject* logit_rules(PyObject*, PyObject* const* o, Py_ssize_t n) {
     a.state = a.state_by_request ? want_i32(o[12], "state", {B}, dev) : want_i32(o[12], "state", {rows}, dev);
     void* const st = stream_of(o[19]);
     enqueue([&] { return atspeed_logit_rules(&a, st); });
+    written(o[16]);
     return given_or_new(o[16], out);
   });
 }

@@ -5,7 +5,8 @@ and ``PagedKV``, the caches and page tables of one target.
 The functions have the library's names, check their tensors, allocate outputs that are
 not given (_marshal.so, csrc/marshal.cpp) and enqueue on the current stream of the
 tensors' GPU.  Everything computed is computed by the library's kernels; no gradients flow
-through it.
+through it, and what it writes in place counts as changed in place for a backward pass
+that saved it.
 """
 from __future__ import annotations
 

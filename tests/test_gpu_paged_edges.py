@@ -11,7 +11,8 @@ torch = pytest.importorskip("torch")
 
 import _paged_reference as ref  # noqa: E402
 from test_gpu_paged import BF16, DEV, F32, TYPES, attention_case, ints  # noqa: E402
-from paper_2410_05165_amd.paged import atspeed_logit_rules, atspeed_page_plan, atspeed_tree_attention  # noqa: E402
+from paper_2410_05165_amd.paged import (atspeed_kv_append, atspeed_logit_rules, atspeed_page_plan,  # noqa: E402
+                                        atspeed_tree_attention)
 
 
 # ---------------------------------------------------------------- step plan
@@ -160,3 +161,36 @@ def test_probabilities_keep_their_bits(dh, ctx, new, tree):
     tol = 2.0 ** -8 * out.abs() + (2.0 ** -15 + 3 * e)[..., None] * spread
     off = (got.cpu().double() - out).abs()
     assert bool((off <= tol).all()), f"{int((off > tol).sum())} of {off.numel()}, worst {float((off / tol).max()):.2f} of the tolerance"
+
+
+# ---------------------------------------------------------------- what autograd is told
+
+def test_writes_are_seen_by_a_backward_pass_that_saved_the_tensor():
+    """Each buffer that a call writes is saved by a product first: its backward pass refuses the new values."""
+    c = attention_case(3, [20], [4], 4, 2, 64, 16, F32, True)
+    table, free = c["block_table"], ints(np.arange(20))
+    logits, off = torch.randn((4, 50), device=DEV), ints([0, 4])
+    k = torch.randn((4, 2, 64), device=DEV)
+    calls = [("k_cache", c["k_cache"], lambda: atspeed_kv_append(k, k, c["k_cache"], c["v_cache"], ints([0, 1, 2, 3]))),
+             ("v_cache", c["v_cache"], lambda: atspeed_kv_append(k, k, c["k_cache"], c["v_cache"], ints([0, 1, 2, 3]))),
+             ("a layer's caches", c["k_cache"], lambda: atspeed_kv_append(k, k, c["k_cache"][:], c["v_cache"][:], ints([0, 1, 2, 3]))),
+             ("q in place", c["q"], lambda: atspeed_tree_attention(**c, out=c["q"])),
+             ("logits in place", logits, lambda: atspeed_logit_rules(logits, off, out=logits))]
+    for name, t, call in calls:
+        x = torch.ones_like(t, requires_grad=True)
+        loss = (x * t).sum()
+        call()
+        with pytest.raises(RuntimeError, match="inplace operation"):
+            loss.backward()
+    before = [t._version for t in (table, free)]
+    atspeed_page_plan(ints([20]), ints([20]), ints([4]), table, free, ints([9]), 16, 4)
+    assert all(t._version > v for t, v in zip((table, free), before))
+    untouched = torch.randn((4, 50), device=DEV)
+    x = torch.ones_like(untouched, requires_grad=True)
+    loss = (x * untouched).sum()
+    atspeed_logit_rules(untouched, off)
+    loss.backward()                                      # read only
+    with torch.inference_mode():
+        caches = [torch.zeros((3, 16, 2, 64), device=DEV) for _ in range(2)]
+    atspeed_kv_append(k, k, *caches, ints([0, 1, 2, 3]))   # tensors without versions
+    assert torch.equal(caches[0].view(-1, 2, 64)[:4], k)
