@@ -476,7 +476,9 @@ ATSPEED_API atspeed_status atspeed_get_timing(atspeed_ctx* ctx, atspeed_kernel_t
  * They allocate nothing, keep nothing between calls, synchronise nothing, and can
  * be captured into a graph; calls on different streams are independent unless
  * they share a buffer that one of them writes.  Argument errors are found on the
- * host before any launch.  What only the device can see (lengths, pages, parents,
+ * host before any launch, and so are calls of 2^24 workgroups or more
+ * (ATSPEED_E_SHAPE; a workgroup takes a row and 1,024 columns at least of logits, 1 to
+ * 32 rows of an append, 16 to 128 of a request's max_new rows x heads of a group).  What only the device can see (lengths, pages, parents,
  * slots) is checked by the kernels: a bad value costs its own request or row,
  * as stated per call, and never makes a kernel leave its buffers.
  *

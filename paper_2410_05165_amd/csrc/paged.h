@@ -6,6 +6,8 @@
 namespace atspeed {
 
 constexpr int kMaxRequests = 1024;
+// Workgroups of 256 threads of a launch: it holds fewer than 2^32 threads.
+constexpr long long kMaxGroups = (1LL << 24) - 1;
 
 // The device's view of atspeed_pages: element offsets, page size as a shift.
 struct PagesDev {

@@ -309,8 +309,9 @@ atspeed_status atspeed_kv_append(const atspeed_kv_append_args* args, void* strea
   while (p.row_threads < p.chunks && p.row_threads < 256) p.row_threads *= 2;
   p.n_slots = (unsigned)a.page_size * (unsigned)a.n_pool;
   const int per = 256 / p.row_threads;
-  hipLaunchKernelGGL(kv_append_kernel, dim3((unsigned)((a.n_rows + (long long)per - 1) / per)), dim3(256), 0,
-                     (hipStream_t)stream, p);
+  const long long groups = (a.n_rows + (long long)per - 1) / per;
+  if (groups > kMaxGroups) return fail(ATSPEED_E_SHAPE, "append: too many rows x heads");
+  hipLaunchKernelGGL(kv_append_kernel, dim3((unsigned)groups), dim3(256), 0, (hipStream_t)stream, p);
   HIP_TRY(hipGetLastError());
   return ATSPEED_OK;
 }

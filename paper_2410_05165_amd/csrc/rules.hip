@@ -156,7 +156,7 @@ template <class T, int VEC, int ITER>
 static atspeed_status launch_rules(const atspeed_logit_rules_args& a, float lowest, hipStream_t st) {
   const int ch = kRuleThreads * VEC * ITER, chunks = (a.n_cols + ch - 1) / ch;
   const long long n = (long long)chunks * a.n_rows;
-  if (n >= (1LL << 31)) return fail(ATSPEED_E_SHAPE, "logit rules: too many rows x columns");
+  if (n > kMaxGroups) return fail(ATSPEED_E_SHAPE, "logit rules: too many rows x columns");
   hipLaunchKernelGGL((logit_rules_kernel<T, VEC, ITER>), dim3((unsigned)n), dim3(kRuleThreads), 0, st, a, chunks,
                      lowest);
   HIP_TRY(hipGetLastError());

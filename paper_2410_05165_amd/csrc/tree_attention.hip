@@ -980,7 +980,7 @@ template <class T, int DH, class F>
 atspeed_status launch_attention(const TreeAttnArgs& p, F kernel, hipStream_t st) {
   const long long pairs = (long long)p.B * p.KH;
   const long long n = p.units ? (p.units * p.KH + 7) / 8 * 8 : (pairs + 7) / 8 * 8 * p.qtiles;
-  if (n >= (1LL << 31)) return fail(ATSPEED_E_SHAPE, "tree attention: too many query tiles");
+  if (n > kMaxGroups) return fail(ATSPEED_E_SHAPE, "tree attention: too many query tiles");
   hipLaunchKernelGGL(kernel, dim3((unsigned)n), dim3(256), 0, st, p);
   HIP_TRY(hipGetLastError());
   if (p.units) {
