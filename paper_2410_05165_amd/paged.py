@@ -104,7 +104,8 @@ class PagedKV:
 
     One page table serves every layer.  ``plan`` starts a step, ``append`` and ``attention`` run per layer.
     A request is a row of the tables; add rows to an ended request's row to start another in its place
-    (keep 0 gives its pages back first).
+    (keep 0 gives its pages back first).  The tables, ``length`` and ``n_free`` change in place, so a step can be
+    captured into a graph: each replay goes on from the step before, captured or not.
     """
 
     def __init__(self, n_layers: int, n_pages: int, page_size: int, n_kv_heads: int, d_head: int, max_batch: int,
@@ -123,7 +124,7 @@ class PagedKV:
         """Keeps keep[b] of each request's tokens and makes room for add[b] rows (atspeed_page_plan)."""
         p = atspeed_page_plan(self.length, keep, add, self.block_table, self.free_pages, self.n_free, self.page_size,
                               max_rows, parent)
-        self.length, self.n_free = p.length, p.n_free
+        torch._foreach_copy_([self.length, self.n_free], [p.length, p.n_free])     # in place: a captured step goes on from here
         return p
 
     def append(self, layer: int, plan: StepPlan, k, v):

@@ -11,8 +11,8 @@ torch = pytest.importorskip("torch")
 
 import _paged_reference as ref  # noqa: E402
 from test_gpu_paged import BF16, DEV, F32, TYPES, attention_case, ints  # noqa: E402
-from paper_2410_05165_amd.paged import (atspeed_kv_append, atspeed_logit_rules, atspeed_page_plan,  # noqa: E402
-                                        atspeed_tree_attention)
+from paper_2410_05165_amd.paged import (PagedKV, atspeed_kv_append, atspeed_logit_rules,  # noqa: E402
+                                        atspeed_page_plan, atspeed_tree_attention)
 
 
 # ---------------------------------------------------------------- step plan
@@ -194,3 +194,54 @@ def test_writes_are_seen_by_a_backward_pass_that_saved_the_tensor():
         caches = [torch.zeros((3, 16, 2, 64), device=DEV) for _ in range(2)]
     atspeed_kv_append(k, k, *caches, ints([0, 1, 2, 3]))   # tensors without versions
     assert torch.equal(caches[0].view(-1, 2, 64)[:4], k)
+
+
+# ---------------------------------------------------------------- caches in captured steps
+
+def test_captured_steps_of_a_cache_go_on_from_each_other():
+    """PagedKV.plan, append and attention in a graph: replays and eager steps in turn equal eager steps alone."""
+    rng = np.random.default_rng(5)
+    g = torch.Generator(device=DEV).manual_seed(5)
+    B, width, heads, kv, dh, page, pool = 5, 12, 4, 2, 64, 8, 60
+    caches = [PagedKV(1, pool, page, kv, dh, B, 96, dtype=F32) for _ in range(2)]
+
+    def inputs():
+        r = lambda n: torch.randn((B * width, n, dh), generator=g, device=DEV)  # noqa: E731
+        return dict(drop=ints(rng.integers(0, 5, B)), add=ints(rng.integers(0, width + 1, B)), q=r(heads), k=r(kv), v=r(kv))
+
+    def step(cache, x):
+        keep = torch.where(cache.length > 60, 0, (cache.length - x["drop"]).clamp(min=0)).int()
+        p = cache.plan(keep, x["add"], B * width)
+        cache.append(0, p, x["k"], x["v"])
+        return p, cache.attention(0, p, x["q"], width, out=torch.zeros_like(x["q"]))
+
+    hold = inputs()
+    side = torch.cuda.Stream(device=DEV)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(PagedKV(1, pool, page, kv, dh, B, 96, dtype=F32), hold)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(caches[0], hold)
+    for i in range(12):
+        x = inputs()
+        want = step(caches[1], x)
+        if i % 4 == 3:
+            now = step(caches[0], x)                     # an eager step between the replays
+        else:
+            for k in hold:
+                hold[k].copy_(x[k])
+            graph.replay()
+            now = got
+        torch.cuda.synchronize()
+        for a, b in zip(now[0][:-1], want[0][:-1]):
+            assert torch.equal(a, b), i
+        n = int(want[0].row_off[-1])
+        assert torch.equal(now[1][:n], want[1][:n]), i
+        for name in ("length", "n_free", "block_table", "k", "v"):
+            assert torch.equal(getattr(caches[0], name), getattr(caches[1], name)), (i, name)
+    held, t, free = (getattr(caches[0], n).cpu().numpy() for n in ("length", "block_table", "free_pages"))
+    mine = [x for b in range(B) for x in t[b, :-(-held[b] // page)]]
+    assert sorted(mine + list(free[:int(caches[0].n_free)])) == list(range(pool))
