@@ -226,6 +226,7 @@ class Engine:
         cfg.stream = self.stream.cuda_stream
         self.cfg = cfg
         self._keep = []
+        self._rules = {}
         self.tw = self._upload(target_w, w.target.n_layers)
         self.target_dev = self._keep[-2]
         self.dw = self._upload(draft_w, w.draft.n_layers) if draft_w is not None else None
@@ -349,12 +350,14 @@ class Engine:
         max_batch requests; mask_value (default -1e4) is what returned logits hold for masked codes, which rank behind
         all others whatever it is.  The tensors are held until the next call.
         """
-        if not rules:
-            self._check(self.lib.atspeed_set_logit_rules(self.ctx, None))
-            self._rules = None
-            return
-        args = pack_rules(self.n_item, self.w.target.item_base, self.cfg.max_batch, self.device, **rules)
-        self._check(self.lib.atspeed_set_logit_rules(self.ctx, C.byref(args)))
+        args = None
+        if rules:
+            args = C.byref(pack_rules(self.n_item, self.w.target.item_base, self.cfg.max_batch, self.device, **rules))
+        self._check(self.lib.atspeed_set_logit_rules(self.ctx, args))
+        # forwards that are under way on the engine's stream still read the rules before
+        for t in self._rules.values():
+            if isinstance(t, self.torch.Tensor):
+                t.record_stream(self.stream)
         self._rules = rules
 
     def atspeed_get_state(self, B: int):

@@ -144,3 +144,31 @@ def test_rules_of_a_context_do_without_the_tensor_calls(monkeypatch):
     torch.cuda.synchronize()
     assert torch.equal(root[0], root[1] * 2)
     eng.close()
+
+
+def test_rules_that_are_replaced_are_held_until_the_forwards_have_read_them():
+    """An engine on a stream of its own, behind other work there: its prefill reads the rules of its call."""
+    e = env("tiny", batch=4)
+    w = e["w"]
+    side = torch.cuda.Stream(device=DEV)
+    eng = Engine(w, e["tw"], e["dw"], e["cat"], stream=side)
+    prefix = torch.from_numpy(e["pre"]).to(DEV)
+    got, want = (torch.zeros((4, w.n_item_tokens), device=DEV) for _ in range(2))
+    g = torch.Generator(device=DEV).manual_seed(1)
+    bias = torch.randn((1, w.n_item_tokens), generator=g, device=DEV)
+    torch.cuda.synchronize()
+    eng.atspeed_set_logit_rules(bias=bias)
+    eng.atspeed_prefill(prefix, want)
+    torch.cuda.synchronize()
+    mine = bias.clone()
+    torch.cuda.synchronize()
+    eng.atspeed_set_logit_rules(bias=mine)
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)                    # about 10 ms
+    eng.atspeed_prefill(prefix, got)
+    eng.atspeed_set_logit_rules()
+    del mine
+    others = [torch.full((1, w.n_item_tokens), 1e6, device=DEV) for _ in range(8)]
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and len(others) == 8
+    eng.close()

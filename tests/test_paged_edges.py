@@ -30,7 +30,7 @@ class Lib:
     atspeed_set_logit_rules = staticmethod(lambda ctx, rules: 0)
 
 eng = object.__new__(binding.Engine)
-eng.lib, eng.ctx, eng.device, eng.stream = Lib, None, torch.device("cuda:0"), None
+eng.lib, eng.ctx, eng.device, eng.torch, eng._rules = Lib, None, torch.device("cuda:0"), torch, {}
 eng.w = type("W", (), dict(L=4, codebook=8, target=type("T", (), dict(item_base=5))))
 eng.cfg = type("C", (), dict(max_batch=2))
 eng.atspeed_set_logit_rules(mask_value=-3.0)
