@@ -356,7 +356,7 @@ class Engine:
         self._check(self.lib.atspeed_set_logit_rules(self.ctx, args))
         # forwards that are under way on the engine's stream still read the rules before
         for t in self._rules.values():
-            if isinstance(t, self.torch.Tensor):
+            if isinstance(t, self.torch.Tensor) and isinstance(self.stream, self.torch.cuda.Stream):
                 t.record_stream(self.stream)
         self._rules = rules
 

@@ -124,7 +124,8 @@ class PagedKV:
         """Keeps keep[b] of each request's tokens and makes room for add[b] rows (atspeed_page_plan)."""
         p = atspeed_page_plan(self.length, keep, add, self.block_table, self.free_pages, self.n_free, self.page_size,
                               max_rows, parent)
-        torch._foreach_copy_([self.length, self.n_free], [p.length, p.n_free])     # in place: a captured step goes on from here
+        with torch.inference_mode():                     # caches made under it are written outside it, too
+            torch._foreach_copy_([self.length, self.n_free], [p.length, p.n_free])   # in place, for captured steps
         return p
 
     def append(self, layer: int, plan: StepPlan, k, v):

@@ -245,3 +245,17 @@ def test_captured_steps_of_a_cache_go_on_from_each_other():
     held, t, free = (getattr(caches[0], n).cpu().numpy() for n in ("length", "block_table", "free_pages"))
     mine = [x for b in range(B) for x in t[b, :-(-held[b] // page)]]
     assert sorted(mine + list(free[:int(caches[0].n_free)])) == list(range(pool))
+
+
+@pytest.mark.parametrize("made,used", [(True, False), (False, True), (True, True)])
+def test_caches_in_and_out_of_inference_mode(made, used):
+    with torch.inference_mode(made):
+        cache = PagedKV(1, 20, 8, 2, 64, 2, 40, dtype=F32)
+    k = torch.ones((7, 2, 64), device=DEV)
+    with torch.inference_mode(used):
+        for held in (0, 4, 9):
+            p = cache.plan(ints([held, 0]), ints([5, 2]), 7)
+            cache.append(0, p, k, k)
+            out = cache.attention(0, p, torch.ones((7, 4, 64), device=DEV), 5)
+            assert cache.length.tolist() == [held + 5, 2] and torch.equal(cache.length, p.length)
+            assert bool((out == 1).all())
