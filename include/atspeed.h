@@ -590,7 +590,8 @@ ATSPEED_API atspeed_status atspeed_kv_append(const atspeed_kv_append_args* args,
  *     ctx[b] means a request that sees nothing.  Keys past max_pages * page_size
  *     or 2^30, and keys in pages outside 0 .. n_pool - 1, are not seen.
  *   max_ctx, max_new: what ctx[b] and a request's row count stay within; they size
- *     the launch (a context above max_ctx is still read whole).
+ *     the launch (a context above max_ctx is still read whole) and choose its kernels,
+ *     so tight ones are faster.
  * Long contexts are cut into pieces by the lengths of all the call's requests, and the
  * pieces joined in order: the same call gives the same bits, a request among others of
  * other lengths need not.

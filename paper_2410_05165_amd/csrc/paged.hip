@@ -19,7 +19,7 @@ namespace atspeed {
 //   - of the free stack S (free_pages, then the released pages) the takers read
 //     entries from the new top on, and the entries written lie below it.
 // Bound by latency: three dependent loads (lengths, table or free list, parents).  5.0 us
-// for one user's 30 nodes, 11.0 for 1,024 users with trees of up to 110.
+// for one user's 30 nodes, 11.4 for 1,024 users with trees of up to 110 (9.6 for chains).
 constexpr int kPlanThreads = 256;
 constexpr int kPlanItems = kMaxRequests / kPlanThreads;
 
@@ -215,9 +215,9 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(PlanArgs p) {
 // ---------------------------------------------------------------- append
 // One 16-byte chunk of k and one of v per thread and step; consecutive threads take
 // consecutive chunks of a row, rows of few chunks share a workgroup.  Bound by memory:
-// chunks of up to 1,024 rows x 32 users, 8 heads of 128 (99 MB), 16.2 us, above the
+// chunks of up to 1,024 rows x 32 users, 8 heads of 128 (99 MB), 16.0 us, above the
 // 4.95 TB/s of a 2 GiB copy, since part of it stays in the last cache; 60 rows x 32 users,
-// 32 heads (27 MB), 4.9.
+// 32 heads (27 MB), 5.2.
 struct AppendArgs {
   const char* k;
   const char* v;

@@ -12,8 +12,8 @@ namespace atspeed {
 // and the row's path; then every logit is read once and written once.  The logits and
 // the row's state are requested before the request is searched, so a short row costs
 // the chain lengths -> tokens -> output and a long one streams.  61 rows x 32 users of
-// 1,024 fp32 columns: 4.8 us; 128 rows of 33,024 bf16 columns with 2,048 tokens of
-// history (26 MB): 9.5, 2.7 TB/s.
+// 1,024 fp32 columns: 5.1 us; 128 rows of 33,024 bf16 columns with 2,048 tokens of
+// history (26 MB): 11.3, 2.3 TB/s, and 9.2 with one token.
 constexpr int kRuleThreads = 256;
 
 template <class T, int VEC> struct LogitVec;

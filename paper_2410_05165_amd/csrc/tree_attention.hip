@@ -6,10 +6,13 @@
 // small trees), bound by the reads of the cache, and more, bound by the matrix and
 // vector instructions and the latencies between them; long contexts are cut into pieces
 // and their parts joined.  Measured (us; share of a 4.95 TB/s copy or of a 1,214 TFLOP/s
-// product): 64 single tokens over up to 8,192 keys, 8 of 32 heads, 145 (99% of the copy);
-// 60 nodes x 32 users over 144 keys, 32 heads, 33.5 (84%); trees of 4 users over up to
-// 65,536 keys 134 (89%); 300 nodes x 128 users over 1,024 keys 1,230 (0.52 PFLOP/s of
-// what the rows see); causal chunks of up to 1,024 x 16 users 108 (0.64 PFLOP/s).
+// product): 64 single tokens over up to 8,192 keys, 8 of 32 heads, 143 (99% of the copy);
+// 60 nodes x 32 users over 144 keys, 32 heads, 33.7 (83%); trees of 4 users over up to
+// 65,536 keys 144 (82%); 300 nodes x 128 users over 1,024 keys 1,431 (0.45 PFLOP/s of
+// what the rows see); causal chunks of up to 1,024 x 16 users 127 (0.54 PFLOP/s).  The
+// comparisons of tiles, pieces and loops below were measured with probabilities as one
+// bf16 number (see Tile), which takes 4 to 20% less where many rows are bound by the
+// matrix work.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
