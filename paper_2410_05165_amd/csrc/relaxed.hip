@@ -410,11 +410,12 @@ verify_relaxed_kernel(StateDev s, TreeDev tr, TrieDev trie, const float* lpt, co
         const int ci = cand_of[i];
         float a = -INFINITY;
         if (ci >= 0) {
-          const float lp = cb.sp[ci] / ra.tau - zp;
-          // Banned codes are drafted where the allowed ones run out.  Where the target has
-          // allowed ones they have no probability (log-probs of -1e20), under either model,
-          // and are not accepted on the quotient of the two.
-          if (lp > -1e15f) a = lp - (tr.q_score[tb + d0 + i] / ra.tau - zq);
+          const float lp = cb.sp[ci] / ra.tau - zp, lq = tr.q_score[tb + d0 + i] / ra.tau - zq;
+          // Banned codes are drafted where the allowed ones run out.  Where a model has
+          // allowed ones, they have no probability under it (log-probs of -1e20) and are
+          // not accepted on a quotient with that 0; what a target that is not ruled gives
+          // them they have in the residual.
+          if (lp > -1e15f && lq > -1e15f) a = lp - lq;
         }
         const bool acc = logf(philox_u(ra, u, step, lvl, i, 0, 1)) <= a;
         acc_flag[i] = acc;

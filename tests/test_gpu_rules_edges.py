@@ -86,6 +86,48 @@ def test_masked_codes_rank_behind_every_allowed_one(how, mode, N):
     eng.close()
 
 
+@pytest.mark.parametrize("N", [10, 60])
+def test_drafts_of_banned_codes_are_not_accepted_by_ones_own_logits(N):
+    """Relaxed acceptance of the caller's logits, which hold the mask value, with more codes drafted than allowed."""
+    e = env("tiny", batch=4, N=N)
+    w, B = e["w"], 4
+    eng = Engine(w, e["tw"], e["dw"], e["cat"], mode=2)
+    ban, ok = narrow(w, e["cat"], B, 0.9)
+    eng.atspeed_set_logit_rules(**ban)
+    root = torch.zeros((B, w.n_item_tokens), device=DEV)
+    eng.atspeed_prefill(torch.from_numpy(e["pre"]).to(DEV), root)
+    eng.atspeed_draft()
+    logits = torch.zeros((B, eng.max_nodes, w.n_item_tokens), device=DEV)
+    eng.atspeed_tree_logits(logits)
+    torch.cuda.synchronize()
+    assert int((root == -1e4).sum()) > 0
+    eng.atspeed_accept(logits, root)
+    t, k, paths = eng.atspeed_get_state(B)[:3]
+    for u in range(B):
+        assert int(t[u]) >= 1 and int(k[u]) >= 1
+        # first codes: 15 or more are allowed
+        banned = [p for p in paths[u, :int(k[u]), :1].tolist() if not ok[p[0]]]
+        assert not banned, (u, banned)
+    eng.close()
+
+
+@pytest.mark.parametrize("lam", [0.0, 0.4, 1.0])
+def test_a_mixed_search_keeps_to_the_rules(lam):
+    e = env("tiny", batch=4)
+    w, B = e["w"], 4
+    eng = Engine(w, e["tw"], e["dw"], e["cat"])
+    ban, ok = narrow(w, e["cat"], B, 0.5)
+    eng.atspeed_set_logit_rules(**ban, **low(w, B, "bias"))
+    items = torch.zeros((B, w.K, w.L), dtype=torch.int32, device=DEV)
+    scores, n = torch.zeros((B, w.K), device=DEV), torch.zeros(B, dtype=torch.int32, device=DEV)
+    eng.atspeed_mixed_search(lam, torch.from_numpy(e["pre"]).to(DEV), items, scores, n)
+    torch.cuda.synchronize()
+    assert n.tolist() == [w.K] * B and not bool(scores.isnan().any())
+    for u in range(B):
+        assert all(ok[w.codebook * l + c] for r in items[u].tolist() for l, c in enumerate(r)), u
+    eng.close()
+
+
 def test_masked_codes_are_listed_where_the_allowed_ones_run_out():
     """Two allowed first codes with few items: they come first, banned ones fill the list; nothing allowed: a whole list."""
     e = env("tiny", batch=4)
