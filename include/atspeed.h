@@ -672,6 +672,203 @@ typedef struct {
 } atspeed_logit_rules_args;
 ATSPEED_API atspeed_status atspeed_logit_rules(const atspeed_logit_rules_args* args, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Beam search and draft training around a caller's own target: what chooses the next
+ * beams from the logits, what carries their caches over, and the loss that trains a
+ * draft towards that target.  The conventions of the calls above hold: no context,
+ * device pointers of one GPU, work enqueued on `stream`, no allocation, nothing kept
+ * between calls, no synchronisation, capturable; a bad value on the device costs its own
+ * request or row and never makes a kernel leave its buffers.
+ *   atspeed_beam_select    the k best continuations of a request's beams,
+ *   atspeed_page_fork      page tables of the chosen beams, pages shared (once a step),
+ *   atspeed_page_copy      the beams' last pages, in every layer,
+ *   atspeed_kv_compact     the accepted path of a verified tree moved together,
+ *   atspeed_distill_loss,  distillation of a draft from the target's top logits,
+ *   atspeed_distill_grad   and its gradient. */
+
+/* The k best continuations of each request's beams (Eq. 1: a sequence's log-probability
+ * is its beam's plus the token's).  Row r of the logits is a beam with cumulative
+ * log-probability score[r]; column v is token token_base + v; request b's beams are rows
+ * row_off[b] .. row_off[b + 1] - 1.  Candidate (r, v) has the score
+ *   score[r] + logit[r][v] - log sum_u exp(logit[r][u]),
+ * or score[r] + logit[r][v] with log_probs (the logits are log-probabilities already).
+ * Scores are computed and compared in 64 bits and rounded to fp32 at the end; equal ones
+ * rank by the lower row, then the lower column (logits of one row that differ, but not in
+ * 64 bits of the score, may rank either way).
+ * A column of -infinity is no candidate.  A row that holds NaN or +infinity, or whose
+ * score is not finite, has none.  A row with done[r] != 0 has ended: its only candidate
+ * is itself, with score[r] and token -1; its logits are not read.
+ *   logits [n_rows, n_cols] in dtype (ATSPEED_FP32 or ATSPEED_BF16), rows logits_stride
+ *     elements apart, at any element; rows past min(row_off[B], n_rows) are not used.
+ *   score, done [n_rows] (nullable: 0, none).
+ *   row_id (nullable) [n_rows]: what parent names row r by, r itself otherwise --
+ *     atspeed_page_plan's row_user gives the rows of its tables, as atspeed_page_fork's src.
+ *   count [B]; parent, token, score_out [B, k], the best first; from count[b] on -1, -1
+ *     and -infinity.
+ *   paths [n_paths, max_path], path_len [n_paths] (nullable): the tokens of each beam so
+ *     far, by the number that parent gives; paths_out [B, k, max_path] and path_len_out
+ *     [B, k] get the parent's path (path_len held to 0 .. max_path) with the token behind
+ *     it where it is one and there is room; places past the path are -1, and a parent
+ *     outside 0 .. n_paths - 1 has an empty path.  No output may overlap an input.
+ * B 1..1024, k 1..256, n_cols 1..2^20, max_path 1..2^16.  workspace as for
+ * atspeed_tree_attention. */
+typedef struct {
+  int32_t dtype, B, n_rows, n_cols, k, token_base, log_probs, n_paths, max_path;
+  const void* logits;
+  int64_t logits_stride;
+  const int32_t* row_off;
+  const float* score;
+  const int32_t* done;
+  const int32_t* row_id;
+  const int32_t* paths;
+  const int32_t* path_len;
+  int32_t* count;
+  int32_t* parent;
+  int32_t* token;
+  float* score_out;
+  int32_t* paths_out;
+  int32_t* path_len_out;
+} atspeed_beam_select_args;
+ATSPEED_API atspeed_status atspeed_beam_select_workspace_bytes(const atspeed_beam_select_args* args, size_t* bytes);
+ATSPEED_API atspeed_status atspeed_beam_select(const atspeed_beam_select_args* args, void* workspace, size_t ws_bytes,
+                                               void* stream);
+
+/* Page tables of forked requests: row j of the tables goes on with the first keep[j]
+ * tokens of row src[j] (src[j] = -1: with none).  Full pages are shared; the page that
+ * holds token keep[j], where keep[j] is no multiple of page_size, is the row's own: the
+ * lowest row that wants it takes the page itself if no row holds it as a full one and no
+ * one else holds it, every other row gets a page from the free list and is to copy the
+ * page's first keep[j] % page_size tokens (atspeed_page_copy, in every layer's caches
+ * before anything is appended).  A page that nobody holds any more goes back to the free
+ * list, in ascending order, before the wanted ones are popped in the rows' order.
+ * shared [n_pool] counts a page's further holders: 0 for a page of one holder or none.  It
+ * starts as zeros and is updated in place; a caller that keeps a page for itself adds 1.
+ * atspeed_page_plan takes fresh pages, which have one holder, but knows nothing of shared
+ * ones: rows whose pages may be shared drop tokens by this call (src null, keep), then
+ * atspeed_page_plan adds rows with held = keep = length.
+ *   held [B]      tokens whose pages each row holds (out of 0 .. max_pages * page_size: 0)
+ *   keep [B]      (nullable: all that src[j] holds)
+ *   src [B]       (nullable: src[j] = j)
+ *   length [B]    keep[j], or what a refused row is left with
+ *   refused [B]   0: done; 1: no page was left to copy to -- the row keeps its full pages,
+ *                 length is keep[j] - keep[j] % page_size; 2: src[j] is not in -1 .. B - 1 or
+ *                 keep[j] not in 0 .. held[src[j]]: the row goes on as src[j] = j, all of it (where
+ *                 no page is left for that, its full pages; length says so)
+ *   copy_src, copy_dst, copy_len [B]: the pages to copy; -1, -1 and 0 where there are none
+ * block_table [B, max_pages], free_pages [n_pool], n_free [1] and shared are updated in
+ * place; table entries from ceil(length / page_size) on and free_pages from n_free on are
+ * undefined.  Table entries outside 0 .. n_pool - 1 are handed on and otherwise ignored.  No
+ * output may overlap an input.  B, page_size, n_pool and B * max_pages as for
+ * atspeed_page_plan.  workspace as for atspeed_tree_attention. */
+typedef struct {
+  int32_t B, page_size, max_pages, n_pool;
+  const int32_t* held;
+  const int32_t* keep;
+  const int32_t* src;
+  int32_t* block_table;
+  int32_t* free_pages;
+  int32_t* n_free;
+  int32_t* shared;
+  int32_t* length;
+  int32_t* refused;
+  int32_t* copy_src;
+  int32_t* copy_dst;
+  int32_t* copy_len;
+} atspeed_page_fork_args;
+ATSPEED_API atspeed_status atspeed_page_fork_workspace_bytes(const atspeed_page_fork_args* args, size_t* bytes);
+ATSPEED_API atspeed_status atspeed_page_fork(const atspeed_page_fork_args* args, void* workspace, size_t ws_bytes,
+                                             void* stream);
+
+/* Copies the first length[i] tokens (held to page_size) of page src[i] to page dst[i], for
+ * i < n, in n_layers layers of the caches, layers k_layer_stride (v_layer_stride) elements
+ * apart.  Copies whose src or dst is outside 0 .. n_pool - 1 are left out.  A page that one
+ * copy writes may be no other copy's src or dst.  Types, heads, strides and paging as for
+ * atspeed_kv_append; n_layers 1..1024. */
+typedef struct {
+  int32_t dtype, n, n_layers, n_kv_heads, d_head, page_size, n_pool;
+  atspeed_pages k_pages, v_pages;
+  int64_t k_layer_stride, v_layer_stride;
+  const int32_t* src;
+  const int32_t* dst;
+  const int32_t* length;
+} atspeed_page_copy_args;
+ATSPEED_API atspeed_status atspeed_page_copy(const atspeed_page_copy_args* args, void* stream);
+
+/* Moves the accepted path of each request's new rows together: the keys and values at cache
+ * position ctx[b] + path[b][i] go to position ctx[b] + i, for i < n_path[b], in n_layers
+ * layers; path[b] are the request's row numbers in ascending order (a path down a
+ * level-ordered tree).  ctx[b] + n_path[b] is then what the next step keeps.  A request with
+ * a negative ctx, an n_path outside 0 .. max_path, a path that is not strictly ascending from
+ * 0 up, or a position whose table entry is missing or outside 0 .. n_pool - 1 is left as it
+ * was.  No two requests may hold a page that one of them writes.  Types, heads, strides and
+ * paging as for atspeed_kv_append; B 1..1024, max_path 1..4096, n_layers 1..1024. */
+typedef struct {
+  int32_t dtype, B, n_layers, n_kv_heads, d_head, page_size, max_pages, n_pool, max_path;
+  atspeed_pages k_pages, v_pages;
+  int64_t k_layer_stride, v_layer_stride;
+  const int32_t* block_table;
+  const int32_t* ctx;
+  const int32_t* path;
+  const int32_t* n_path;
+} atspeed_kv_compact_args;
+ATSPEED_API atspeed_status atspeed_kv_compact(const atspeed_kv_compact_args* args, void* stream);
+
+/* Distillation of a draft from a teacher's top logits, per row: the divergence between the
+ * teacher's distribution p and the draft's q over buckets -- each top column a bucket, all
+ * other columns one more --
+ *   p = softmax of [teacher_logit[r][j] / temperature, tail[r]],
+ *   q = softmax of the draft's logits[r] / temperature over all n_cols columns, summed
+ *       within each bucket;
+ *   loss[r] = weight[r] temperature^2 sum_b p_b log(p_b / q_b)          (forward)
+ *   loss[r] = weight[r] temperature^2 sum_b q_b log(q_b / p_b)          (reverse)
+ * where tail[r] is the log of the sum of exp(logit / temperature) over the teacher's other
+ * columns (nullable with the forward form: the teacher has no others, p is renormalised
+ * over the tops).  With d = weight temperature, q_v the probability of column v and b(v) its
+ * bucket, the gradient with respect to logits[r][v] is
+ *   forward: d (q_v - p_v) at a top, d q_v (1 - p_rest / q_rest) elsewhere,
+ *   reverse: d q_v (log(q_b(v) / p_b(v)) - sum_b q_b log(q_b / p_b)).
+ * Terms with probability 0 in front of the logarithm are 0; a term whose divisor alone is
+ * 0 is infinite.  A column that teacher_index names more than once is one bucket with the
+ * sum of their probabilities.  Entries whose index is outside 0 .. n_cols - 1 or whose
+ * logit is -infinity are no tops.  A row without tops, or of weight 0, has loss 0 and
+ * gradient 0, whatever its logits hold; columns of logit -infinity have q_v = 0, and where
+ * all are, q is 0.  The share of columns more than 2^126 below the largest counts as 0.
+ * Sums and statistics are fp32, what is summed over the tops 64 bits.
+ *   logits [n_rows, n_cols], rows logits_stride elements apart, at any element;
+ *   teacher_logit [n_rows, n_tops], both in dtype; teacher_index [n_rows, n_tops];
+ *   tail, weight [n_rows] fp32 (weight nullable: 1); temperature positive.
+ *   loss [n_rows] fp32; saved [n_rows, 2 + n_tops] fp32: what atspeed_distill_grad reads.
+ * n_rows from 0, n_cols 1..2^20, n_tops 1..256.  No output may overlap an input. */
+typedef struct {
+  int32_t dtype, n_rows, n_cols, n_tops, reverse;
+  float temperature;
+  const void* logits;
+  int64_t logits_stride;
+  const void* teacher_logit;
+  const int32_t* teacher_index;
+  const float* tail;
+  const float* weight;
+  float* loss;
+  float* saved;
+} atspeed_distill_loss_args;
+ATSPEED_API atspeed_status atspeed_distill_loss(const atspeed_distill_loss_args* args, void* stream);
+
+/* grad[r] = grad_loss[r] (nullable: 1) times the gradient of loss[r] with respect to
+ * logits[r], in dtype, rows grad_stride elements apart, at any element; every column is
+ * written.  logits, teacher_index, temperature and saved are those of the loss. */
+typedef struct {
+  int32_t dtype, n_rows, n_cols, n_tops;
+  float temperature;
+  const void* logits;
+  int64_t logits_stride;
+  const int32_t* teacher_index;
+  const float* saved;
+  const float* grad_loss;
+  void* grad;
+  int64_t grad_stride;
+} atspeed_distill_grad_args;
+ATSPEED_API atspeed_status atspeed_distill_grad(const atspeed_distill_grad_args* args, void* stream);
+
 /* Rules on the item logits of a context's own forwards: from the next forward on the
  * target's and the draft's logits pass atspeed_logit_rules before their log-softmax, so
  * prefill, draft, verify, tree_logits, decode_topk and the searches rank, accept and

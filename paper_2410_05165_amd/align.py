@@ -5,13 +5,30 @@ This module holds the buffers the two calls take (the batch, the fp32 master
 copy of the head and the AdamW moments) and the learning-rate schedule (the
 paper's implementation details: AdamW, lr 1e-3, cosine decay after a linear
 warmup).  Every loss, gradient and update runs in the library's kernels.
+
+A draft of the caller's own, trained by PyTorch, is aligned by distillation from
+the target's top logits: ``distill`` is the loss with its gradient for autograd,
+``atspeed_distill_loss`` and ``atspeed_distill_grad`` are the two calls under it.
 """
 from __future__ import annotations
 
 import math
 from typing import Optional
 
+import torch
+
 from .binding import AlignArgs, Engine
+
+try:
+    from .paged import _marshal, _run
+except ImportError as e:                                 # AlignTrainer needs libatspeed.so alone
+    _missing = str(e)
+
+    class _marshal:
+        distill_loss = distill_grad = None
+
+    def _run(*args):
+        raise ImportError(_missing)
 
 MODES = {"S": 0, "R": 1}
 
@@ -26,6 +43,51 @@ def cosine_lr(step: int, total: int, peak: float, warmup: int) -> float:
     return 0.5 * peak * (1.0 + math.cos(math.pi * x))
 
 
+def atspeed_distill_loss(logits, teacher_logit, teacher_index, tail=None, weight=None, temperature: float = 1.0,
+                         reverse: bool = False):
+    """The divergence of a draft's logits [rows, cols] (fp32 or bf16) from a teacher's top logits, a number a row.
+
+    teacher_logit [rows, tops] of the logits' type at the columns teacher_index [rows, tops] (int32; outside the columns:
+    no top); tail [rows] fp32: the log of the sum of exp(logit / temperature) over the teacher's other columns (None: it
+    has none); weight [rows] fp32.  reverse: sum q log(q / p), which needs the tail, for sum p log(p / q).  Returns
+    (loss [rows], saved), saved for atspeed_distill_grad.
+    """
+    return _run(_marshal.distill_loss, logits, logits, teacher_logit, teacher_index, tail, weight, temperature, reverse)
+
+
+def atspeed_distill_grad(logits, teacher_index, saved, grad_loss=None, temperature: float = 1.0, out=None):
+    """The gradient of atspeed_distill_loss with respect to the logits, in their type; grad_loss [rows] fp32 (None: 1)."""
+    return _run(_marshal.distill_grad, logits, logits, teacher_index, saved, grad_loss, temperature, out)
+
+
+class _Distill(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, teacher_logit, teacher_index, tail, weight, temperature, reverse):
+        loss, saved = atspeed_distill_loss(logits, teacher_logit, teacher_index, tail, weight, temperature, reverse)
+        ctx.save_for_backward(logits, teacher_index, saved)
+        ctx.temperature = temperature
+        return loss
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_loss):
+        logits, teacher_index, saved = ctx.saved_tensors
+        grad = atspeed_distill_grad(logits, teacher_index, saved, grad_loss.contiguous(), ctx.temperature)
+        return grad, None, None, None, None, None, None
+
+
+def distill(logits, teacher_logit, teacher_index, tail=None, weight=None, temperature: float = 1.0, reverse: bool = False):
+    """atspeed_distill_loss for autograd: loss [rows] fp32, differentiable once and by the logits alone.
+
+    A backward pass that is captured into a graph wants no other graph of the same parameters alive, as any other
+    backward pass of PyTorch.
+    """
+    for name, t in (("teacher_logit", teacher_logit), ("tail", tail), ("weight", weight)):
+        if t is not None and t.requires_grad:
+            raise ValueError(f"{name}: no gradient flows to it; detach it")
+    return _Distill.apply(logits, teacher_logit, teacher_index, tail, weight, temperature, reverse)
+
+
 class AlignTrainer:
     """Buffers of one engine's draft-head training.
 
@@ -36,7 +98,6 @@ class AlignTrainer:
 
     def __init__(self, eng: Engine, mode: str, alpha: float = 1.0, lr: float = 1e-3, betas=(0.9, 0.999),
                  eps: float = 1e-8, weight_decay: float = 0.01):
-        torch = eng.torch
         if eng.draft_dev is None:
             raise ValueError("the engine has no draft model")
         self.eng = eng

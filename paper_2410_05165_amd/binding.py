@@ -26,7 +26,9 @@ SYMBOLS = ("atspeed_workspace_bytes", "atspeed_create", "atspeed_destroy", "atsp
            "atspeed_set_timing", "atspeed_get_timing", "atspeed_align_data", "atspeed_align_step",
            "atspeed_target_search", "atspeed_mixed_search", "atspeed_page_plan", "atspeed_kv_append",
            "atspeed_tree_attention_workspace_bytes", "atspeed_tree_attention", "atspeed_logit_rules",
-           "atspeed_set_logit_rules")
+           "atspeed_set_logit_rules", "atspeed_beam_select_workspace_bytes", "atspeed_beam_select",
+           "atspeed_page_fork_workspace_bytes", "atspeed_page_fork", "atspeed_page_copy", "atspeed_kv_compact",
+           "atspeed_distill_loss", "atspeed_distill_grad")
 KERNEL_CLASSES = ("qkv", "o", "gu", "down", "lm_head", "attention", "row", "select")
 
 
@@ -100,6 +102,21 @@ LogitRulesArgs = _struct("LogitRulesArgs", """i: dtype B n_rows n_cols token_bas
        n_states n_out_rows state_by_request; f: mask_value; p: logits; l: logits_stride; p: out; l: out_stride;
     p: out_row row_off history hist_len node_token mask repetition frequency presence temperature bias;
     l: bias_stride; p: bias_index allowed state""")
+
+BeamSelectArgs = _struct("BeamSelectArgs", """i: dtype B n_rows n_cols k token_base log_probs n_paths max_path; p: logits;
+    l: logits_stride; p: row_off score done row_id paths path_len count parent token score_out paths_out path_len_out""")
+PageForkArgs = _struct("PageForkArgs", """i: B page_size max_pages n_pool;
+    p: held keep src block_table free_pages n_free shared length refused copy_src copy_dst copy_len""")
+PageCopyArgs = _struct("PageCopyArgs", """i: dtype n n_layers n_kv_heads d_head page_size n_pool;
+    p: k_data; l: k_page k_token k_head; p: v_data; l: v_page v_token v_head k_layer_stride v_layer_stride;
+    p: src dst length""")
+KvCompactArgs = _struct("KvCompactArgs", """i: dtype B n_layers n_kv_heads d_head page_size max_pages n_pool max_path;
+    p: k_data; l: k_page k_token k_head; p: v_data; l: v_page v_token v_head k_layer_stride v_layer_stride;
+    p: block_table ctx path n_path""")
+DistillLossArgs = _struct("DistillLossArgs", """i: dtype n_rows n_cols n_tops reverse; f: temperature; p: logits;
+    l: logits_stride; p: teacher_logit teacher_index tail weight loss saved""")
+DistillGradArgs = _struct("DistillGradArgs", """i: dtype n_rows n_cols n_tops; f: temperature; p: logits; l: logits_stride;
+    p: teacher_index saved grad_loss grad; l: grad_stride""")
 
 
 class AtspeedError(RuntimeError):

@@ -15,7 +15,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libatspeed.so")
 MARSHAL = os.path.join(HERE, "_marshal.so")
 SOURCES = ["runtime.hip", "gemm.hip", "gemm_f32.hip", "attention.hip", "misc.hip", "select.hip", "relaxed.hip", "align.hip",
-           "paged.hip", "tree_attention.hip", "rules.hip"]
+           "paged.hip", "tree_attention.hip", "rules.hip", "beam.hip", "fork.hip", "distill.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -50,6 +50,14 @@ __device__ __forceinline__ uint32_t float_order_key(float f) {
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
+// Orders a wave's LDS accesses before and behind it, in the compiler's eyes too: what its
+// lanes wrote is there for the others (the hardware keeps a wave's LDS accesses in order).
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // Row descriptors of one forward: which token runs where, and where its K/V go.
 struct Rows {
   int* M;            // [1] number of rows (device)

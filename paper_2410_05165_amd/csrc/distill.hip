@@ -1,0 +1,294 @@
+// Distillation of a draft from a teacher's top logits: the loss (atspeed_distill_loss) and
+// its gradient (atspeed_distill_grad).
+//
+// Both divergences live on n_tops + 1 buckets, the tops and the rest, and every column of
+// the rest has the gradient d A q_v with one A a row.  So the loss needs one pass over the
+// logits for their largest and the sums of their exponentials, the gradient one more that
+// writes exp(z - largest) times a number of the row, and then the tops' own values.
+//
+// The rest's share of q is summed by itself, without the tops (a bit a column in LDS says
+// which these are): as 1 - sum of the tops it would keep only what fp32 leaves of a small
+// difference, and A = 1 - p_rest / q_rest with it.
+#include <cfloat>
+#include <cmath>
+
+#include "common.h"
+#include "paged.h"
+
+namespace atspeed {
+
+typedef u32x4_t u32x4_any_t __attribute__((aligned(2)));   // 16 bytes at any element
+
+constexpr int kDistThreads = 256;
+constexpr int kMaxTops = 256;
+constexpr float kNoTop = -0.f;   // in the place of a top's gradient, which is never -0: no top
+
+template <class T>
+__device__ __forceinline__ void unpack(const u32x4_t raw, float (&x)[16 / sizeof(T)]) {
+  constexpr int VEC = 16 / sizeof(T);
+#pragma unroll
+  for (int i = 0; i < VEC; ++i)
+    x[i] = VEC == 4 ? __uint_as_float(raw[i]) : __uint_as_float(i & 1 ? raw[i / 2] & 0xffff0000u : raw[i / 2] << 16);
+}
+
+// Sums over the workgroup, the same bits in every thread.
+template <class F>
+__device__ __forceinline__ F sum_threads(F x, F* part) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
+  __syncthreads();
+  x = part[0];
+#pragma unroll
+  for (int w = 1; w < kDistThreads / 64; ++w) x += part[w];
+  return x;
+}
+template <class F>
+__device__ __forceinline__ F max_threads(F x, F* part) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) x = fmax(x, __shfl_xor(x, o));
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
+  __syncthreads();
+  x = part[0];
+#pragma unroll
+  for (int w = 1; w < kDistThreads / 64; ++w) x = fmax(x, part[w]);
+  return x;
+}
+
+// c: log2(e) / temperature.  exp2 of (z - top) * c with -infinity as 0 whatever top is.
+__device__ __forceinline__ float weight_of(float z, float top, float c) {
+  return z == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((z - top) * c);
+}
+
+template <class T>
+__global__ void __launch_bounds__(kDistThreads) distill_loss_kernel(atspeed_distill_loss_args a, float c) {
+  constexpr int VEC = 16 / sizeof(T);
+  extern __shared__ uint32_t bits[];               // a bit a column: a top
+  __shared__ int index[kMaxTops];
+  __shared__ double prob[kMaxTops], part64[kDistThreads / 64];
+  __shared__ float part32[kDistThreads / 64];
+  const int r = blockIdx.x, tid = threadIdx.x, m = a.n_tops, V = a.n_cols;
+  const T* row = static_cast<const T*>(a.logits) + (int64_t)r * a.logits_stride;
+  for (int i = tid; i < (V + 31) / 32; i += kDistThreads) bits[i] = 0;
+
+  // the teacher's buckets; thread j has top j
+  int mine = -1;
+  double t = -INFINITY;
+  if (tid < m) {
+    mine = a.teacher_index[(int64_t)r * m + tid];
+    const float z = St<T>::ld(static_cast<const T*>(a.teacher_logit) + (int64_t)r * m + tid);
+    if ((unsigned)mine >= (unsigned)V || z == -INFINITY) mine = -1;
+    if (mine >= 0) t = (double)z / (double)a.temperature;
+    index[tid] = mine;
+  }
+  const float weight = a.weight ? a.weight[r] : 1.f;
+  float* saved = a.saved + (int64_t)r * (2 + m);
+  __syncthreads();
+  if (mine >= 0) atomicOr(&bits[mine >> 5], 1u << (mine & 31));
+  if (!__syncthreads_or(mine >= 0) || weight == 0.f) {
+    if (tid < 2) saved[tid] = 0.f;
+    if (tid < m) saved[2 + tid] = kNoTop;
+    if (tid == 0) a.loss[r] = 0.f;
+    return;
+  }
+  const double tail = a.tail ? (double)a.tail[r] : -INFINITY;
+  const double t_top = fmax(max_threads(t, part64), tail);
+  const double w = mine >= 0 ? exp(t - t_top) : 0.0, w_rest = exp(tail - t_top);
+  const double w_all = sum_threads(w, part64) + w_rest;
+  const double log_w = t_top + log(w_all);
+  if (tid < m) prob[tid] = w / w_all;
+  __syncthreads();
+  // columns that were named twice: the first one has the sum
+  bool first = mine >= 0;
+  double p = 0.0;
+  if (mine >= 0)
+    for (int j = 0; j < m; ++j)
+      if (index[j] == mine) {
+        if (j < tid) first = false;
+        p += prob[j];
+      }
+
+  // one pass over the logits: the largest, and the sum of the others' exponentials
+  float top = -INFINITY, sum = 0.f;
+  for (int v0 = tid * VEC; v0 < V; v0 += kDistThreads * VEC) {
+    float x[VEC];
+    if (v0 + VEC <= V) {
+      unpack<T>(*reinterpret_cast<const u32x4_any_t*>(row + v0), x);
+    } else {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) x[i] = v0 + i < V ? St<T>::ld(row + v0 + i) : -INFINITY;
+    }
+    const uint32_t tops = bits[v0 >> 5] >> (v0 & 31);
+    float most = x[0];
+#pragma unroll
+    for (int i = 1; i < VEC; ++i) most = __builtin_elementwise_maximum(most, x[i]);
+    if (!(most <= top)) {
+      const float now = __builtin_elementwise_maximum(most, top);
+      if (top > -INFINITY) sum *= __builtin_amdgcn_exp2f((top - now) * c);
+      top = now;
+    }
+    if (top == -INFINITY) continue;
+    float some = 0.f;                              // vectors first: a thread's sum has few terms
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      const float e = __builtin_amdgcn_exp2f((x[i] - top) * c);
+      some += tops >> i & 1 ? 0.f : e;
+    }
+    sum += some;
+  }
+  // NaN and +infinity go through to the loss
+  const bool bad = __syncthreads_or(!(top < INFINITY));
+  const float z_top = bad ? NAN : max_threads(top, part32);
+  const double rest = sum_threads(top > -INFINITY ? (double)(sum * __builtin_amdgcn_exp2f((top - z_top) * c)) : 0.0, part64);
+  float z = 0.f;
+  double e = 0.0;
+  if (mine >= 0) {
+    z = St<T>::ld(row + mine);
+    e = weight_of(z, z_top, c);
+  }
+  const double all = rest + sum_threads(first ? e : 0.0, part64);
+
+  // the divergence, bucket by bucket
+  const bool empty = all == 0.0;                   // no logit but -infinity: q is 0
+  const double q = empty ? 0.0 : e / all, q_rest = empty ? 0.0 : rest / all, p_rest = w_rest / w_all;
+  const double log_all = log(all), inv_t = 1.0 / (double)a.temperature;
+  const double log_q = z == -INFINITY ? -INFINITY : (double)(z - z_top) * inv_t - log_all;
+  const double log_qr = rest == 0.0 ? -INFINITY : log(rest) - log_all, log_pr = tail - log_w;
+  double mass = 0.0, far = 0.0, mass_r = 0.0, far_r = 0.0;     // a bucket's weight, log of the quotient
+  if (a.reverse) {
+    mass = first && e > 0.0 ? q : 0.0;
+    far = log_q - log(p);
+    mass_r = rest > 0.0 ? q_rest : 0.0;
+    far_r = log_qr - log_pr;
+  } else {
+    mass = first && p > 0.0 ? p : 0.0;
+    far = log(p) - log_q;
+    mass_r = p_rest;
+    far_r = log_pr - log_qr;
+  }
+  if (bad || !(all == all)) mass_r = far_r = NAN;
+  const double loss = sum_threads(mass > 0.0 ? mass * far : 0.0, part64) + (mass_r == 0.0 ? 0.0 : mass_r * far_r);
+  const double step = (double)weight * (double)a.temperature;
+  double at_top = 0.0, a_rest = 0.0;
+  if (a.reverse) {
+    at_top = e > 0.0 ? q * (far - loss) : 0.0;
+    a_rest = rest > 0.0 ? far_r - loss : 0.0;
+  } else {
+    at_top = q - p;
+    a_rest = rest > 0.0 ? 1.0 - p_rest / q_rest : 0.0;
+  }
+  if (bad) at_top = a_rest = NAN;
+  if (tid < m) saved[2 + tid] = mine >= 0 ? (float)(step * at_top) + 0.f : kNoTop;
+  if (tid == 0) {
+    // beyond fp32's range where the rest is next to nothing
+    const double to_rest = all > 0.0 || bad ? step * a_rest / all : 0.0;
+    saved[0] = z_top;
+    saved[1] = fabs(to_rest) > FLT_MAX ? (float)copysign((double)FLT_MAX, to_rest) : (float)to_rest;
+    a.loss[r] = (float)(step * (double)a.temperature * loss);
+  }
+}
+
+// A workgroup a row and 4,096 columns.
+constexpr int kGradVecs = 16;   // columns a thread
+
+template <class T>
+__global__ void __launch_bounds__(kDistThreads) distill_grad_kernel(atspeed_distill_grad_args a, float c, int chunks) {
+  constexpr int VEC = 16 / sizeof(T), COLS = kDistThreads * kGradVecs;
+  const int r = blockIdx.x / chunks, v0 = blockIdx.x % chunks * COLS, m = a.n_tops, V = a.n_cols, tid = threadIdx.x;
+  const T* row = static_cast<const T*>(a.logits) + (int64_t)r * a.logits_stride;
+  T* out = static_cast<T*>(a.grad) + (int64_t)r * a.grad_stride;
+  const float* saved = a.saved + (int64_t)r * (2 + m);
+  const float g = a.grad_loss ? a.grad_loss[r] : 1.f;
+  const float top = saved[0], scale = saved[1] == 0.f ? 0.f : saved[1] * g;
+#pragma unroll
+  for (int k = 0; k < kGradVecs / VEC; ++k) {
+    const int v = v0 + (k * kDistThreads + tid) * VEC;
+    if (v >= V) continue;
+    if (v + VEC <= V) {
+      float x[VEC];
+      unpack<T>(*reinterpret_cast<const u32x4_any_t*>(row + v), x);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) x[i] = scale == 0.f ? 0.f : scale * weight_of(x[i], top, c);
+      u32x4_t raw;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        raw[i] = VEC == 4 ? __float_as_uint(x[i])
+                          : (uint32_t)f2bf(x[VEC == 4 ? 0 : 2 * i]) | (uint32_t)f2bf(x[VEC == 4 ? 0 : 2 * i + 1]) << 16;
+      *reinterpret_cast<u32x4_any_t*>(out + v) = raw;
+    } else {
+      for (int i = v; i < V; ++i) St<T>::st(out + i, scale == 0.f ? 0.f : scale * weight_of(St<T>::ld(row + i), top, c));
+    }
+  }
+  __syncthreads();               // the tops' own values come behind
+  if (tid < m) {
+    const int at = a.teacher_index[(int64_t)r * m + tid];
+    const float x = saved[2 + tid];
+    const bool is = __float_as_uint(x) != __float_as_uint(kNoTop);
+    if (is && at >= v0 && at < min(v0 + COLS, V)) St<T>::st(out + at, x == 0.f ? 0.f : x * g);
+  }
+}
+
+static atspeed_status check_distill(int dtype, int n_rows, int n_cols, int n_tops, float temperature) {
+  if (dtype != ATSPEED_FP32 && dtype != ATSPEED_BF16) return fail(ATSPEED_E_INVALID, "dtype");
+  if (n_rows < 0) return fail(ATSPEED_E_INVALID, "n_rows must be >= 0");
+  if (n_cols < 1 || n_cols > (1 << 20)) return fail(ATSPEED_E_INVALID, "n_cols must be 1..2^20");
+  if (n_tops < 1 || n_tops > kMaxTops) return fail(ATSPEED_E_INVALID, "n_tops must be 1..256");
+  if (!(temperature > 0.f) || !(temperature < INFINITY)) return fail(ATSPEED_E_INVALID, "temperature must be positive");
+  return ATSPEED_OK;
+}
+static float exponent_scale(float temperature) { return (float)(1.4426950408889634 / (double)temperature); }
+
+}  // namespace atspeed
+
+using namespace atspeed;
+
+extern "C" {
+
+atspeed_status atspeed_distill_loss(const atspeed_distill_loss_args* args, void* stream) {
+  if (!args) return fail(ATSPEED_E_INVALID, "args is null");
+  const atspeed_distill_loss_args& a = *args;
+  ST_TRY(check_distill(a.dtype, a.n_rows, a.n_cols, a.n_tops, a.temperature));
+  if (a.reverse && !a.tail) return fail(ATSPEED_E_INVALID, "the reverse form needs the teacher's tail");
+  if (a.n_rows == 0) return ATSPEED_OK;
+  if (!a.logits || !a.teacher_logit || !a.teacher_index || !a.loss || !a.saved)
+    return fail(ATSPEED_E_INVALID, "distill loss: null pointer");
+  if (a.logits_stride < a.n_cols && a.n_rows > 1) return fail(ATSPEED_E_SHAPE, "a row stride is below n_cols");
+  if (a.n_rows > kMaxGroups) return fail(ATSPEED_E_SHAPE, "distill loss: too many rows");
+  const size_t lds = (size_t)(a.n_cols + 31) / 32 * 4;
+  const float c = exponent_scale(a.temperature);
+  const dim3 grid(a.n_rows), threads(kDistThreads);
+  const bool bf16 = a.dtype == ATSPEED_BF16;
+  if (lds > (48 << 10))
+    HIP_TRY(hipFuncSetAttribute(bf16 ? (const void*)distill_loss_kernel<bf16_t> : (const void*)distill_loss_kernel<float>,
+                                hipFuncAttributeMaxDynamicSharedMemorySize, 1 << 17));
+  if (bf16) hipLaunchKernelGGL((distill_loss_kernel<bf16_t>), grid, threads, lds, (hipStream_t)stream, a, c);
+  else hipLaunchKernelGGL((distill_loss_kernel<float>), grid, threads, lds, (hipStream_t)stream, a, c);
+  HIP_TRY(hipGetLastError());
+  return ATSPEED_OK;
+}
+
+atspeed_status atspeed_distill_grad(const atspeed_distill_grad_args* args, void* stream) {
+  if (!args) return fail(ATSPEED_E_INVALID, "args is null");
+  const atspeed_distill_grad_args& a = *args;
+  ST_TRY(check_distill(a.dtype, a.n_rows, a.n_cols, a.n_tops, a.temperature));
+  if (a.n_rows == 0) return ATSPEED_OK;
+  if (!a.logits || !a.teacher_index || !a.saved || !a.grad) return fail(ATSPEED_E_INVALID, "distill grad: null pointer");
+  if ((a.logits_stride < a.n_cols || a.grad_stride < a.n_cols) && a.n_rows > 1)
+    return fail(ATSPEED_E_SHAPE, "a row stride is below n_cols");
+  if (a.grad == a.logits) return fail(ATSPEED_E_INVALID, "distill grad: an output is one of the inputs");
+  const int cols = kDistThreads * kGradVecs, chunks = (a.n_cols + cols - 1) / cols;
+  const long long groups = (long long)a.n_rows * chunks;
+  if (groups > kMaxGroups) return fail(ATSPEED_E_SHAPE, "distill grad: too many rows x columns");
+  const float c = exponent_scale(a.temperature);
+  const dim3 grid((unsigned)groups), threads(kDistThreads);
+  if (a.dtype == ATSPEED_BF16)
+    hipLaunchKernelGGL((distill_grad_kernel<bf16_t>), grid, threads, 0, (hipStream_t)stream, a, c, chunks);
+  else
+    hipLaunchKernelGGL((distill_grad_kernel<float>), grid, threads, 0, (hipStream_t)stream, a, c, chunks);
+  HIP_TRY(hipGetLastError());
+  return ATSPEED_OK;
+}
+
+}  // extern "C"

@@ -8,6 +8,7 @@
 // for a tensor that does not fit and AtspeedError for a status.
 #include <Python.h>
 
+#include <algorithm>
 #include <cmath>
 #include <initializer_list>
 #include <limits>
@@ -435,6 +436,261 @@ PyObject* logit_rules(PyObject*, PyObject* const* o, Py_ssize_t n) {
   });
 }
 
+// A float32 or bfloat16 [rows, cols] whose rows are contiguous, rows `stride` elements apart.
+struct Matrix {
+  const at::Tensor& t;
+  int64_t rows, cols, stride;
+  int32_t dtype;
+};
+Matrix matrix(const at::Tensor& t, const char* name) {
+  if (t.dim() != 2 || (t.size(1) > 1 && t.stride(1) != 1)) bad(std::string(name) + ": want [rows, cols], rows contiguous");
+  return {t, t.size(0), t.size(1), t.size(0) > 1 ? t.stride(0) : t.size(1), dtype_of(t, name)};
+}
+
+// logits, row_off, k, score, done, token_base, log_probs, row_id, paths, path_len, stream
+PyObject* beam_select(PyObject*, PyObject* const* o, Py_ssize_t n) {
+  return guarded(n, 11, [&]() -> PyObject* {
+    const Matrix x = matrix(gpu_tensor(o[0], "logits"), "logits");
+    const at::Device dev = x.t.device();
+    const c10::ScalarType f32 = c10::ScalarType::Float, i32 = c10::ScalarType::Int;
+    const int64_t B = tensor(o[1], "row_off").numel() - 1;
+    atspeed_beam_select_args a{};
+    a.dtype = x.dtype;
+    a.B = int32(B, "B");
+    a.n_rows = int32(x.rows, "rows");
+    a.n_cols = int32(x.cols, "cols");
+    a.k = int32(o[2], "k");
+    a.token_base = int32(o[5], "token_base");
+    a.log_probs = flag(o[6]);
+    a.logits = address<void>(x.t);
+    a.logits_stride = x.stride;
+    a.row_off = want_i32(o[1], "row_off", {B + 1}, dev);
+    a.score = want<float>(o[3], "score", f32, {x.rows}, dev);
+    a.done = want_i32(o[4], "done", {x.rows}, dev);
+    a.row_id = want_i32(o[7], "row_id", {x.rows}, dev);
+    const bool with_paths = o[8] != Py_None;
+    if (with_paths != (o[9] != Py_None)) bad("paths and path_len go together");
+    if (with_paths) {
+      const at::Tensor& paths = tensor(o[8], "paths");
+      if (paths.dim() != 2) bad("paths: want [n, max_path]");
+      a.n_paths = int32(paths.size(0), "paths");
+      a.max_path = int32(paths.size(1), "max_path");
+      a.paths = want_i32(o[8], "paths", {paths.size(0), paths.size(1)}, dev);
+    }
+    a.path_len = want_i32(o[9], "path_len", {a.n_paths}, dev);
+    if (B < 1 || a.k < 1) bad("want row_off of two numbers at least, and k of 1 at least");
+    const int64_t k = std::min(a.k, 256), P = a.max_path;   // a larger k is refused below
+    const at::Tensor count = fresh({B}, i32, dev), parent = fresh({B, k}, i32, dev), token = fresh({B, k}, i32, dev),
+                     score = fresh({B, k}, f32, dev);
+    at::Tensor paths, path_len, ws;
+    a.count = address<int32_t>(count);
+    a.parent = address<int32_t>(parent);
+    a.token = address<int32_t>(token);
+    a.score_out = address<float>(score);
+    if (with_paths) {
+      paths = fresh({B, k, P}, i32, dev);
+      path_len = fresh({B, k}, i32, dev);
+      a.paths_out = address<int32_t>(paths);
+      a.path_len_out = address<int32_t>(path_len);
+    }
+    size_t need = 0;
+    check(atspeed_beam_select_workspace_bytes(&a, &need));
+    ws = fresh({(int64_t)need}, c10::ScalarType::Byte, dev);
+    void *const st = stream_of(o[10]), *const at = address<void>(ws);
+    enqueue([&] { return atspeed_beam_select(&a, at, need, st); });
+    Ref r(PyTuple_New(6));
+    const at::Tensor* outs[6] = {&count, &parent, &token, &score, &paths, &path_len};
+    for (int i = 0; i < 6; ++i)
+      PyTuple_SET_ITEM(r.o, i, outs[i]->defined() ? Ref(THPVariable_Wrap(*outs[i])).release() : held(Py_None));
+    return r.release();
+  });
+}
+
+// held, keep, block_table, free_pages, n_free, shared, page_size, src, stream
+PyObject* page_fork(PyObject*, PyObject* const* o, Py_ssize_t n) {
+  return guarded(n, 9, [&]() -> PyObject* {
+    const at::Tensor& table = gpu_tensor(o[2], "block_table");
+    if (table.dim() != 2) bad("block_table: want [B, max_pages]");
+    const at::Device dev = table.device();
+    const int64_t B = table.size(0), most = table.size(1), pool = tensor(o[3], "free_pages").numel();
+    atspeed_page_fork_args a{};
+    a.B = int32(B, "B");
+    a.page_size = int32(o[6], "page_size");
+    a.max_pages = int32(most, "max_pages");
+    a.n_pool = int32(pool, "free_pages");
+    a.held = want_i32(o[0], "held", {B}, dev);
+    a.keep = want_i32(o[1], "keep", {B}, dev);
+    a.src = want_i32(o[7], "src", {B}, dev);
+    a.block_table = want_i32(o[2], "block_table", {B, most}, dev);
+    a.free_pages = want_i32(o[3], "free_pages", {pool}, dev);
+    a.n_free = want_i32(o[4], "n_free", {1}, dev);
+    a.shared = want_i32(o[5], "shared", {pool}, dev);
+    const at::Tensor buf = fresh({5 * B}, c10::ScalarType::Int, dev);
+    int32_t* p = address<int32_t>(buf);
+    a.length = p;
+    a.refused = p + B;
+    a.copy_src = p + 2 * B;
+    a.copy_dst = p + 3 * B;
+    a.copy_len = p + 4 * B;
+    size_t need = 0;
+    check(atspeed_page_fork_workspace_bytes(&a, &need));
+    const at::Tensor ws = fresh({(int64_t)need}, c10::ScalarType::Byte, dev);
+    void *const st = stream_of(o[8]), *const at = address<void>(ws);
+    enqueue([&] { return atspeed_page_fork(&a, at, need, st); });
+    for (const int i : {2, 3, 4, 5}) written(o[i]);
+    Ref r(PyTuple_New(5));
+    for (int i = 0; i < 5; ++i) PyTuple_SET_ITEM(r.o, i, Ref(THPVariable_Wrap(piece(buf, i * B, B))).release());
+    return r.release();
+  });
+}
+
+// Caches of one layer [pages, page_size, kv_heads, d_head] or several [layers, ...].
+struct Layers {
+  Caches c;
+  int32_t n;
+  int64_t k_stride, v_stride;
+};
+Layers layers(PyObject* ko, PyObject* vo) {
+  const at::Tensor& k = gpu_tensor(ko, "k_cache");
+  const at::Tensor& v = tensor(vo, "v_cache");
+  if (k.dim() == 4) return {caches(ko, vo), 1, 0, 0};
+  if (k.dim() != 5) bad("k_cache: want [layers, pages, page_size, kv_heads, d_head]");
+  if (v.sizes() != k.sizes() || v.scalar_type() != k.scalar_type() || v.device() != k.device() || k.stride(4) != 1 ||
+      v.stride(4) != 1)
+    bad("the caches want one type, shape and device, the last dimension contiguous");
+  return {{k.device(), k.scalar_type(), dtype_of(k, "k_cache"), int32(k.size(1), "pages"), int32(k.size(2), "page_size"),
+           int32(k.size(3), "kv_heads"), int32(k.size(4), "d_head"),
+           {address<void>(k), stride(k, 1), stride(k, 2), stride(k, 3)},
+           {address<void>(v), stride(v, 1), stride(v, 2), stride(v, 3)}},
+          int32(k.size(0), "layers"), stride(k, 0), stride(v, 0)};
+}
+template <class A>
+void set_layers(A& a, const Layers& l) {
+  a.dtype = l.c.dtype;
+  a.n_layers = l.n;
+  a.n_kv_heads = l.c.heads;
+  a.d_head = l.c.dh;
+  a.page_size = l.c.page;
+  a.n_pool = l.c.pool;
+  a.k_pages = l.c.k;
+  a.v_pages = l.c.v;
+  a.k_layer_stride = l.k_stride;
+  a.v_layer_stride = l.v_stride;
+}
+
+// k_cache, v_cache, src, dst, length, stream
+PyObject* page_copy(PyObject*, PyObject* const* o, Py_ssize_t n) {
+  return guarded(n, 6, [&]() -> PyObject* {
+    const Layers l = layers(o[0], o[1]);
+    const int64_t rows = tensor(o[2], "src").numel();
+    atspeed_page_copy_args a{};
+    set_layers(a, l);
+    a.n = int32(rows, "copies");
+    a.src = want_i32(o[2], "src", {rows}, l.c.dev);
+    a.dst = want_i32(o[3], "dst", {rows}, l.c.dev);
+    a.length = want_i32(o[4], "length", {rows}, l.c.dev);
+    void* const st = stream_of(o[5]);
+    enqueue([&] { return atspeed_page_copy(&a, st); });
+    written(o[0]);
+    written(o[1]);
+    Py_RETURN_NONE;
+  });
+}
+
+// k_cache, v_cache, block_table, ctx, path, n_path, stream
+PyObject* kv_compact(PyObject*, PyObject* const* o, Py_ssize_t n) {
+  return guarded(n, 7, [&]() -> PyObject* {
+    const Layers l = layers(o[0], o[1]);
+    const at::Tensor& table = tensor(o[2], "block_table");
+    const at::Tensor& path = tensor(o[4], "path");
+    if (table.dim() != 2 || path.dim() != 2) bad("want block_table [B, max_pages] and path [B, max_path]");
+    const int64_t B = table.size(0), most = table.size(1), P = path.size(1);
+    atspeed_kv_compact_args a{};
+    set_layers(a, l);
+    a.B = int32(B, "B");
+    a.max_pages = int32(most, "max_pages");
+    a.max_path = int32(P, "max_path");
+    a.block_table = want_i32(o[2], "block_table", {B, most}, l.c.dev);
+    a.ctx = want_i32(o[3], "ctx", {B}, l.c.dev);
+    a.path = want_i32(o[4], "path", {B, P}, l.c.dev);
+    a.n_path = want_i32(o[5], "n_path", {B}, l.c.dev);
+    void* const st = stream_of(o[6]);
+    enqueue([&] { return atspeed_kv_compact(&a, st); });
+    written(o[0]);
+    written(o[1]);
+    Py_RETURN_NONE;
+  });
+}
+
+// logits, teacher_logit, teacher_index, tail, weight, temperature, reverse, stream
+PyObject* distill_loss(PyObject*, PyObject* const* o, Py_ssize_t n) {
+  return guarded(n, 8, [&]() -> PyObject* {
+    const Matrix x = matrix(gpu_tensor(o[0], "logits"), "logits");
+    const at::Device dev = x.t.device();
+    const c10::ScalarType f32 = c10::ScalarType::Float;
+    const at::Tensor& index = tensor(o[2], "teacher_index");
+    if (index.dim() != 2) bad("teacher_index: want [rows, tops]");
+    const int64_t m = index.size(1);
+    atspeed_distill_loss_args a{};
+    a.dtype = x.dtype;
+    a.n_rows = int32(x.rows, "rows");
+    a.n_cols = int32(x.cols, "cols");
+    a.n_tops = int32(m, "tops");
+    a.reverse = flag(o[6]);
+    a.temperature = number(o[5]);
+    a.logits = address<void>(x.t);
+    a.logits_stride = x.stride;
+    tensor(o[1], "teacher_logit");
+    a.teacher_logit = want<void>(o[1], "teacher_logit", x.t.scalar_type(), {x.rows, m}, dev);
+    a.teacher_index = want_i32(o[2], "teacher_index", {x.rows, m}, dev);
+    a.tail = want<float>(o[3], "tail", f32, {x.rows}, dev);
+    a.weight = want<float>(o[4], "weight", f32, {x.rows}, dev);
+    const at::Tensor loss = fresh({x.rows}, f32, dev), saved = fresh({x.rows, 2 + m}, f32, dev);
+    a.loss = address<float>(loss);
+    a.saved = address<float>(saved);
+    void* const st = stream_of(o[7]);
+    enqueue([&] { return atspeed_distill_loss(&a, st); });
+    Ref r(PyTuple_New(2));
+    PyTuple_SET_ITEM(r.o, 0, Ref(THPVariable_Wrap(loss)).release());
+    PyTuple_SET_ITEM(r.o, 1, Ref(THPVariable_Wrap(saved)).release());
+    return r.release();
+  });
+}
+
+// logits, teacher_index, saved, grad_loss, temperature, out, stream
+PyObject* distill_grad(PyObject*, PyObject* const* o, Py_ssize_t n) {
+  return guarded(n, 7, [&]() -> PyObject* {
+    const Matrix x = matrix(gpu_tensor(o[0], "logits"), "logits");
+    const at::Device dev = x.t.device();
+    const c10::ScalarType f32 = c10::ScalarType::Float;
+    const at::Tensor& index = tensor(o[1], "teacher_index");
+    if (index.dim() != 2) bad("teacher_index: want [rows, tops]");
+    const int64_t m = index.size(1);
+    const at::Tensor out = o[5] == Py_None ? fresh({x.rows, x.cols}, x.t.scalar_type(), dev) : tensor(o[5], "out");
+    const Matrix g = matrix(out, "out");
+    if (g.rows != x.rows || g.cols != x.cols || g.dtype != x.dtype || out.device() != dev)
+      bad("out: want the logits' type, shape and device");
+    atspeed_distill_grad_args a{};
+    a.dtype = x.dtype;
+    a.n_rows = int32(x.rows, "rows");
+    a.n_cols = int32(x.cols, "cols");
+    a.n_tops = int32(m, "tops");
+    a.temperature = number(o[4]);
+    a.logits = address<void>(x.t);
+    a.logits_stride = x.stride;
+    a.teacher_index = want_i32(o[1], "teacher_index", {x.rows, m}, dev);
+    tensor(o[2], "saved");
+    a.saved = want<float>(o[2], "saved", f32, {x.rows, 2 + m}, dev);
+    a.grad_loss = want<float>(o[3], "grad_loss", f32, {x.rows}, dev);
+    a.grad = address<void>(out);
+    a.grad_stride = g.stride;
+    void* const st = stream_of(o[6]);
+    enqueue([&] { return atspeed_distill_grad(&a, st); });
+    written(o[5]);
+    return given_or_new(o[5], out);
+  });
+}
+
 PyObject* set_error(PyObject*, PyObject* cls) {
   Py_XINCREF(cls);
   Py_XSETREF(g_error, cls);
@@ -443,6 +699,8 @@ PyObject* set_error(PyObject*, PyObject* cls) {
 
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(page_plan), FAST(kv_append), FAST(tree_attention), FAST(logit_rules),
+                         FAST(beam_select), FAST(page_fork), FAST(page_copy), FAST(kv_compact), FAST(distill_loss),
+                         FAST(distill_grad),
                          {"set_error", set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

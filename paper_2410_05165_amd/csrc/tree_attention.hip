@@ -79,13 +79,6 @@ __device__ __forceinline__ N wave_scan(N x) {
   x += from(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});   // 31 to the rows behind
   return x;
 }
-// Orders a wave's LDS accesses before and behind it, in the compiler's eyes too: what its
-// lanes wrote is there for the others (the hardware keeps a wave's LDS accesses in order).
-__device__ __forceinline__ void wave_sync() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
 __device__ __forceinline__ int round_up64(int n) { return (n + 63) & ~63; }
 
 // One workgroup's share: a request, a key/value head, a tile of its queries (row i, head

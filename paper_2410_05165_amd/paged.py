@@ -1,6 +1,7 @@
-"""Verifying drafted trees on a caller's own target: the step plan, the cache append,
-tree attention over pages and the logit rules of include/atspeed.h on PyTorch tensors,
-and ``PagedKV``, the caches and page tables of one target.
+"""Verifying drafted trees and beam search on a caller's own target: the step plan, the
+cache append, tree attention over pages, the logit rules, beam selection, forked pages and
+accepted paths of include/atspeed.h on PyTorch tensors, and ``PagedKV``, the caches and page
+tables of one target.
 
 The functions have the library's names, check their tensors, allocate outputs that are
 not given (_marshal.so, csrc/marshal.cpp) and enqueue on the current stream of the
@@ -99,17 +100,75 @@ def atspeed_logit_rules(logits, row_off, token_base: int = 0, history=None, hist
                 state_by_request)
 
 
+class BeamSelection(NamedTuple):
+    """What atspeed_beam_select writes: the best first, -1, -1 and -inf from ``count`` on."""
+    count: torch.Tensor                  # [B] int32
+    parent: torch.Tensor                 # [B, k] int32
+    token: torch.Tensor                  # [B, k] int32
+    score: torch.Tensor                  # [B, k] fp32
+    paths: Optional[torch.Tensor]        # [B, k, max_path] int32
+    path_len: Optional[torch.Tensor]     # [B, k] int32
+
+
+def atspeed_beam_select(logits, row_off, k: int, score=None, done=None, token_base: int = 0, log_probs: bool = False,
+                        row_id=None, paths=None, path_len=None) -> BeamSelection:
+    """The k best continuations of each request's beams, by score + log-softmax of the logits.
+
+    logits [rows, cols] (fp32 or bf16) with a beam a row, row_off [B + 1]; score [rows] fp32; done, row_id [rows] int32;
+    log_probs: the logits are log-probabilities.  paths [n, max_path] and path_len [n] int32 are the beams' tokens by
+    the numbers that parent gives (row_id's, or the rows'); the outputs are those of the chosen ones, grown.
+    """
+    return BeamSelection._make(_run(_marshal.beam_select, logits, logits, row_off, k, score, done, token_base, log_probs,
+                                    row_id, paths, path_len))
+
+
+class PageFork(NamedTuple):
+    """What atspeed_page_fork writes (int32 [B]): the rows' lengths, and the pages to copy (-1, -1, 0: none)."""
+    length: torch.Tensor
+    refused: torch.Tensor
+    copy_src: torch.Tensor
+    copy_dst: torch.Tensor
+    copy_len: torch.Tensor
+
+
+def atspeed_page_fork(held, keep, block_table, free_pages, n_free, shared, page_size: int, src=None) -> PageFork:
+    """Row j of the tables goes on with the first keep[j] tokens of row src[j] (-1: none; None: its own).
+
+    held, keep (None: all), src [B] int32; ``block_table`` [B, max_pages], ``free_pages`` and ``shared`` [pool] and
+    ``n_free`` [1] change in place.  Copy copy_len tokens of copy_src to copy_dst (atspeed_page_copy) in every layer.
+    """
+    return PageFork._make(_run(_marshal.page_fork, block_table, held, keep, block_table, free_pages, n_free, shared,
+                               page_size, src))
+
+
+def atspeed_page_copy(k_cache, v_cache, src, dst, length):
+    """Copies the first length[i] tokens of page src[i] to page dst[i] (int32 [n]; pages outside the pool: skipped).
+
+    Caches [layers, pages, page_size, kv_heads, d_head] or without layers; strided, the last dimension contiguous.
+    """
+    _run(_marshal.page_copy, k_cache, k_cache, v_cache, src, dst, length)
+
+
+def atspeed_kv_compact(k_cache, v_cache, block_table, ctx, path, n_path):
+    """Moves the new rows path[b][:n_path[b]] (ascending row numbers) of each request to positions ctx[b], ctx[b] + 1, ...
+
+    Caches as for atspeed_page_copy; block_table [B, max_pages], ctx, n_path [B], path [B, max_path] int32.
+    """
+    _run(_marshal.kv_compact, k_cache, k_cache, v_cache, block_table, ctx, path, n_path)
+
+
 class PagedKV:
     """Key and value caches of one target in pages, with the requests' page tables and the free list.
 
-    One page table serves every layer.  ``plan`` starts a step, ``append`` and ``attention`` run per layer.
-    A request is a row of the tables; add rows to an ended request's row to start another in its place
-    (keep 0 gives its pages back first).  The tables, ``length`` and ``n_free`` change in place, so a step can be
-    captured into a graph: each replay goes on from the step before, captured or not.
+    One page table serves every layer.  ``plan`` starts a step, ``append`` and ``attention`` run per layer, and
+    ``compact`` ends a verified one.  A request is a row of the tables; add rows to an ended request's row to start
+    another in its place (keep 0 gives its pages back first).  With ``share`` rows may hold pages together: ``plan``
+    takes ``src`` and forks (a beam search has a row a beam).  The tables, ``length`` and ``n_free`` change in place, so
+    a step can be captured into a graph: each replay goes on from the step before, captured or not.
     """
 
     def __init__(self, n_layers: int, n_pages: int, page_size: int, n_kv_heads: int, d_head: int, max_batch: int,
-                 max_len: int, dtype=torch.bfloat16, device="cuda:0"):
+                 max_len: int, dtype=torch.bfloat16, device="cuda:0", share: bool = False):
         dev = torch.device(device)
         shape = (n_layers, n_pages, page_size, n_kv_heads, d_head)
         i32 = dict(dtype=torch.int32, device=dev)
@@ -119,11 +178,27 @@ class PagedKV:
         self.free_pages = torch.arange(n_pages, **i32)
         self.n_free = torch.full((1,), n_pages, **i32)
         self.length = torch.zeros(max_batch, **i32)      # tokens whose pages each request holds
+        self.shared = torch.zeros(n_pages, **i32) if share else None    # further holders of each page
 
-    def plan(self, keep, add, max_rows: int, parent=None) -> StepPlan:
-        """Keeps keep[b] of each request's tokens and makes room for add[b] rows (atspeed_page_plan)."""
-        p = atspeed_page_plan(self.length, keep, add, self.block_table, self.free_pages, self.n_free, self.page_size,
-                              max_rows, parent)
+    def plan(self, keep, add, max_rows: int, parent=None, src=None) -> StepPlan:
+        """Keeps keep[b] of each request's tokens and makes room for add[b] rows (atspeed_page_plan).
+
+        With ``share``: row b goes on with keep[b] tokens (keep None: all) of row src[b] (-1: none; src None: its own).
+        A row that the fork refuses is refused by the plan too, as a request that keeps more than it holds.
+        """
+        held = self.length
+        if self.shared is not None:
+            f = atspeed_page_fork(held, keep, self.block_table, self.free_pages, self.n_free, self.shared, self.page_size,
+                                  src=src)
+            atspeed_page_copy(self.k, self.v, f.copy_src, f.copy_dst, f.copy_len)
+            held = f.length
+            keep = torch.where(f.refused == 0, held, held + 1)
+        elif src is not None:
+            raise ValueError("src: rows go on as others in caches with share=True alone")
+        elif keep is None:
+            keep = held
+        p = atspeed_page_plan(held, keep, add, self.block_table, self.free_pages, self.n_free, self.page_size, max_rows,
+                              parent)
         with torch.inference_mode():                     # caches made under it are written outside it, too
             torch._foreach_copy_([self.length, self.n_free], [p.length, p.n_free])   # in place, for captured steps
         return p
@@ -137,3 +212,12 @@ class PagedKV:
         return atspeed_tree_attention(q, self.k[layer], self.v[layer], self.block_table, plan.row_off, plan.ctx,
                                       self.max_len if max_ctx is None else max_ctx, max_new,
                                       mask=None if plan.mask is None else plan.mask[:q.shape[0]], **kw)
+
+    def compact(self, plan: StepPlan, path, n_path):
+        """Moves each request's accepted rows path[b][:n_path[b]] of the plan behind its context, in every layer.
+
+        Returns what the next plan keeps: the context and the path (the context alone where n_path is below 1 or the
+        request was refused: then its length).
+        """
+        atspeed_kv_compact(self.k, self.v, self.block_table, plan.ctx, path, n_path)
+        return torch.where(plan.ctx < 0, self.length, plan.ctx + n_path.clamp(min=0))
