@@ -6,7 +6,7 @@
 // ranks a request's lists by score[r] - log sum + logit.
 //
 // Scores of different beams are compared, so the normaliser must not move them past each
-// other: it is taken in 64 bits (exponentials to 1.1e-12), where fp32 exponentials (1e-7 of the sum)
+// other: it is taken in 64 bits (exponentials to 2.4e-10), where fp32 exponentials (1e-7 of the sum)
 // would swap one pair of neighbours in some thousand lists.  64-bit vector instructions
 // run at the rate of 32-bit ones here.
 #include <algorithm>
@@ -22,395 +22,651 @@ typedef u32x4_t u32x4_any_t __attribute__((aligned(2)));   // 16 bytes at any el
 
 constexpr int kBeamThreads = 256, kBeamWaves = kBeamThreads / 64;
 constexpr int kLane = 16;              // columns of a lane in a tile
-constexpr int kTile = 64 * kLane;      // columns of a wave's tile
+constexpr int kTile = 64 * kLane;      // columns of a tile, which a wave takes at once
 constexpr int kMaxBeams = 256;         // k
 
-// e^d for d from -740 to 0, to 1.1e-12 of itself and 1 at 0: 2^n by the exponent, 2^r for r on
-// [-1/2, 1/2] by the polynomial of degree 8 that is 1 at 0 and has the least largest relative
-// error (found by exchanging its extrema).  The difference of two fp32 logits is exact enough however large they are.
+// Where differences are held at it, nothing is left of the exponential.
 constexpr float kLeast = -740.f;
-__device__ __forceinline__ double exp_64(double d) {
+// e^d for N numbers d from -1e9 to 0, to 2.4e-10 of themselves and 1 at 0, side by side: 2^n by
+// the exponent, 2^r for r on [-1/2, 1/2] by the polynomial of degree 7 that is 1 at 0 and has
+// the least largest relative error (found by exchanging its extrema).
+template <int N>
+__device__ __forceinline__ void exp_64(double (&d)[N]) {
   constexpr double log2e = 0x1.71547652b82fep0;
-  const double shifted = __builtin_fma(d, log2e, 0x1.8p52);   // its low bits are the nearest whole number
-  const double r = __builtin_fma(d, log2e, 0x1.8p52 - shifted);
-  double p = 0x1.663487d8abc81p-20;
-  p = __builtin_fma(p, r, 0x1.00ee071c7c030p-16);
-  p = __builtin_fma(p, r, 0x1.4306c1165a375p-13);
-  p = __builtin_fma(p, r, 0x1.5d872975c4ed2p-10);
-  p = __builtin_fma(p, r, 0x1.3b2ab7f3b3217p-7);
-  p = __builtin_fma(p, r, 0x1.c6b08defc25fdp-5);
-  p = __builtin_fma(p, r, 0x1.ebfbdff7c5a79p-3);
-  p = __builtin_fma(p, r, 0x1.62e42fef7a78bp-1);
-  p = __builtin_fma(p, r, 1.0);
-  return __builtin_ldexp(p, (int)(unsigned)__double_as_longlong(shifted));
+  constexpr double c[8] = {1.0, 0x1.62e4300b9dab4p-1, 0x1.ebfbe045705a1p-3, 0x1.c6b0551d56c6dp-5,
+                           0x1.3b2a1bf5b7f04p-7, 0x1.5dc05149ba9cap-10, 0x1.443f95e689c5dp-13, 0x1.c04815415f25ep-17};
+  double shifted[N], r[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) shifted[i] = __builtin_fma(d[i], log2e, 0x1.8p52);   // its low bits: the nearest whole number
+#pragma unroll
+  for (int i = 0; i < N; ++i) r[i] = __builtin_fma(d[i], log2e, 0x1.8p52 - shifted[i]);
+#pragma unroll
+  for (int i = 0; i < N; ++i) d[i] = c[7];
+#pragma unroll
+  for (int s = 6; s >= 0; --s)
+#pragma unroll
+    for (int i = 0; i < N; ++i) d[i] = __builtin_fma(d[i], r[i], c[s]);
+#pragma unroll
+  for (int i = 0; i < N; ++i) d[i] = __builtin_ldexp(d[i], (int)(unsigned)__double_as_longlong(shifted[i]));
 }
 // e^(x - top), x <= top
-__device__ __forceinline__ double exp_below(double x, double top) { return exp_64(fmax(x - top, (double)kLeast)); }
-
-// fp32 (no NaN) to whole numbers of the same order, -0 as 0; and back.
-__device__ __forceinline__ uint32_t order_of(float x) { return float_order_key(x + 0.f); }
-__device__ __forceinline__ float logit_of(uint32_t key) {
-  return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
+__device__ __forceinline__ double exp_below(double x, double top) {
+  double d[1] = {fmax(x - top, (double)kLeast)};
+  exp_64(d);
+  return d[0];
 }
-// A column's place among its row's: by the logit, then the lower column.
-__device__ __forceinline__ u64 column_key(uint32_t order, int col) { return ((u64)order << 32) | (0xffffffffu - (unsigned)col); }
+
+// Logits (no NaN) to whole numbers of the same order and as many bits, -0 as 0; and back.
+template <class T>
+__device__ __forceinline__ uint32_t order_of(float x) { return float_order_key(x + 0.f) >> (32 - 8 * sizeof(T)); }
+template <class T>
+__device__ __forceinline__ float logit_of(uint32_t order) {
+  const uint32_t key = order << (32 - 8 * sizeof(T));
+  const uint32_t bits = key & 0x80000000u ? key ^ 0x80000000u : ~key;
+  return __uint_as_float(sizeof(T) == 2 ? bits & 0xffff0000u : bits);
+}
+// A column's place among its row's, by the logit, then the lower column: the logit's order over
+// 0xffffffff - column.
 __device__ __forceinline__ int column_of(u64 key) { return (int)(0xffffffffu - (unsigned)key); }
 __device__ __forceinline__ u64 order64(double x) {
   const u64 u = (u64)__double_as_longlong(x + 0.0);
   return u >> 63 ? ~u : u | (1ull << 63);
 }
+__device__ __forceinline__ double score_of(u64 u) {
+  return __longlong_as_double((long long)(u >> 63 ? u ^ (1ull << 63) : ~u));
+}
 
 // Largest of two, NaN if either is.
 __device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+// A word of the lane that step s of a reduction over the wave pairs this one with: lanes 1,
+// 2, then mirrored within 8 and 16 (whose parts are alike by then), 16 and 32 apart.
+template <int S>
+__device__ __forceinline__ uint32_t partner(uint32_t x) {
+  if (S == 0) return __builtin_amdgcn_mov_dpp(x, 0xB1, 0xf, 0xf, true);         // quad_perm 1 0 3 2
+  if (S == 1) return __builtin_amdgcn_mov_dpp(x, 0x4E, 0xf, 0xf, true);         // quad_perm 2 3 0 1
+  if (S == 2) return __builtin_amdgcn_mov_dpp(x, 0x141, 0xf, 0xf, true);        // row_half_mirror
+  if (S == 3) return __builtin_amdgcn_mov_dpp(x, 0x140, 0xf, 0xf, true);        // row_mirror
+  return __shfl_xor(x, S == 4 ? 16 : 32);
+}
+template <int S>
+__device__ __forceinline__ double partner(double x) {
+  const u64 u = (u64)__double_as_longlong(x);
+  return __longlong_as_double((long long)((u64)partner<S>((uint32_t)(u >> 32)) << 32 | partner<S>((uint32_t)u)));
+}
 __device__ __forceinline__ float wave_max_nan(float x) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) x = max_nan(x, __shfl_xor(x, o));
+  static_for<6>([&](auto s) { x = max_nan(x, __uint_as_float(partner<s>(__float_as_uint(x)))); });
+  return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x)));
+}
+__device__ __forceinline__ double wave_sum(double x) {
+  static_for<6>([&](auto s) { x += partner<s>(x); });
+  return x;
+}
+
+// Sum of the lanes up to this one.
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);     // row_shr 1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, true);     // the rows before: row_bcast 15, 31
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, true);
   return x;
 }
 
 // A lane's 16 columns of a tile: 16-byte loads of consecutive lanes, wherever the row begins.
 template <class T>
-__device__ __forceinline__ int column_at(int lane, int e) {
-  constexpr int VEC = 16 / sizeof(T);
-  return (e / VEC) * (64 * VEC) + lane * VEC + e % VEC;
-}
-template <class T>
-__device__ __forceinline__ void load_tile(const T* row, int c0, int n_cols, int lane, float (&x)[kLane]) {
-  constexpr int VEC = 16 / sizeof(T);
-  if (c0 + kTile <= n_cols) {
-#pragma unroll
-    for (int v = 0; v < kLane / VEC; ++v) {
-      const u32x4_t raw = *reinterpret_cast<const u32x4_any_t*>(row + c0 + (v * 64 + lane) * VEC);
-#pragma unroll
-      for (int i = 0; i < VEC; ++i)
-        x[v * VEC + i] = VEC == 4 ? __uint_as_float(raw[i])
-                                  : __uint_as_float(i & 1 ? raw[i / 2] & 0xffff0000u : raw[i / 2] << 16);
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < kLane; ++e) {
-      const int c = c0 + column_at<T>(lane, e);
-      x[e] = c < n_cols ? St<T>::ld(row + c) : -INFINITY;
-    }
-  }
-}
+struct Tile {
+  static constexpr int VEC = 16 / sizeof(T);
+  static constexpr uint32_t kNone = sizeof(T) == 2 ? 0xff80u : 0xff800000u;   // -infinity
+  u32x4_t raw[kLane / VEC];
 
-// Largest t such that at least k of the wave's N numbers a lane are >= t, in steps of
-// 2^low (0 if there are fewer than k numbers above 0).
-template <int N, class U>
-__device__ __forceinline__ U kth_largest(const U (&x)[N], int k, int low) {
-  U t = 0;
-#pragma unroll 1
-  for (int bit = 8 * sizeof(U) - 1; bit >= low; --bit) {
-    const U at = t | ((U)1 << bit);
-    int n = 0;
+  static __device__ __forceinline__ int column(int lane, int e) { return (e / VEC) * (64 * VEC) + lane * VEC + e % VEC; }
+  // Columns c0 .. c0 + kTile - 1 of a row that has them.
+  __device__ __forceinline__ void load(const T* row, int c0, int lane) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) n += __popcll(__ballot(x[i] >= at));
-    if (n >= k) t = at;
+    for (int v = 0; v < kLane / VEC; ++v) raw[v] = *reinterpret_cast<const u32x4_any_t*>(row + c0 + (v * 64 + lane) * VEC);
+  }
+  // All columns of a row of less than a tile, -infinity behind them.
+  __device__ __forceinline__ void load_short(const T* row, int n_cols, int lane) {
+#pragma unroll
+    for (int v = 0; v < kLane / VEC; ++v)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        uint32_t word = 0;
+#pragma unroll
+        for (int i = 0; i < VEC / 4; ++i) {
+          const int c = column(lane, v * VEC + w * (VEC / 4) + i);
+          uint32_t x = kNone;
+          if (c < n_cols) x = VEC == 4 ? reinterpret_cast<const uint32_t*>(row)[c] : reinterpret_cast<const uint16_t*>(row)[c];
+          word |= x << (16 * i);
+        }
+        raw[v][w] = word;
+      }
+  }
+  // -infinity in the first n columns.
+  __device__ __forceinline__ void drop(int n, int lane) {
+    const int at = lane * VEC;
+#pragma unroll
+    for (int v = 0; v < kLane / VEC; ++v)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const int c = v * 64 * VEC + w * (VEC / 4);
+        if (VEC == 4) {
+          raw[v][w] = at < n - c ? kNone : raw[v][w];
+        } else {
+          const uint32_t lo = at < n - c ? kNone : raw[v][w] & 0xffffu;
+          raw[v][w] = lo | (at < n - c - 1 ? kNone << 16 : raw[v][w] & 0xffff0000u);
+        }
+      }
+  }
+  // What is computed from the tile behind this is not computed before.
+  __device__ __forceinline__ void here() {
+#pragma unroll
+    for (int v = 0; v < kLane / VEC; ++v) asm volatile("" : "+v"(raw[v]));
+  }
+  __device__ __forceinline__ float operator[](int e) const {
+    const uint32_t w = raw[e / VEC][e % VEC / (VEC / 4)];
+    return __uint_as_float(VEC == 4 ? w : e & 1 ? w & 0xffff0000u : w << 16);
+  }
+};
+
+// Largest t such that at least k of the wave's N numbers a lane are >= t, from bits
+// 2 from + 1 and 2 from down to those of `to`; the bits above are t's.  Two bits a step: a
+// step's length is that of one chain vector compare, count, scalar compare.
+template <int N>
+__device__ __forceinline__ uint32_t kth_largest(uint32_t (&x)[N], int k, uint32_t t, int from, int to) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(x[i]));   // as numbers, not as the conditions they come from
+#pragma unroll 1
+  for (int step = from; step >= to; --step) {
+    const uint32_t one = 1u << (2 * step);
+    int n[3] = {0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int d = 0; d < 3; ++d) n[d] += __popcll(__ballot(x[i] >= t + (d + 1) * one));
+    t += n[2] >= k ? 3 * one : n[1] >= k ? 2 * one : n[0] >= k ? one : 0;
   }
   return t;
 }
 
-// A wave's best columns so far, up to P * 64 of them in LDS, in no order.
-template <int P>
+// The k-th largest of the lanes' numbers, k up to 64, by counting the larger ones (scratch: 64
+// words of LDS): 64 vector compares, where bit by bit costs a round trip to the scalar unit
+// for each (900 cycles to 2,900).
+__device__ __forceinline__ uint32_t kth_lane(uint32_t x, int k, uint32_t* scratch, int lane) {
+  wave_sync();
+  scratch[lane] = x;
+  wave_sync();
+  int ahead = 0;
+#pragma unroll
+  for (int j = 0; j < 64; j += 4) {
+    const u32x4_t y = *reinterpret_cast<const u32x4_t*>(scratch + j);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) ahead += y[i] > x;
+  }
+  wave_sync();
+  // equal numbers have the same count: the largest number with fewer than k ahead and k at least
+  // up to itself is the smallest with fewer than k ahead
+  const u64 in = __ballot(ahead < k);
+  uint32_t least = ahead < k ? x : 0xffffffffu;
+  static_for<6>([&](auto s) { least = min(least, partner<s>(least)); });
+  return in ? __builtin_amdgcn_readfirstlane(least) : 0;
+}
+
+// Lanes before this one with a set bit.
+__device__ __forceinline__ int lanes_before(u64 bits) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(bits >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)bits, 0));
+}
+
+// A wave's best columns so far, up to P * 64 of them in LDS, in no order: the logit's bits
+// over the column's, which few instructions put there; their keys are made when they are read.
+template <class T, int P>
 struct Pool {
   static constexpr int CAP = P * 64;
-  u64* key;
+  u64* at;
   int n;
-  u64 least;   // columns at or below it are not among the wave's k best
+  u64 least;    // columns at or below it are not among the wave's k best
+  float bound;  // columns of the tiles to come are above it, or not above `least`
 
-  // Keeps the k best.
-  __device__ __forceinline__ void cut(int k, int lane) {
-    u64 x[P];
+  static __device__ __forceinline__ u64 key_of(u64 x) {
+    return (u64)order_of<T>(__uint_as_float((uint32_t)(x >> 32))) << 32 | (0xffffffffu - (uint32_t)x);
+  }
+  // Keeps the k best; high: no column lies above it.
+  __device__ __forceinline__ void cut(int k, uint32_t high, int lane) {
+    u64 own[P], x[P];
     uint32_t hi[P];
     wave_sync();
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      x[i] = i * 64 + lane < n ? key[i * 64 + lane] : 0;
+      own[i] = at[i * 64 + lane];
+      x[i] = i * 64 + lane < n ? key_of(own[i]) : 0;
       hi[i] = (uint32_t)(x[i] >> 32);
     }
-    const uint32_t t = kth_largest<P>(hi, k, 0);
+    // the bits that the bounds have in common are the k-th's, too
+    const uint32_t differ = (uint32_t)(least >> 32) ^ high;
+    const int from = differ ? (31 - __builtin_clz(differ)) / 2 : -1;
+    const uint32_t t = kth_largest<P>(hi, k, from == 15 ? 0u : high >> (2 * from + 2) << (2 * from + 2), from, 0);
     int above = 0, level = 0;
 #pragma unroll
     for (int i = 0; i < P; ++i) {
       above += __popcll(__ballot(hi[i] > t));
       level += __popcll(__ballot(hi[i] == t));
     }
-    u64 from = (u64)t << 32;
+    u64 first = (u64)t << 32;
     if (above + level > k) {                    // equal logits: the lowest columns
       uint32_t lo[P];
 #pragma unroll
       for (int i = 0; i < P; ++i) lo[i] = hi[i] == t ? (uint32_t)x[i] : 0;
-      from |= kth_largest<P>(lo, k - above, 0);
+      first |= kth_largest<P>(lo, k - above, 0u, 15, 0);
     }
     wave_sync();
     n = 0;
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      const u64 in = __ballot(x[i] >= from && x[i]);
-      if (x[i] >= from && x[i]) key[n + __popcll(in & ((1ull << lane) - 1))] = x[i];
-      n += __popcll(in);
+      const bool in = x[i] >= first && x[i];
+      const u64 all = __ballot(in);
+      if (in) at[n + lanes_before(all)] = own[i];
+      n += __popcll(all);
     }
-    least = from - 1;
+    n = min(n, k);                              // rows with NaN: any k
+    least = max(least, first - 1);
+    bound = logit_of<T>(t);                     // an equal logit further on has a higher column
+    wave_sync();
   }
 
-  // Takes in a tile's columns; k and 64 more have room.
-  template <class T>
-  __device__ __forceinline__ void add(const float (&x)[kLane], int c0, int k, int lane) {
-    uint32_t todo = 0;
+  // Takes in a tile's columns above the bound (c: the lane's first one); k and 64 more have room.
+  __device__ __forceinline__ void add(Tile<T> x, int c, int k, uint32_t high, int lane) {
+    u64 in[kLane];
+    int all = 0;
 #pragma unroll
-    for (int e = 0; e < kLane; ++e)
-      if (x[e] > -INFINITY && order_of(x[e]) >= (uint32_t)(least >> 32)) todo |= 1u << e;
-    while (__any(todo)) {
-      bool full = false;
+    for (int e = 0; e < kLane; ++e) {
+      in[e] = __ballot(x[e] > bound);
+      all += __popcll(in[e]);
+    }
+    if (n + all <= CAP) {
 #pragma unroll
       for (int e = 0; e < kLane; ++e) {
-        const u64 mine = column_key(order_of(x[e]), c0 + column_at<T>(lane, e));
-        const bool is = (todo >> e & 1) && mine > least;
-        const u64 in = __ballot(is);
-        full = full || n + __popcll(in) > CAP;
-        if (full || !in) continue;
-        if (is) key[n + __popcll(in & ((1ull << lane) - 1))] = mine;
-        n += __popcll(in);
-        todo &= ~(1u << e);
+        if (!in[e]) continue;
+        if (in[e] >> lane & 1)
+          at[n + lanes_before(in[e])] = (u64)__float_as_uint(x[e]) << 32 | (uint32_t)(c + Tile<T>::column(0, e));
+        n += __popcll(in[e]);
       }
-      if (!full) break;
-      cut(k, lane);
+      return;
+    }
+    // more than there is room for: 64 at a time, each against the bound that the last cut left
+    for (int e = 0; e < kLane; ++e) {
+      if (n + 64 > CAP) cut(k, high, lane);
+      x.here();
+      float z = -INFINITY;
+      int col = 0;
+#pragma unroll
+      for (int i = 0; i < kLane; ++i)
+        if (e == i) {
+          z = x[i];
+          col = c + Tile<T>::column(0, i);
+        }
+      const u64 is = (u64)__float_as_uint(z) << 32 | (uint32_t)col;
+      const bool mine = z > -INFINITY && key_of(is) > least;
+      const u64 lanes = __ballot(mine);
+      if (mine) at[n + lanes_before(lanes)] = is;
+      n += __popcll(lanes);
     }
   }
 };
+
+// sum += e^(x(e) - top) over a lane's columns, four chains at a time.
+template <class F>
+__device__ __forceinline__ void add_exps(double& sum, float top, F x) {
+#pragma unroll
+  for (int e = 0; e < kLane; e += 4) {
+    double d[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) d[i] = (double)x(e + i) - (double)top;
+    exp_64(d);
+    sum += (d[0] + d[1]) + (d[2] + d[3]);
+  }
+}
 
 struct BeamArgs {
   atspeed_beam_select_args a;
   u64* list;        // [n_rows, parts, k] the best columns, best first
   double2* stat;    // [n_rows, parts] largest logit and sum of exponentials; NaN: the row has no candidates
   int* len;         // [n_rows, parts]
-  int parts, tiles; // parts of a row, tiles of a part
+  int parts, tiles, shift; // parts of a row, tiles of a part; parts <= 1 << shift
 };
 
-// Sorts key[0 .. n) with the payloads after it, n a power of two, largest key first, equal
-// ones by the lower payload, by the whole workgroup.
-template <bool PAY>
-__device__ __forceinline__ void sort_desc(u64* key, u64* pay, int n) {
-  for (int size = 2; size <= n; size <<= 1)
-    for (int step = size >> 1; step; step >>= 1) {
-      __syncthreads();
-      for (int i = threadIdx.x; i < n / 2; i += kBeamThreads) {
-        const int a = 2 * i - (i & (step - 1)), b = a + step;
-        const u64 x = key[a], y = key[b];
-        const bool ahead = x > y || (PAY && x == y && pay[a] < pay[b]);
-        if (ahead == ((a & size) != 0) && (x != y || PAY)) {
-          key[a] = y;
-          key[b] = x;
-          if (PAY) {
-            const u64 p = pay[a];
-            pay[a] = pay[b];
-            pay[b] = p;
-          }
-        }
-      }
-    }
-  __syncthreads();
-}
-
+// A wave takes a part of a row by itself, tile by tile: the running maximum and 64-bit sum
+// of its exponentials, and its k best columns behind a bound that rises with them.
 template <class T, int P, bool PROBS>
 __global__ void __launch_bounds__(kBeamThreads) beam_rows_kernel(BeamArgs p) {
-  extern __shared__ u64 smem[];
-  __shared__ float s_top[kBeamWaves];
-  __shared__ double s_sum[kBeamWaves];
-  __shared__ int s_n[kBeamWaves];
+  __shared__ u64 keys[kBeamWaves * P * 64];
   const atspeed_beam_select_args& a = p.a;
-  const int r = blockIdx.x / p.parts, part = blockIdx.x % p.parts, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if (r >= a.row_off[a.B] || (a.done && a.done[r])) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int q = blockIdx.x * kBeamWaves + wave, r = q / p.parts, part = q % p.parts;
+  if (r >= a.n_rows) return;
   const int k = a.k, n_cols = a.n_cols;
   const T* row = static_cast<const T*>(a.logits) + (int64_t)r * a.logits_stride;
-  Pool<P> pool{smem + wave * Pool<P>::CAP, 0, 0};
+  const uint32_t lowest = order_of<T>(-INFINITY);
+  Pool<T, P> pool{keys + wave * P * 64, 0, (u64)lowest << 32 | 0xffffffffu, -INFINITY};
   float top = -INFINITY;
   double sum = 0.0;
-  bool bad = false;
+  uint32_t high = 0;
 
-  const int end = min((part + 1) * p.tiles, (n_cols + kTile - 1) / kTile);
-  for (int tile = part * p.tiles + wave; tile < end; tile += kBeamWaves) {
-    const int c0 = tile * kTile;
-    float x[kLane], most[4];
-    load_tile(row, c0, n_cols, lane, x);
+  const int begin = part * p.tiles, end = min(begin + p.tiles, (n_cols + kTile - 1) / kTile);
+  // the last tile of a row ends with it and drops what the one before had
+  const int last = n_cols - kTile;
+  Tile<T> x, next;
+  if (last < 0) next.load_short(row, n_cols, lane);
+  else next.load(row, min(begin * kTile, last), lane);
+  if (r >= a.row_off[a.B] || (a.done && a.done[r])) return;
+  for (int tile = begin; tile < end; ++tile) {
+    const int c0 = last < 0 ? 0 : min(tile * kTile, last);
+    x = next;
+    if (tile + 1 < end) next.load(row, min(c0 + kTile, last), lane);
+    if (c0 != tile * kTile) x.drop(tile * kTile - c0, lane);
+    float most[4];
 #pragma unroll
-    for (int g = 0; g < 4; ++g)
-      most[g] = max_nan(max_nan(x[4 * g], x[4 * g + 1]), max_nan(x[4 * g + 2], x[4 * g + 3]));
+    for (int g = 0; g < 4; ++g) most[g] = max_nan(max_nan(x[4 * g], x[4 * g + 1]), max_nan(x[4 * g + 2], x[4 * g + 3]));
     const float mine = max_nan(max_nan(most[0], most[1]), max_nan(most[2], most[3]));
-    if (PROBS) {
-      bad |= !(mine < INFINITY);
-    } else {
-      if (__any(!(mine <= top))) {
-        const float now = wave_max_nan(max_nan(mine, top));
-        if (top > -INFINITY) sum *= exp_below(top, now);
-        top = now;
-      }
-      if (top > -INFINITY) {
-        const float least = top + kLeast;             // below it nothing is left of the exponential
+    if (__any(!(mine <= top))) {
+      const float now = wave_max_nan(max_nan(mine, top));
+      if (!PROBS && top > -INFINITY) sum *= exp_below(top, now);
+      top = now;
+      high = __builtin_amdgcn_readfirstlane(order_of<T>(top));
+    }
+    x.here();
+    if (!PROBS && top > -INFINITY) {
+      // the exponential wants finite differences: where there are others, they are held at what
+      // leaves nothing
+      float few = INFINITY;
 #pragma unroll
-        for (int e = 0; e < kLane; ++e) sum += exp_64((double)fmaxf(x[e], least) - (double)top);
+      for (int e = 0; e < kLane; ++e) few = fminf(few, x[e]);
+      if (__any(!(few >= top - 1e6f))) {
+        const float least = top + kLeast;
+        add_exps(sum, top, [&](int e) { return max_nan(x[e], least); });
+      } else {
+        add_exps(sum, top, [&](int e) { return x[e]; });
       }
     }
-    // the first tile: fewer than k of its columns lie above this bound, of 256 groups' largest
-    if (tile == part * p.tiles + wave) {
-      uint32_t o[4];
+    if (tile == begin) {
+      // At least k columns are at or above the k-th of the lanes' largest, or of the largest of
+      // four groups a lane; of the latter, found bit by bit, the upper 16 bits.
+      uint32_t t;
+      if (k <= 32) {
+        t = kth_lane(order_of<T>(mine), k, reinterpret_cast<uint32_t*>(pool.at), lane);
+      } else {
+        uint32_t o[4];
 #pragma unroll
-      for (int g = 0; g < 4; ++g) o[g] = most[g] > -INFINITY ? order_of(most[g]) : 0;
-      const uint32_t t = kth_largest<4>(o, k, 16);
-      pool.least = t ? ((u64)t << 32) - 1 : 0;
+        for (int g = 0; g < 4; ++g) o[g] = order_of<T>(most[g]);
+        constexpr int STEPS = 4 * sizeof(T);
+        t = kth_largest<4>(o, k, 0u, STEPS - 1, STEPS - 8);
+      }
+      if (t > lowest + 1) {
+        pool.least = ((u64)t << 32) - 1;
+        pool.bound = logit_of<T>(t - (t == order_of<T>(0.f) ? 2 : 1));   // -0 is no number of its own
+      }
     }
-    if (__any(mine > -INFINITY && order_of(mine) >= (uint32_t)(pool.least >> 32))) pool.template add<T>(x, c0, k, lane);
+    if (__any(mine > pool.bound)) pool.add(x, c0 + Tile<T>::column(lane, 0), k, high, lane);
   }
-  if (pool.n > k) pool.cut(k, lane);
+  if (P > 2 && pool.n > k) pool.cut(k, high, lane);
+  sum = wave_sum(sum);
+  // in order: a column's place is the number of better ones
+  wave_sync();
+  const int n = pool.n, n8 = (n + 7) & ~7;
+  u64 own[P];
+  int place[P];
 #pragma unroll
-  for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
-  if (PROBS) {
-    top = 0.f;
-    sum = __any(bad) ? NAN : 1.0;
+  for (int i = 0; i < P; ++i) {
+    own[i] = i * 64 + lane < n ? pool.key_of(pool.at[i * 64 + lane]) : 0;
+    place[i] = 0;
+    pool.at[i * 64 + lane] = own[i];
   }
+  wave_sync();
+  for (int j = 0; j < n8; j += 8) {
+    u64 other[8];
+#pragma unroll
+    for (int o = 0; o < 8; ++o) other[o] = pool.at[j + o];
+#pragma unroll
+    for (int o = 0; o < 8; ++o)
+#pragma unroll
+      for (int i = 0; i < P; ++i) place[i] += other[o] > own[i];
+  }
+#pragma unroll
+  for (int i = 0; i < P; ++i)
+    if (i * 64 + lane < n && place[i] < k) p.list[(int64_t)q * k + place[i]] = own[i];
   if (lane == 0) {
-    s_top[wave] = top;
-    s_sum[wave] = sum;
-    s_n[wave] = pool.n;
+    p.stat[q] = {(double)top, top < INFINITY ? sum : NAN};
+    p.len[q] = min(n, k);
   }
-  __syncthreads();
-
-  // the part's statistics, and its k best in order
-  if (threadIdx.x == 0) {
-    float all = s_top[0];
-    for (int w = 1; w < kBeamWaves; ++w) all = max_nan(all, s_top[w]);
-    double total = 0.0;
-    for (int w = 0; w < kBeamWaves; ++w)
-      if (s_top[w] > -INFINITY || PROBS) total += s_sum[w] * exp_below(s_top[w], all);
-    p.stat[blockIdx.x] = {(double)all, all < INFINITY ? total : NAN};
-  }
-  u64* sorted = smem + kBeamWaves * Pool<P>::CAP;
-  int n = 0, size = 64;
-#pragma unroll
-  for (int w = 0; w < kBeamWaves; ++w) {
-    if (w == wave)
-      for (int i = lane; i < s_n[w]; i += 64) sorted[n + i] = pool.key[i];
-    n += s_n[w];
-  }
-  while (size < n) size <<= 1;
-  for (int i = n + threadIdx.x; i < size; i += kBeamThreads) sorted[i] = 0;
-  sort_desc<false>(sorted, nullptr, size);
-  n = min(n, k);
-  for (int i = threadIdx.x; i < n; i += kBeamThreads) p.list[(int64_t)blockIdx.x * k + i] = sorted[i];
-  if (threadIdx.x == 0) p.len[blockIdx.x] = n;
 }
 
 // ---------------------------------------------------------------- ranking a request's lists
-// A workgroup a request.  Rounds: every list whose next entry may still count gives a few,
-// all that came are sorted, the k best stay, and the k-th is the bound of the next round.
-// Entries are taken best first, so a list is left at its first one below the bound.
-constexpr int kJoinPool = 2048, kJoinLists = 1024;
+// A workgroup a request.  Rounds: every list that may still count gives its next few
+// entries, as many as the workgroup holds; the k-th of the threads' largest is a bound that
+// few more than k of them pass; these are ranked, the k best stay.  A list is left once its
+// last entry is behind them.  Mostly one round or two.
+constexpr int kEach = 4, kJoinLists = 1024;
+constexpr short kItself = -1;              // length of the list of a row that has ended
 
-__global__ void __launch_bounds__(kBeamThreads) beam_join_kernel(BeamArgs p) {
-  __shared__ u64 key[kJoinPool], pay[kJoinPool];   // the score's order; row << 32 | column + 1
-  __shared__ double base[kJoinLists];              // of a row: score - log sum
-  __shared__ short at[kJoinLists], len[kJoinLists];
-  __shared__ int s_n, s_more;
+struct alignas(16) Entry {
+  u64 key;   // the score's order; 0: none
+  u64 who;   // row << 32 | column + 1
+};
+__device__ __forceinline__ bool ahead_of(u64 key, u64 who, u64 than_key, u64 than_who) {
+  return (key > than_key) | ((key == than_key) & (who < than_who));
+}
+
+constexpr int kBins = 256;
+// The bin of a distance: its exponent and two bits of it, from 2^-24 to 2^40.
+__device__ __forceinline__ uint32_t bin_of(double d) {
+  const int b = (int)(__float_as_uint((float)d) >> 21) - ((127 - 24) << 2);
+  return (uint32_t)min(max(b, 0), kBins - 1);
+}
+
+template <class T, int THREADS>
+__global__ void __launch_bounds__(THREADS) beam_join_kernel(BeamArgs p) {
+  constexpr int WAVES = THREADS / 64, ROUND = THREADS * kEach, POOL = 2 * ROUND;   // a power of two
+  extern __shared__ Entry entry[];                 // [POOL]
+  double* const base = (double*)(entry + POOL);    // [kJoinLists] of a row: score - log sum
+  unsigned short* const open = (unsigned short*)(base + kJoinLists);   // [kJoinLists]
+  short* const at = (short*)(open + kJoinLists);   // [kJoinLists]
+  short* const len = at + kJoinLists;              // [kJoinLists]
+  __shared__ Entry best[kMaxBeams];
+  __shared__ u64 most[WAVES];
+  __shared__ int bin[kBins], rank[THREADS], s_n, s_open[2];
   const atspeed_beam_select_args& a = p.a;
-  const int b = blockIdx.x, tid = threadIdx.x, k = a.k, parts = p.parts;
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, k = a.k, parts = p.parts, shift = p.shift;
   const int r1 = min(min(a.row_off[b + 1], a.row_off[a.B]), a.n_rows);   // rows that the first kernel read
-  int r0 = max(a.row_off[b], 0);
-  const int group = max(1, kJoinLists / parts);
-  int n = 0;
-  for (; r0 < r1; r0 += group) {
-    const int rows = min(group, r1 - r0), lists = rows * parts;
+  const int group = kJoinLists >> shift;           // lists: row << shift | part
+  int n = 0;                                       // best[0 .. n) are the best so far, in order
+  if (tid < 2) s_open[tid] = 0;
+  for (int r0 = max(a.row_off[b], 0); r0 < r1; r0 += group) {
+    const int rows = min(group, r1 - r0), lists = rows << shift;
     __syncthreads();
-    for (int i = tid; i < rows; i += kBeamThreads) {
-      const int r = r0 + i;
+    // a group of lanes a row, a lane a part
+    const int wide = min(shift, 6), lanes = 1 << wide;
+    for (int i0 = 0; i0 < rows; i0 += THREADS >> wide) {
+      const int i = i0 + (tid >> wide), r = min(r0 + i, r1 - 1), l = tid & (lanes - 1);
       const double score = a.score ? (double)a.score[r] : 0.0;
-      double x = score;
-      bool none = !(fabs(score) < INFINITY);
-      if (!(a.done && a.done[r])) {
-        const double2* st = p.stat + (int64_t)r * parts;
-        double all = -INFINITY, total = 0.0;
-        for (int q = 0; q < parts; ++q)
-          if (st[q].x > all) all = st[q].x;
-        for (int q = 0; q < parts; ++q) {
-          // a part whose largest logit is -infinity has sum 0; NaN stays
-          if (st[q].x > -INFINITY) total += st[q].y * exp_below(st[q].x, all);
-          else if (!(st[q].x == -INFINITY)) total = NAN;
-        }
-        if (a.log_probs) {
-          if (!(total == total)) none = true;
-        } else {
-          x = score - (all + log(total));
-          if (!(fabs(x) < INFINITY)) none = true;
-        }
-      }
-      base[i] = none ? NAN : x;
-    }
-    __syncthreads();
-    for (int l = tid; l < lists; l += kBeamThreads) {
-      const int i = l / parts, r = r0 + i;
       const bool ended = a.done && a.done[r];
-      at[l] = 0;
-      len[l] = !(base[i] == base[i]) ? 0 : ended ? l % parts == 0 : p.len[(int64_t)r * parts + l % parts];
-    }
-    for (;;) {
-      __syncthreads();
-      if (tid == 0) {
-        s_n = n;
-        s_more = 0;
-      }
-      __syncthreads();
-      const u64 low_key = n == k ? key[k - 1] : 0, low_pay = n == k ? pay[k - 1] : 0;
-      const int quota = max(1, min((2 * k + lists - 1) / lists, (kJoinPool - k) / lists));
-      __syncthreads();
-      for (int l = tid; l < lists; l += kBeamThreads) {
-        const int i = l / parts, r = r0 + i;
-        const bool ended = a.done && a.done[r];
-        int j = at[l], stop = min((int)len[l], j + quota);
-        for (; j < stop; ++j) {
-          const u64 c = ended ? 0 : p.list[((int64_t)r * parts + l % parts) * k + j];
-          const u64 score = order64(ended ? base[i] : base[i] + (double)logit_of((uint32_t)(c >> 32)));
-          const u64 who = ((u64)r << 32) | (unsigned)(ended ? 0 : column_of(c) + 1);
-          if (n == k && !(score > low_key || (score == low_key && who < low_pay))) {
-            len[l] = 0;
-            break;
-          }
-          const int to = atomicAdd(&s_n, 1);
-          key[to] = score;
-          pay[to] = who;
+      double all = -INFINITY, total = 0.0;
+      for (int q = l; q < 1 << shift; q += lanes) {
+        const bool in = q < parts && !ended;
+        const double2 st = in ? p.stat[(int64_t)r * parts + q] : double2{-INFINITY, 0.0};
+        if (i < rows) {
+          at[i << shift | q] = 0;
+          len[i << shift | q] = in ? (short)p.len[(int64_t)r * parts + q] : ended && q == 0 ? kItself : 0;
         }
-        at[l] = j;
-        if (j < len[l]) s_more = 1;
+        // NaN stays; a part whose largest logit is -infinity has nothing to add
+        const double now = st.x > all ? st.x : all;
+        const double add = st.x > -INFINITY ? a.log_probs ? st.y : st.y * exp_below(st.x, now) : st.x == -INFINITY ? 0.0 : NAN;
+        total = (all > -INFINITY ? total * exp_below(all, now) : total) + add;
+        all = now;
       }
+      for (int o = 1; o < lanes; o <<= 1) {
+        const double x = __shfl_xor(all, o), y = __shfl_xor(total, o), now = fmax(all, x);
+        if (now > -INFINITY) total = total * exp_below(all, now) + y * exp_below(x, now);
+        else total += y;
+        all = now;
+      }
+      bool none = !(fabs(score) < INFINITY) || !(total == total);
+      double x = score;
+      if (!ended && !a.log_probs) {
+        x = score - (all + log(total));
+        none = none || !(fabs(x) < INFINITY);
+      }
+      if (i < rows && l == 0) base[i] = x;
+      if (i < rows && none)
+        for (int q = l; q < 1 << shift; q += lanes) len[i << shift | q] = 0;
+    }
+    for (int round = 0;; round ^= 1) {
+      // the lists that are left
+      __syncthreads();
+      for (int l0 = 0; l0 < lists; l0 += THREADS) {
+        const int l = l0 + tid, length = l < lists ? len[l] : 0;
+        const bool is = l < lists && at[l] < (length == kItself ? 1 : length);
+        const u64 all = __ballot(is);
+        int to = 0;
+        if (lane == 0 && all) to = atomicAdd(&s_open[round], __popcll(all));
+        to = __builtin_amdgcn_readfirstlane(to) + lanes_before(all);
+        if (is) open[to] = (unsigned short)l;
+      }
+      if (tid == 0) s_n = 0;
+      __syncthreads();
+      const int n_open = s_open[round];
+      if (tid == 0) s_open[round ^ 1] = 0;
+      if (!n_open) break;
+      // a power of two of each, k at most
+      int depth = 31 - __builtin_clz((unsigned)(ROUND / n_open));
+      while (depth > 0 && 1 << (depth - 1) >= k) --depth;
+
+      // a thread's entries, and its place among the best so far
+      u64 mine[kEach + 1], who[kEach + 1], largest = 0;
+      int from[kEach], next[kEach];                // next: where its list goes on, -1: it ends here, 0: not the last one taken
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const int e = tid + i * THREADS, o = e >> depth;
+        mine[i] = who[i] = 0;
+        from[i] = -1;
+        if (o >= n_open) continue;
+        const int l = open[o], d = e & ((1 << depth) - 1), j = at[l] + d, length = len[l], i_row = l >> shift, r = r0 + i_row;
+        if (j >= (length == kItself ? 1 : length)) continue;
+        from[i] = l;
+        next[i] = j + 1 >= length ? -1 : d + 1 == 1 << depth ? j + 1 : 0;
+        if (length == kItself) {
+          mine[i] = order64(base[i_row]);
+          who[i] = (u64)r << 32;
+        } else {
+          const u64 c = p.list[((int64_t)r * parts + (l & ((1 << shift) - 1))) * k + j];
+          mine[i] = order64(base[i_row] + (double)logit_of<T>((uint32_t)(c >> 32)));
+          who[i] = ((u64)r << 32) | (unsigned)(column_of(c) + 1);
+        }
+        largest = max(largest, mine[i]);
+      }
+      mine[kEach] = tid < n ? best[tid].key : 0;
+      who[kEach] = tid < n ? best[tid].who : 0;
+      largest = max(largest, mine[kEach]);
+      // Few entries are all ranked.  Of many, those that are at or above the k-th of the threads'
+      // largest, in bins of a quarter of their distance to the best of all.
+      uint32_t limit = kBins;
+      double top = 0.0;
+      if (n_open << depth > THREADS) {
+        u64 high = largest;
+        static_for<6>([&](auto s) { high = max(high, (u64)partner<s>((uint32_t)(high >> 32)) << 32 | partner<s>((uint32_t)high)); });
+        if (lane == 0) most[wave] = high;
+        if (tid < kBins) bin[tid] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) high = max(high, most[w]);
+        top = score_of(high);
+        if (largest) atomicAdd(&bin[bin_of(top - score_of(largest))], 1);
+        __syncthreads();
+        // a lane has four bins: how many there are up to each
+        int upto[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) upto[i] = bin[lane * 4 + i] + (i ? upto[i - 1] : 0);
+        const int before = wave_scan(upto[3]) - upto[3];
+        int mine_limit = kBins;
+#pragma unroll
+        for (int i = 3; i >= 0; --i)
+          if (before + upto[i] >= k) mine_limit = lane * 4 + i;
+        const u64 enough = __ballot(mine_limit < kBins);
+        if (enough) limit = __builtin_amdgcn_readlane(mine_limit, __builtin_ctzll(enough));
+      } else {
+        __syncthreads();
+      }
+#pragma unroll
+      for (int i = 0; i <= kEach; ++i)
+        if (mine[i] && (limit == kBins || bin_of(top - score_of(mine[i])) <= limit)) entry[atomicAdd(&s_n, 1)] = {mine[i], who[i]};
+      rank[tid] = 0;
       __syncthreads();
       const int came = s_n;
-      const bool more = s_more;
-      if (came > n) {
-        int size = 64;
-        while (size < came) size <<= 1;
-        for (int i = came + tid; i < size; i += kBeamThreads) key[i] = 0, pay[i] = ~0ull;
-        sort_desc<true>(key, pay, size);
-        n = min(came, k);
+      int size = 64;
+      while (size < came) size <<= 1;
+      if (size <= THREADS) {
+        // a place is the number of better ones, counted by THREADS / size threads each
+        const int slices = THREADS / size, per = ((came + slices - 1) / slices + 7) & ~7;
+        const int e = tid & (size - 1), j0 = tid / size * per, j1 = min(came, j0 + per);
+        if (e < came && j0 < j1) {
+          const Entry x = entry[e];
+          int before = 0;
+          for (int j = j0; j < j1; j += 8) {
+            Entry y[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = entry[min(j + i, came - 1)];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) before += j + i < j1 && ahead_of(y[i].key, y[i].who, x.key, x.who);
+          }
+          if (before) atomicAdd(&rank[e], before);
+        }
+        __syncthreads();
+        if (tid < came && rank[tid] < k) best[rank[tid]] = entry[tid];
+      } else {
+        for (int i = came + tid; i < size; i += THREADS) entry[i] = {0, ~0ull};
+        for (int sorted = 2; sorted <= size; sorted <<= 1)
+          for (int step = sorted >> 1; step; step >>= 1) {
+            __syncthreads();
+            for (int i = tid; i < size / 2; i += THREADS) {
+              const int x = 2 * i - (i & (step - 1)), y = x + step;
+              const Entry ex = entry[x], ey = entry[y];
+              if (ahead_of(ex.key, ex.who, ey.key, ey.who) == ((x & sorted) != 0)) {
+                entry[x] = ey;
+                entry[y] = ex;
+              }
+            }
+          }
+        __syncthreads();
+        if (tid < min(came, k)) best[tid] = entry[tid];
       }
-      if (!more) break;
+      n = min(came, k);
+      __syncthreads();
+      // lists at their end or behind the k-th are done
+      const Entry worst = n == k ? best[k - 1] : Entry{0, ~0ull};
+#pragma unroll
+      for (int i = 0; i < kEach; ++i)
+        if (from[i] >= 0 && next[i]) {
+          if (next[i] < 0 || ahead_of(worst.key, worst.who, mine[i], who[i])) len[from[i]] = 0;
+          else at[from[i]] = (short)next[i];
+        }
     }
   }
   __syncthreads();
 
   if (tid == 0) a.count[b] = n;
-  for (int i = tid; i < k; i += kBeamThreads) {
+  for (int i = tid; i < k; i += THREADS) {
     const int64_t o = (int64_t)b * k + i;
-    const int r = i < n ? (int)(pay[i] >> 32) : -1, col = i < n ? (int)(unsigned)pay[i] - 1 : -1;
-    const u64 u = i < n ? key[i] : 0;
+    const int r = i < n ? (int)(best[i].who >> 32) : -1, col = i < n ? (int)(unsigned)best[i].who - 1 : -1;
     a.parent[o] = r < 0 ? -1 : a.row_id ? a.row_id[r] : r;
     a.token[o] = col < 0 ? -1 : a.token_base + col;
-    a.score_out[o] = r < 0 ? -INFINITY : (float)__longlong_as_double((long long)(u >> 63 ? u ^ (1ull << 63) : ~u));
+    a.score_out[o] = r < 0 ? -INFINITY : (float)score_of(best[i].key);
   }
   if (!a.paths) return;
-  for (int i = tid; i < k * a.max_path; i += kBeamThreads) {
+  for (int i = tid; i < k * a.max_path; i += THREADS) {
     const int j = i / a.max_path, s = i % a.max_path;
     int v = -1;
     if (j < n) {
-      const int r = (int)(pay[j] >> 32), col = (int)(unsigned)pay[j] - 1, id = a.row_id ? a.row_id[r] : r;
+      const int r = (int)(best[j].who >> 32), col = (int)(unsigned)best[j].who - 1, id = a.row_id ? a.row_id[r] : r;
       const bool known = (unsigned)id < (unsigned)a.n_paths;
       const int held = known ? min(max(a.path_len[id], 0), a.max_path) : 0;
       if (s < held) v = a.paths[(int64_t)id * a.max_path + s];
@@ -421,6 +677,22 @@ __global__ void __launch_bounds__(kBeamThreads) beam_join_kernel(BeamArgs p) {
     }
     a.paths_out[((int64_t)b * k + j) * a.max_path + s] = v;
   }
+}
+
+template <class T, int THREADS>
+static atspeed_status launch_join(const BeamArgs& p, hipStream_t st) {
+  constexpr int lds = 2 * THREADS * kEach * 16 + kJoinLists * 14;
+  if (lds > (64 << 10))
+    HIP_TRY(hipFuncSetAttribute((const void*)beam_join_kernel<T, THREADS>, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+  hipLaunchKernelGGL((beam_join_kernel<T, THREADS>), dim3(p.a.B), dim3(THREADS), lds, st, p);
+  HIP_TRY(hipGetLastError());
+  return ATSPEED_OK;
+}
+template <class T>
+static atspeed_status run_join(const BeamArgs& p, hipStream_t st) {
+  // few entries a request or many requests: smaller workgroups, more of them on a CU
+  const long long entries = (long long)p.a.n_rows * p.parts * p.a.k;
+  return p.a.B > 256 || entries <= 1024LL * p.a.B ? launch_join<T, 256>(p, st) : launch_join<T, 1024>(p, st);
 }
 
 static atspeed_status check_beam(const atspeed_beam_select_args& a) {
@@ -448,12 +720,13 @@ static atspeed_status check_beam(const atspeed_beam_select_args& a) {
   return ATSPEED_OK;
 }
 
-// Parts of a row: enough workgroups for the card, of four tiles (one a wave) at least.
+// Parts of a row: a wave each, enough waves for the card.
 static void cut_rows(const atspeed_beam_select_args& a, BeamArgs& p) {
   const int tiles = (a.n_cols + kTile - 1) / kTile, rows = std::max(a.n_rows, 1);
-  const int most = std::max(1, tiles / kBeamWaves), want = (1024 + rows - 1) / rows;
-  p.tiles = (tiles + std::min(most, want) - 1) / std::min(most, want);
+  const int most = std::min(tiles, kJoinLists), want = std::min(most, (4096 + rows - 1) / rows);
+  p.tiles = (tiles + want - 1) / want;
   p.parts = (tiles + p.tiles - 1) / p.tiles;
+  while (1 << p.shift < p.parts) ++p.shift;
 }
 
 static size_t lay_out(BeamArgs& p, char* base) {
@@ -472,13 +745,10 @@ static size_t lay_out(BeamArgs& p, char* base) {
 
 template <class T, int P>
 static void launch_rows(const BeamArgs& p, unsigned grid, hipStream_t st) {
-  int sorted = 64;
-  while (sorted < kBeamWaves * p.a.k) sorted <<= 1;
-  const size_t lds = ((size_t)kBeamWaves * Pool<P>::CAP + sorted) * 8;
   if (p.a.log_probs)
-    hipLaunchKernelGGL((beam_rows_kernel<T, P, true>), dim3(grid), dim3(kBeamThreads), lds, st, p);
+    hipLaunchKernelGGL((beam_rows_kernel<T, P, true>), dim3(grid), dim3(kBeamThreads), 0, st, p);
   else
-    hipLaunchKernelGGL((beam_rows_kernel<T, P, false>), dim3(grid), dim3(kBeamThreads), lds, st, p);
+    hipLaunchKernelGGL((beam_rows_kernel<T, P, false>), dim3(grid), dim3(kBeamThreads), 0, st, p);
 }
 // A pool holds k columns and 64 more at least.
 template <class T>
@@ -510,7 +780,7 @@ atspeed_status atspeed_beam_select(const atspeed_beam_select_args* args, void* w
   BeamArgs p{};
   p.a = *args;
   cut_rows(*args, p);
-  const long long groups = (long long)args->n_rows * p.parts;
+  const long long groups = ((long long)args->n_rows * p.parts + kBeamWaves - 1) / kBeamWaves;
   if (groups > kMaxGroups) return fail(ATSPEED_E_SHAPE, "beam select: too many rows x columns");
   const size_t need = lay_out(p, nullptr);
   if (!workspace || !aligned16(workspace) || ws_bytes < need)
@@ -522,9 +792,7 @@ atspeed_status atspeed_beam_select(const atspeed_beam_select_args* args, void* w
     else launch_pool<float>(p, (unsigned)groups, st);
     HIP_TRY(hipGetLastError());
   }
-  hipLaunchKernelGGL(beam_join_kernel, dim3(args->B), dim3(kBeamThreads), 0, st, p);
-  HIP_TRY(hipGetLastError());
-  return ATSPEED_OK;
+  return args->dtype == ATSPEED_BF16 ? run_join<bf16_t>(p, st) : run_join<float>(p, st);
 }
 
 }  // extern "C"

@@ -65,8 +65,8 @@ def check(c, got=None):
     score, w = got.score.double().cpu().numpy(), np.array(want["score"])
     live = np.isfinite(w)
     assert (np.isneginf(score) == ~live).all()
-    # one rounding to fp32, and 64-bit sums whose exponentials are off by 1.1e-12
-    assert (np.abs(score[live] - w[live]) <= 2.0 ** -24 * np.abs(w[live]) + 4e-12).all()
+    # one rounding to fp32, and the logarithm of a sum of exponentials that are off by 2.4e-10 each
+    assert (np.abs(score[live] - w[live]) <= 2.0 ** -24 * np.abs(w[live]) + 2.5e-10).all()
     return got
 
 
