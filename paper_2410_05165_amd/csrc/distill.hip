@@ -14,12 +14,10 @@
 
 #include "common.h"
 #include "paged.h"
+#include "wave.h"
 
 namespace atspeed {
 
-typedef u32x4_t u32x4_any_t __attribute__((aligned(2)));   // 16 bytes at any element
-
-constexpr int kDistThreads = 256;
 constexpr int kMaxTops = 256;
 constexpr float kNoTop = -0.f;   // in the place of a top's gradient, which is never -0: no top
 
@@ -31,145 +29,173 @@ __device__ __forceinline__ void unpack(const u32x4_t raw, float (&x)[16 / sizeof
     x[i] = VEC == 4 ? __uint_as_float(raw[i]) : __uint_as_float(i & 1 ? raw[i / 2] & 0xffff0000u : raw[i / 2] << 16);
 }
 
-// Sums over the workgroup, the same bits in every thread.
-template <class F>
-__device__ __forceinline__ F sum_threads(F x, F* part) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
-  __syncthreads();
-  x = part[0];
-#pragma unroll
-  for (int w = 1; w < kDistThreads / 64; ++w) x += part[w];
-  return x;
-}
-template <class F>
-__device__ __forceinline__ F max_threads(F x, F* part) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) x = fmax(x, __shfl_xor(x, o));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
-  __syncthreads();
-  x = part[0];
-#pragma unroll
-  for (int w = 1; w < kDistThreads / 64; ++w) x = fmax(x, part[w]);
-  return x;
-}
-
 // c: log2(e) / temperature.  exp2 of (z - top) * c with -infinity as 0 whatever top is.
 __device__ __forceinline__ float weight_of(float z, float top, float c) {
   return z == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((z - top) * c);
 }
 
-template <class T>
-__global__ void __launch_bounds__(kDistThreads) distill_loss_kernel(atspeed_distill_loss_args a, float c) {
-  constexpr int VEC = 16 / sizeof(T);
-  extern __shared__ uint32_t bits[];               // a bit a column: a top
-  __shared__ int index[kMaxTops];
-  __shared__ double prob[kMaxTops], part64[kDistThreads / 64];
-  __shared__ float part32[kDistThreads / 64];
-  const int r = blockIdx.x, tid = threadIdx.x, m = a.n_tops, V = a.n_cols;
-  const T* row = static_cast<const T*>(a.logits) + (int64_t)r * a.logits_stride;
-  for (int i = tid; i < (V + 31) / 32; i += kDistThreads) bits[i] = 0;
+// Sum over the threads that have tops: those of a wave, or of four through LDS.
+__device__ __forceinline__ double sum_tops(double x, bool one_wave, double* part) {
+  x = wave_sum(x);
+  if (one_wave) return x;
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0 && threadIdx.x < kMaxTops) part[threadIdx.x >> 6] = x;
+  __syncthreads();
+  return (part[0] + part[1]) + (part[2] + part[3]);
+}
 
-  // the teacher's buckets; thread j has top j
+// A workgroup a row.  Three barriers for up to 64 tops: the tops' bits and the teacher's
+// largest logit, the teacher's sum, the row's largest and sum; then the tops' wave is alone.
+template <class T, int THREADS>
+__global__ void __launch_bounds__(THREADS) distill_loss_kernel(atspeed_distill_loss_args a, float c) {
+  constexpr int VEC = 16 / sizeof(T), WAVES = THREADS / 64, STEP = THREADS * VEC;
+  extern __shared__ uint32_t bits[];               // a bit a column: a top
+  __shared__ int index[kMaxTops], twice;
+  __shared__ double share[kMaxTops], part[4], wave_top[WAVES], wave_all[WAVES];
+  __shared__ float row_top[WAVES], row_sum[WAVES];
+  const int r = blockIdx.x, tid = threadIdx.x, wave = tid >> 6, m = a.n_tops, V = a.n_cols;
+  const T* row = static_cast<const T*>(a.logits) + (int64_t)r * a.logits_stride;
+  float* saved = a.saved + (int64_t)r * (2 + m);
+
+  // asked for at once: the row's first columns and the teacher's; thread j has top j
+  auto load = [&](int v) {
+    u32x4_t raw = {};
+    if (v + VEC <= V) {
+      raw = *reinterpret_cast<const u32x4_any_t*>(row + v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        uint32_t x = sizeof(T) == 2 ? 0xff80u : 0xff800000u;       // -infinity
+        if (v + i < V) x = VEC == 4 ? reinterpret_cast<const uint32_t*>(row)[v + i] : reinterpret_cast<const uint16_t*>(row)[v + i];
+        raw[i * 4 / VEC] |= x << (VEC == 4 ? 0 : 16 * (i & 1));
+      }
+    }
+    return raw;
+  };
+  u32x4_t ahead[2] = {load(tid * VEC), load(tid * VEC + STEP)};
   int mine = -1;
-  double t = -INFINITY;
+  float teacher = -INFINITY;
   if (tid < m) {
     mine = a.teacher_index[(int64_t)r * m + tid];
-    const float z = St<T>::ld(static_cast<const T*>(a.teacher_logit) + (int64_t)r * m + tid);
-    if ((unsigned)mine >= (unsigned)V || z == -INFINITY) mine = -1;
-    if (mine >= 0) t = (double)z / (double)a.temperature;
-    index[tid] = mine;
+    teacher = St<T>::ld(static_cast<const T*>(a.teacher_logit) + (int64_t)r * m + tid);
   }
   const float weight = a.weight ? a.weight[r] : 1.f;
-  float* saved = a.saved + (int64_t)r * (2 + m);
-  __syncthreads();
-  if (mine >= 0) atomicOr(&bits[mine >> 5], 1u << (mine & 31));
-  if (!__syncthreads_or(mine >= 0) || weight == 0.f) {
+  const double tail = a.tail ? (double)a.tail[r] : -INFINITY, inv_t = 1.0 / (double)a.temperature;
+  if (tid == 0) twice = 0;
+  for (int i = tid; i < (V + 31) / 32; i += THREADS) bits[i] = 0;
+  if ((unsigned)mine >= (unsigned)V || teacher == -INFINITY) mine = -1;
+  const double t = mine >= 0 ? (double)teacher * inv_t : -INFINITY;
+  const float z = mine >= 0 ? St<T>::ld(row + mine) : -INFINITY;
+  double t_top = t;
+  static_for<6>([&](auto s) { t_top = fmax(t_top, partner<s>(t_top)); });
+  if ((tid & 63) == 0) wave_top[wave] = t_top;
+  if (tid < m) index[tid] = mine;
+  const bool counts = __syncthreads_or(mine >= 0) && weight != 0.f;
+  if (!counts) {
     if (tid < 2) saved[tid] = 0.f;
     if (tid < m) saved[2 + tid] = kNoTop;
     if (tid == 0) a.loss[r] = 0.f;
     return;
   }
-  const double tail = a.tail ? (double)a.tail[r] : -INFINITY;
-  const double t_top = fmax(max_threads(t, part64), tail);
-  const double w = mine >= 0 ? exp(t - t_top) : 0.0, w_rest = exp(tail - t_top);
-  const double w_all = sum_threads(w, part64) + w_rest;
-  const double log_w = t_top + log(w_all);
-  if (tid < m) prob[tid] = w / w_all;
+  if (mine >= 0 && (atomicOr(&bits[mine >> 5], 1u << (mine & 31)) >> (mine & 31) & 1)) twice = 1;
+  t_top = tail;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) t_top = fmax(t_top, wave_top[w]);
+  const double w = mine >= 0 ? exp_below(t, t_top) : 0.0, w_rest = tail > -INFINITY ? exp_below(tail, t_top) : 0.0;
+  const double w_wave = wave_sum(w);
+  if ((tid & 63) == 0) wave_all[wave] = w_wave;
+  if (tid < m) share[tid] = w;
   __syncthreads();
+  // one pass over the logits: the largest, and the sum of the others' exponentials
+  float top = -INFINITY, sum = 0.f;
+  for (int v0 = tid * VEC; __any(v0 < V); v0 += 2 * STEP) {
+    u32x4_t raw[2] = {ahead[0], ahead[1]};
+    if (v0 + 2 * STEP < V) ahead[0] = load(v0 + 2 * STEP);
+    if (v0 + 3 * STEP < V) ahead[1] = load(v0 + 3 * STEP);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int v = v0 + h * STEP;
+      if (v >= V) continue;
+      float x[VEC];
+      unpack<T>(raw[h], x);
+      float most = x[0];
+#pragma unroll
+      for (int i = 1; i < VEC; ++i) most = max_nan(most, x[i]);
+      if (!(most <= top)) {
+        const float now = max_nan(most, top);
+        if (top > -INFINITY) sum *= __builtin_amdgcn_exp2f((top - now) * c);
+        top = now;
+      }
+      if (top == -INFINITY) continue;
+      const uint32_t tops = (bits[v >> 5] >> (v & 31)) & ((1u << VEC) - 1);
+      float some = 0.f;                            // vectors first: a thread's sum has few terms
+      if (!__any(tops)) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) some += __builtin_amdgcn_exp2f((x[i] - top) * c);
+      } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) some += tops >> i & 1 ? 0.f : __builtin_amdgcn_exp2f((x[i] - top) * c);
+      }
+      sum += some;
+    }
+  }
+  float z_top = wave_max_nan(top);
+  const float w_sum = wave_sum(top > -INFINITY ? sum * __builtin_amdgcn_exp2f((top - z_top) * c) : 0.f);
+  if ((tid & 63) == 0) {
+    row_top[wave] = z_top;
+    row_sum[wave] = w_sum;
+  }
+  __syncthreads();
+  const bool one_wave = m <= 64;
+  if (one_wave && wave) return;
+  z_top = row_top[0];
+#pragma unroll
+  for (int i = 1; i < WAVES; ++i) z_top = max_nan(z_top, row_top[i]);
+  const bool bad = !(z_top < INFINITY);            // NaN and +infinity go through to the loss
+  if (bad) z_top = NAN;
+  double rest = 0.0, w_all = w_rest;
+#pragma unroll
+  for (int i = 0; i < WAVES; ++i) {
+    if (row_top[i] > -INFINITY) rest += (double)(row_sum[i] * __builtin_amdgcn_exp2f((row_top[i] - z_top) * c));
+    w_all += wave_all[i];
+  }
   // columns that were named twice: the first one has the sum
   bool first = mine >= 0;
-  double p = 0.0;
-  if (mine >= 0)
+  double p = w;
+  if (twice && mine >= 0) {
+    p = 0.0;
     for (int j = 0; j < m; ++j)
       if (index[j] == mine) {
         if (j < tid) first = false;
-        p += prob[j];
+        p += share[j];
       }
-
-  // one pass over the logits: the largest, and the sum of the others' exponentials
-  float top = -INFINITY, sum = 0.f;
-  for (int v0 = tid * VEC; v0 < V; v0 += kDistThreads * VEC) {
-    float x[VEC];
-    if (v0 + VEC <= V) {
-      unpack<T>(*reinterpret_cast<const u32x4_any_t*>(row + v0), x);
-    } else {
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) x[i] = v0 + i < V ? St<T>::ld(row + v0 + i) : -INFINITY;
-    }
-    const uint32_t tops = bits[v0 >> 5] >> (v0 & 31);
-    float most = x[0];
-#pragma unroll
-    for (int i = 1; i < VEC; ++i) most = __builtin_elementwise_maximum(most, x[i]);
-    if (!(most <= top)) {
-      const float now = __builtin_elementwise_maximum(most, top);
-      if (top > -INFINITY) sum *= __builtin_amdgcn_exp2f((top - now) * c);
-      top = now;
-    }
-    if (top == -INFINITY) continue;
-    float some = 0.f;                              // vectors first: a thread's sum has few terms
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-      const float e = __builtin_amdgcn_exp2f((x[i] - top) * c);
-      some += tops >> i & 1 ? 0.f : e;
-    }
-    sum += some;
   }
-  // NaN and +infinity go through to the loss
-  const bool bad = __syncthreads_or(!(top < INFINITY));
-  const float z_top = bad ? NAN : max_threads(top, part32);
-  const double rest = sum_threads(top > -INFINITY ? (double)(sum * __builtin_amdgcn_exp2f((top - z_top) * c)) : 0.0, part64);
-  float z = 0.f;
-  double e = 0.0;
-  if (mine >= 0) {
-    z = St<T>::ld(row + mine);
-    e = weight_of(z, z_top, c);
-  }
-  const double all = rest + sum_threads(first ? e : 0.0, part64);
+  p /= w_all;
+  const double e = mine >= 0 ? (double)weight_of(z, z_top, c) : 0.0;
+  const double all = rest + sum_tops(first ? e : 0.0, one_wave, part);
 
   // the divergence, bucket by bucket
   const bool empty = all == 0.0;                   // no logit but -infinity: q is 0
-  const double q = empty ? 0.0 : e / all, q_rest = empty ? 0.0 : rest / all, p_rest = w_rest / w_all;
-  const double log_all = log(all), inv_t = 1.0 / (double)a.temperature;
+  const double inv_all = 1.0 / all, q = empty ? 0.0 : e * inv_all, q_rest = empty ? 0.0 : rest * inv_all;
+  const double p_rest = w_rest / w_all;
+  const double log_all = log(all);
   const double log_q = z == -INFINITY ? -INFINITY : (double)(z - z_top) * inv_t - log_all;
-  const double log_qr = rest == 0.0 ? -INFINITY : log(rest) - log_all, log_pr = tail - log_w;
+  const double log_qr = rest == 0.0 ? -INFINITY : log(rest) - log_all, log_pr = tail - (t_top + log(w_all));
+  const double log_p = log(p);
   double mass = 0.0, far = 0.0, mass_r = 0.0, far_r = 0.0;     // a bucket's weight, log of the quotient
   if (a.reverse) {
     mass = first && e > 0.0 ? q : 0.0;
-    far = log_q - log(p);
+    far = log_q - log_p;
     mass_r = rest > 0.0 ? q_rest : 0.0;
     far_r = log_qr - log_pr;
   } else {
     mass = first && p > 0.0 ? p : 0.0;
-    far = log(p) - log_q;
+    far = log_p - log_q;
     mass_r = p_rest;
     far_r = log_pr - log_qr;
   }
   if (bad || !(all == all)) mass_r = far_r = NAN;
-  const double loss = sum_threads(mass > 0.0 ? mass * far : 0.0, part64) + (mass_r == 0.0 ? 0.0 : mass_r * far_r);
+  const double loss = sum_tops(mass > 0.0 ? mass * far : 0.0, one_wave, part) + (mass_r == 0.0 ? 0.0 : mass_r * far_r);
   const double step = (double)weight * (double)a.temperature;
   double at_top = 0.0, a_rest = 0.0;
   if (a.reverse) {
@@ -191,6 +217,7 @@ __global__ void __launch_bounds__(kDistThreads) distill_loss_kernel(atspeed_dist
 }
 
 // A workgroup a row and 4,096 columns.
+constexpr int kDistThreads = 256;
 constexpr int kGradVecs = 16;   // columns a thread
 
 template <class T>
@@ -230,6 +257,20 @@ __global__ void __launch_bounds__(kDistThreads) distill_grad_kernel(atspeed_dist
   }
 }
 
+template <class T, int THREADS>
+static atspeed_status launch_loss(const atspeed_distill_loss_args& a, size_t lds, float c, hipStream_t st) {
+  if (lds > (48 << 10))
+    HIP_TRY(hipFuncSetAttribute((const void*)distill_loss_kernel<T, THREADS>, hipFuncAttributeMaxDynamicSharedMemorySize, 1 << 17));
+  hipLaunchKernelGGL((distill_loss_kernel<T, THREADS>), dim3(a.n_rows), dim3(THREADS), lds, st, a, c);
+  HIP_TRY(hipGetLastError());
+  return ATSPEED_OK;
+}
+// Long rows that do not fill the card four to a CU take workgroups of 1,024.
+template <class T>
+static atspeed_status run_loss(const atspeed_distill_loss_args& a, size_t lds, float c, hipStream_t st) {
+  return a.n_cols >= 16384 && a.n_rows <= 1024 ? launch_loss<T, 1024>(a, lds, c, st) : launch_loss<T, 256>(a, lds, c, st);
+}
+
 static atspeed_status check_distill(int dtype, int n_rows, int n_cols, int n_tops, float temperature) {
   if (dtype != ATSPEED_FP32 && dtype != ATSPEED_BF16) return fail(ATSPEED_E_INVALID, "dtype");
   if (n_rows < 0) return fail(ATSPEED_E_INVALID, "n_rows must be >= 0");
@@ -258,15 +299,7 @@ atspeed_status atspeed_distill_loss(const atspeed_distill_loss_args* args, void*
   if (a.n_rows > kMaxGroups) return fail(ATSPEED_E_SHAPE, "distill loss: too many rows");
   const size_t lds = (size_t)(a.n_cols + 31) / 32 * 4;
   const float c = exponent_scale(a.temperature);
-  const dim3 grid(a.n_rows), threads(kDistThreads);
-  const bool bf16 = a.dtype == ATSPEED_BF16;
-  if (lds > (48 << 10))
-    HIP_TRY(hipFuncSetAttribute(bf16 ? (const void*)distill_loss_kernel<bf16_t> : (const void*)distill_loss_kernel<float>,
-                                hipFuncAttributeMaxDynamicSharedMemorySize, 1 << 17));
-  if (bf16) hipLaunchKernelGGL((distill_loss_kernel<bf16_t>), grid, threads, lds, (hipStream_t)stream, a, c);
-  else hipLaunchKernelGGL((distill_loss_kernel<float>), grid, threads, lds, (hipStream_t)stream, a, c);
-  HIP_TRY(hipGetLastError());
-  return ATSPEED_OK;
+  return a.dtype == ATSPEED_BF16 ? run_loss<bf16_t>(a, lds, c, (hipStream_t)stream) : run_loss<float>(a, lds, c, (hipStream_t)stream);
 }
 
 atspeed_status atspeed_distill_grad(const atspeed_distill_grad_args* args, void* stream) {

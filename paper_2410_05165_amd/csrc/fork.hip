@@ -10,24 +10,28 @@ namespace atspeed {
 typedef unsigned long long u64;
 
 // ---------------------------------------------------------------- page tables
-// What a page's holders are after the call depends on every row, so the work goes in steps
-// that each end a launch:
-//   clear   the pages' counters,
-//   count   per page the old entries and the new full ones, and the lowest row that wants it
-//           as its last page; the new tables are put down beside the old ones,
-//   decide  how many pages of each piece of the pool come free; which rows copy, numbered,
+// What becomes of a page depends on every row, so the work has steps, each behind the one
+// before:
+//   count   shared[page] loses one for each old entry and gains one for each new full one; the
+//           new tables are put down beside the old ones, which other rows still read,
+//   claim   a last page that is left without a holder (-1) goes to the lowest row that wants
+//           it,
+//   decide  the other rows that want one copy; they are numbered, and so are the pages that
+//           come free (-1) in pieces of the pool,
 //   write   tables, holders, free list.
-// All sums are of whole numbers, so the atomics' order changes nothing.
-constexpr int kForkThreads = 256;
-constexpr int kForkRows = 8;         // consecutive rows of a thread that counts
-constexpr int kNoRow = 0x7fffffff;
+// Sums and minima of whole numbers: the order of the atomics changes nothing.  Launches of
+// their own for count, claim and decide (one workgroup), and write; one workgroup does it all
+// where there is little to do.
+constexpr int kForkThreads = 256, kForkOne = 1024;
+constexpr int kForkFew = 4096;       // entries of the tables, and pages, that one workgroup takes by itself
+constexpr int kPieces = 1024;        // of the pool, at most
+constexpr int kRun = 8;              // consecutive rows of a thread that counts
 
 struct ForkArgs {
   atspeed_page_fork_args a;
-  u64* holders;      // [n_pool] old entries << 32 | new full entries
-  int* first;        // [n_pool] lowest row that wants the page as its last one
   int* next;         // [B, max_pages] the new tables, up to the last page
-  int* gone;         // [pieces] pages of a piece of the pool that come free
+  int* last;         // [B] the page that a row wants as its last one, -1: none
+  int* gone;         // [pieces + 1] pages that come free before a piece of the pool, and in all
   int* rank;         // [B] 1, 2, ... for the rows that copy, 0 for the others
   int* taker;        // [B] the rows that copy, in order
   int* total;        // [2] rows that copy; pages that were free
@@ -46,9 +50,10 @@ __device__ __forceinline__ ForkRow row_of(const ForkArgs& p, int j) {
   ForkRow r;
   const int mine = held_of(p, j), tail = (1 << p.shift) - 1;
   r.from = p.a.src ? p.a.src[j] : j;
+  r.kept = p.a.keep ? p.a.keep[j] : -1;
   r.bad = r.from < -1 || r.from >= p.a.B;
   const int there = r.bad || r.from < 0 ? 0 : held_of(p, r.from);
-  r.kept = r.from == -1 ? 0 : p.a.keep ? p.a.keep[j] : there;
+  r.kept = r.from == -1 ? 0 : p.a.keep ? r.kept : there;
   r.bad = r.bad || r.kept < 0 || r.kept > there;
   if (r.bad) {
     r.from = j;
@@ -59,65 +64,55 @@ __device__ __forceinline__ ForkRow row_of(const ForkArgs& p, int j) {
   r.over = r.kept & tail;
   return r;
 }
-
-__global__ void __launch_bounds__(kForkThreads) fork_clear_kernel(ForkArgs p) {
-  const int step = gridDim.x * kForkThreads;
-  for (int i = blockIdx.x * kForkThreads + threadIdx.x; i < p.a.n_pool; i += step) {
-    p.holders[i] = 0;
-    p.first[i] = kNoRow;
-  }
+// Waits until what the workgroup stored, added and loaded is done.
+__device__ __forceinline__ void sync_memory() {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
 }
+// What this launch may have changed.
+__device__ __forceinline__ int fresh(const int* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ bool is_page(const ForkArgs& p, int q) { return (unsigned)q < (unsigned)p.a.n_pool; }
 
-// A thread takes one column of a few consecutive rows: where these hold the same page, as
+// Column c of rows j0 .. j1 - 1 (row: theirs, from j0 on).  Where these hold the same page, as
 // the beams of one request do, it is counted once for all of them.
-__global__ void __launch_bounds__(kForkThreads) fork_count_kernel(ForkArgs p, int columns) {
-  const int c = blockIdx.x % columns * kForkThreads + threadIdx.x, j0 = blockIdx.x / columns * kForkRows;
+template <int RUN>
+__device__ __forceinline__ void count_column(const ForkArgs& p, const ForkRow* row, int c, int j0, int j1) {
   const int most = p.a.max_pages;
-  int page = -1;
-  u64 n = 0;
-  auto add = [&](int q, u64 d) {
-    if ((unsigned)q >= (unsigned)p.a.n_pool) return;
+  int was[RUN], will[RUN];
+#pragma unroll
+  for (int i = 0; i < RUN; ++i) {
+    was[i] = will[i] = -1;
+    if (j0 + i >= j1) continue;
+    const ForkRow& r = row[i];
+    if (c < r.before) was[i] = p.a.block_table[(int64_t)(j0 + i) * most + c];
+    if (r.from >= 0 && c < r.full + (r.over > 0)) {
+      const int q = p.a.block_table[(int64_t)r.from * most + c];
+      p.next[(int64_t)(j0 + i) * most + c] = q;
+      if (c < r.full) will[i] = q;
+      else p.last[j0 + i] = is_page(p, q) ? q : -1;
+    }
+    if (c == 0 && (r.from < 0 || !r.over)) p.last[j0 + i] = -1;
+  }
+  int page = -1, n = 0;
+  auto add = [&](int q, int d) {
+    if (!is_page(p, q)) return;
     if (q != page) {
-      if (n) atomicAdd(&p.holders[page], n);
+      if (n) atomicAdd(&p.a.shared[page], n);
       page = q;
       n = 0;
     }
     n += d;
   };
-  for (int j = j0; j < min(j0 + kForkRows, p.a.B); ++j) {
-    const ForkRow r = row_of(p, j);
-    if (c >= most) continue;
-    if (c < r.before) add(p.a.block_table[(int64_t)j * most + c], 1ull << 32);
-    if (r.from < 0 || c > r.full || (c == r.full && !r.over)) continue;
-    const int q = p.a.block_table[(int64_t)r.from * most + c];
-    p.next[(int64_t)j * most + c] = q;
-    if (c < r.full) add(q, 1);
-    else if ((unsigned)q < (unsigned)p.a.n_pool) atomicMin(&p.first[q], j);
+#pragma unroll
+  for (int i = 0; i < RUN; ++i) {
+    add(was[i], -1);
+    add(will[i], 1);
   }
-  if (n) atomicAdd(&p.holders[page], n);
+  if (n) atomicAdd(&p.a.shared[page], n);
 }
 
-// A page's further holders after the call (below 0: nobody holds it), and whether the first
-// row that wants it as its last page takes it as it is.
-__device__ __forceinline__ int left_of(const ForkArgs& p, int page, u64 h, bool& takes) {
-  const int was = (int)(h >> 32), stays = (int)(unsigned)h;
-  const int others = p.a.shared[page] - was;      // below 0: no holder but rows
-  takes = stays == 0 && others < 0 && p.first[page] != kNoRow;
-  return others + stays + takes;
-}
-
-__device__ __forceinline__ int sum_threads(int x, int* part) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
-  __syncthreads();
-  x = 0;
-#pragma unroll
-  for (int w = 0; w < kForkThreads / 64; ++w) x += part[w];
-  return x;
-}
 // Sum of the threads before this one, and of all.
+template <int THREADS>
 __device__ __forceinline__ int scan_threads(int x, int* part, int* all) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int inc = x;
@@ -131,7 +126,7 @@ __device__ __forceinline__ int scan_threads(int x, int* part, int* all) {
   __syncthreads();
   int before = inc - x, total = 0;
 #pragma unroll
-  for (int w = 0; w < kForkThreads / 64; ++w) {
+  for (int w = 0; w < THREADS / 64; ++w) {
     if (w < wave) before += part[w];
     total += part[w];
   }
@@ -139,111 +134,154 @@ __device__ __forceinline__ int scan_threads(int x, int* part, int* all) {
   return before;
 }
 
-// Workgroup i < pieces: a piece of the pool; the last one: the rows.
-__global__ void __launch_bounds__(kForkThreads) fork_decide_kernel(ForkArgs p) {
-  __shared__ int part[kForkThreads / 64];
-  if ((int)blockIdx.x < p.pieces) {
-    const int begin = blockIdx.x * p.piece, end = min(begin + p.piece, p.a.n_pool);
-    int n = 0;
-    for (int i = begin + threadIdx.x; i < end; i += kForkThreads) {
-      const u64 h = p.holders[i];
-      bool takes;
-      n += (h >> 32) && left_of(p, i, h, takes) < 0;
-    }
-    n = sum_threads(n, part);
-    if (threadIdx.x == 0) p.gone[blockIdx.x] = n;
-    return;
+// claim and decide, by one workgroup of kForkOne threads: a thread a row, a wave 64 pages at a
+// time.  Rows that want the same page meet in a table of pages in LDS, half full at most.
+constexpr int kSlots = 2 * kForkOne;
+
+__device__ __forceinline__ void decide(const ForkArgs& p) {
+  __shared__ int part[kForkOne / 64], gone[kPieces], page[kSlots], lowest[kSlots];
+  const int j = threadIdx.x, B = p.a.B, lane = j & 63, chunks = (p.a.n_pool + 63) / 64;
+  const int q = j < B ? fresh(&p.last[j]) : -1;
+  for (int i = j; i < kSlots; i += kForkOne) {
+    page[i] = -1;
+    lowest[i] = kForkOne;
   }
-  int before = 0;
-  for (int j0 = 0; j0 < p.a.B; j0 += kForkThreads) {
-    const int j = j0 + threadIdx.x;
-    bool copies = false;
-    if (j < p.a.B) {
-      const ForkRow r = row_of(p, j);
-      if (r.from >= 0 && r.over) {
-        const int q = p.next[(int64_t)j * p.a.max_pages + r.full];
-        if ((unsigned)q < (unsigned)p.a.n_pool) {
-          bool takes;
-          left_of(p, q, p.holders[q], takes);
-          copies = !(takes && p.first[q] == j);
-        }
+  gone[j] = 0;
+  const bool may = q >= 0 && fresh(&p.a.shared[q]) < 0;
+  __syncthreads();
+  int slot = (unsigned)(q * 0x9E3779B1u) >> 21;
+  if (may) {
+    for (;; slot = (slot + 1) & (kSlots - 1)) {
+      const int there = atomicCAS(&page[slot], -1, q);
+      if (there == -1 || there == q) break;
+    }
+    atomicMin(&lowest[slot], j);
+  }
+  for (int c0 = j >> 6; c0 < chunks; c0 += 8 * (kForkOne / 64)) {
+    int left[8];
+#pragma unroll
+    for (int o = 0; o < 8; ++o) {
+      const int i = (c0 + o * (kForkOne / 64)) * 64 + lane;
+      left[o] = i < p.a.n_pool ? fresh(&p.a.shared[i]) : 0;
+    }
+#pragma unroll
+    for (int o = 0; o < 8; ++o) {
+      const int n = __popcll(__ballot(left[o] == -1));
+      if (n && lane == 0) atomicAdd(&gone[(c0 + o * (kForkOne / 64)) * 64 / p.piece], n);
+    }
+  }
+  sync_memory();                           // nobody looks at the pool any more
+  const bool takes = may && lowest[slot] == j, copies = q >= 0 && !takes;
+  if (takes) {
+    p.a.shared[q] = 0;
+    atomicSub(&gone[q / p.piece], 1);
+  }
+  int all;
+  const int at = scan_threads<kForkOne>(copies, part, &all);
+  if (j < B) p.rank[j] = copies ? at + 1 : 0;
+  if (copies) p.taker[at] = j;
+  if (j == 0) {
+    p.total[0] = all;
+    p.total[1] = min(max(*p.a.n_free, 0), p.a.n_pool);
+  }
+  const int ahead = scan_threads<kForkOne>(gone[j], part, &all);
+  if (j < p.pieces) p.gone[j] = ahead;
+  if (j == 0) p.gone[p.pieces] = all;
+}
+
+// Of the stack of free pages -- those that were free, then the released ones in ascending
+// order -- the k-th row that copies has the k-th from the top.
+struct Stack {
+  int F, have, top;
+};
+__device__ __forceinline__ Stack stack_of(const ForkArgs& p) {
+  Stack s;
+  s.F = fresh(&p.total[1]);
+  s.have = (int)min((long long)s.F + fresh(&p.gone[p.pieces]), (long long)p.a.n_pool);
+  s.top = s.have - min(fresh(&p.total[0]), s.have);
+  return s;
+}
+// Holders and free list of a piece of the pool, a wave.
+template <class Row>
+__device__ __forceinline__ void write_piece(const ForkArgs& p, const Stack& s, int i, int lane, Row row) {
+  const int begin = i * p.piece, end = min(begin + p.piece, p.a.n_pool);
+  int at = s.F + fresh(&p.gone[i]);
+#pragma unroll 4
+  for (int c0 = begin; c0 < end; c0 += 64) {
+    const int c = c0 + lane, left = c < end ? fresh(&p.a.shared[c]) : 0;
+    const u64 out = __ballot(left == -1);
+    if (left == -1) {
+      p.a.shared[c] = 0;
+      const int place = at + __popcll(out & ((1ull << lane) - 1));
+      if (place < s.top) {
+        p.a.free_pages[place] = c;
+      } else if (place < s.have) {
+        const int j = fresh(&p.taker[s.have - 1 - place]);
+        p.a.block_table[(int64_t)j * p.a.max_pages + row(j).full] = c;
+        p.a.copy_dst[j] = c;
       }
     }
-    int all;
-    const int at = before + scan_threads(copies, part, &all);
-    if (j < p.a.B) p.rank[j] = copies ? at + 1 : 0;
-    if (copies) p.taker[at] = j;
-    before += all;
+    at += __popcll(out);
   }
-  if (threadIdx.x == 0) {
-    p.total[0] = before;
-    p.total[1] = min(max(*p.a.n_free, 0), p.a.n_pool);
+}
+// A row's table and outputs, a wave.
+__device__ __forceinline__ void write_row(const ForkArgs& p, const Stack& s, int j, int lane, const ForkRow& r) {
+  const int rank = fresh(&p.rank[j]), most = p.a.max_pages;
+  const bool copies = rank > 0 && rank <= s.have, refused = rank > s.have;
+  if (r.from >= 0 && r.from != j) {
+    const int n = r.full + (r.over && !rank);
+#pragma unroll 4
+    for (int c = lane; c < n; c += 64) p.a.block_table[(int64_t)j * most + c] = p.next[(int64_t)j * most + c];
+  }
+  if (lane) return;
+  p.a.length[j] = refused ? r.full << p.shift : r.kept;
+  p.a.refused[j] = r.bad ? 2 : refused;
+  p.a.copy_src[j] = copies ? p.next[(int64_t)j * most + r.full] : -1;
+  p.a.copy_len[j] = copies ? r.over : 0;
+  if (!copies) {
+    p.a.copy_dst[j] = -1;
+  } else if (s.have - rank < s.F) {
+    const int q = p.a.free_pages[s.have - rank];
+    p.a.block_table[(int64_t)j * most + r.full] = q;
+    p.a.copy_dst[j] = q;
   }
 }
 
-// Workgroup i < pieces: holders and free list of a piece of the pool; the others: a row each.
-// Of the stack of free pages -- those that were free, then the released ones in ascending
-// order -- the k-th row that copies has the k-th from the top.
+__global__ void __launch_bounds__(kForkThreads) fork_count_kernel(ForkArgs p, int columns) {
+  __shared__ ForkRow row[kRun];
+  const int c = blockIdx.x % columns * kForkThreads + threadIdx.x, j0 = blockIdx.x / columns * kRun;
+  if (threadIdx.x < kRun && j0 + (int)threadIdx.x < p.a.B) row[threadIdx.x] = row_of(p, j0 + threadIdx.x);
+  __syncthreads();
+  if (c < p.a.max_pages) count_column<kRun>(p, row, c, j0, min(j0 + kRun, p.a.B));
+}
+
+__global__ void __launch_bounds__(kForkOne) fork_decide_kernel(ForkArgs p) {
+  decide(p);
+}
+
+// A wave a piece of the pool, then a wave a row.
 __global__ void __launch_bounds__(kForkThreads) fork_write_kernel(ForkArgs p) {
-  __shared__ int part[kForkThreads / 64];
-  const int tid = threadIdx.x, most = p.a.max_pages, piece = min((int)blockIdx.x, p.pieces);
-  int ahead = 0, all = 0;
-  for (int i = tid; i < p.pieces; i += kForkThreads) {
-    const int n = p.gone[i];
-    all += n;
-    ahead += i < piece ? n : 0;
-  }
-  all = sum_threads(all, part);
-  ahead = sum_threads(ahead, part);
-  const int F = p.total[1], have = (int)min((long long)F + all, (long long)p.a.n_pool);
-  const int top = have - min(p.total[0], have);
-  if ((int)blockIdx.x < p.pieces) {
-    const int begin = blockIdx.x * p.piece, end = min(begin + p.piece, p.a.n_pool);
-    int s = F + ahead;
-    for (int i0 = begin; i0 < end; i0 += kForkThreads) {
-      const int i = i0 + tid;
-      bool out = false;
-      if (i < end) {
-        const u64 h = p.holders[i];
-        if (h >> 32) {
-          bool takes;
-          const int left = left_of(p, i, h, takes);
-          out = left < 0;
-          p.a.shared[i] = max(left, 0);
-        }
-      }
-      int n;
-      const int at = s + scan_threads(out, part, &n);
-      if (out && at < top) p.a.free_pages[at] = i;
-      if (out && at >= top && at < have) {
-        const int j = p.taker[have - 1 - at];
-        const ForkRow r = row_of(p, j);
-        p.a.block_table[(int64_t)j * most + r.full] = i;
-        p.a.copy_dst[j] = i;
-      }
-      s += n;
-    }
-    if (blockIdx.x == 0 && tid == 0) *p.a.n_free = top;
-    return;
-  }
-  const int j = blockIdx.x - p.pieces, rank = p.rank[j];
-  const ForkRow r = row_of(p, j);
-  const bool copies = rank > 0 && rank <= have, refused = rank > have;
-  for (int c = tid; c < r.full + (r.over && !rank); c += kForkThreads)
-    if (r.from >= 0 && r.from != j) p.a.block_table[(int64_t)j * most + c] = p.next[(int64_t)j * most + c];
-  if (tid == 0) {
-    p.a.length[j] = refused ? r.full << p.shift : r.kept;
-    p.a.refused[j] = r.bad ? 2 : refused;
-    p.a.copy_src[j] = copies ? p.next[(int64_t)j * most + r.full] : -1;
-    p.a.copy_len[j] = copies ? r.over : 0;
-    if (!copies) {
-      p.a.copy_dst[j] = -1;
-    } else if (have - rank < F) {
-      const int q = p.a.free_pages[have - rank];
-      p.a.block_table[(int64_t)j * most + r.full] = q;
-      p.a.copy_dst[j] = q;
-    }
-  }
+  const int i = __builtin_amdgcn_readfirstlane(blockIdx.x * (kForkThreads / 64) + (threadIdx.x >> 6)), lane = threadIdx.x & 63;
+  const Stack s = stack_of(p);
+  if (i < p.pieces) write_piece(p, s, i, lane, [&](int j) { return row_of(p, j); });
+  else if (i < p.pieces + p.a.B) write_row(p, s, i - p.pieces, lane, row_of(p, i - p.pieces));
+  if (i == 0 && lane == 0) *p.a.n_free = s.top;
+}
+
+__global__ void __launch_bounds__(kForkOne) fork_one_kernel(ForkArgs p) {
+  __shared__ ForkRow row[kForkOne];
+  const int B = p.a.B, most = p.a.max_pages, lane = threadIdx.x & 63;
+  if ((int)threadIdx.x < B) row[threadIdx.x] = row_of(p, threadIdx.x);
+  __syncthreads();
+  for (int i = threadIdx.x; i < B * most; i += kForkOne) count_column<1>(p, row + i / most, i % most, i / most, B);
+  sync_memory();
+  decide(p);
+  sync_memory();
+  const Stack s = stack_of(p);
+  for (int i = threadIdx.x >> 6; i < p.pieces; i += kForkOne / 64)
+    write_piece(p, s, i, lane, [&](int j) -> const ForkRow& { return row[j]; });
+  for (int j = threadIdx.x >> 6; j < B; j += kForkOne / 64) write_row(p, s, j, lane, row[j]);
+  if (threadIdx.x == 0) *p.a.n_free = s.top;
 }
 
 // ---------------------------------------------------------------- moving tokens
@@ -371,14 +409,13 @@ static size_t lay_out(ForkArgs& p, char* base) {
     at += (bytes + 255) & ~(size_t)255;
     return q;
   };
-  // at most 1,024 pieces, since every workgroup of the last step adds them up
-  p.piece = std::max(1024, (a.n_pool + 1023) / 1024);
+  p.piece = 256;
+  while (p.piece < (a.n_pool + kPieces - 1) / kPieces) p.piece *= 2;
   p.pieces = (a.n_pool + p.piece - 1) / p.piece;
   p.shift = log2_of(a.page_size);
-  p.holders = (u64*)take((size_t)a.n_pool * 8);
-  p.first = (int*)take((size_t)a.n_pool * 4);
   p.next = (int*)take((size_t)a.B * a.max_pages * 4);
-  p.gone = (int*)take((size_t)p.pieces * 4);
+  p.last = (int*)take((size_t)a.B * 4);
+  p.gone = (int*)take((size_t)(p.pieces + 1) * 4);
   p.rank = (int*)take((size_t)a.B * 4);
   p.taker = (int*)take((size_t)a.B * 4);
   p.total = (int*)take(8);
@@ -406,18 +443,21 @@ atspeed_status atspeed_page_fork(const atspeed_page_fork_args* args, void* works
   ForkArgs p{};
   p.a = *args;
   const int columns = (args->max_pages + kForkThreads - 1) / kForkThreads;
-  const long long count = (long long)columns * ((args->B + kForkRows - 1) / kForkRows);
+  const long long count = (long long)columns * ((args->B + kRun - 1) / kRun);
   if (count > kMaxGroups) return fail(ATSPEED_E_SHAPE, "page fork: too many rows x pages");
   const size_t need = lay_out(p, nullptr);
   if (!workspace || !aligned16(workspace) || ws_bytes < need)
     return fail(ATSPEED_E_WORKSPACE, "page fork: workspace is too small or not 16-byte aligned");
   lay_out(p, (char*)workspace);
   const hipStream_t st = (hipStream_t)stream;
-  const int clear = std::min((args->n_pool + kForkThreads - 1) / kForkThreads, 1024);
-  hipLaunchKernelGGL(fork_clear_kernel, dim3(clear), dim3(kForkThreads), 0, st, p);
-  hipLaunchKernelGGL(fork_count_kernel, dim3((unsigned)count), dim3(kForkThreads), 0, st, p, columns);
-  hipLaunchKernelGGL(fork_decide_kernel, dim3(p.pieces + 1), dim3(kForkThreads), 0, st, p);
-  hipLaunchKernelGGL(fork_write_kernel, dim3(p.pieces + args->B), dim3(kForkThreads), 0, st, p);
+  if (args->B * (long long)args->max_pages <= kForkFew && args->n_pool <= kForkFew) {
+    hipLaunchKernelGGL(fork_one_kernel, dim3(1), dim3(kForkOne), 0, st, p);
+  } else {
+    hipLaunchKernelGGL(fork_count_kernel, dim3((unsigned)count), dim3(kForkThreads), 0, st, p, columns);
+    hipLaunchKernelGGL(fork_decide_kernel, dim3(1), dim3(kForkOne), 0, st, p);
+    const int waves = kForkThreads / 64;
+    hipLaunchKernelGGL(fork_write_kernel, dim3((p.pieces + args->B + waves - 1) / waves), dim3(kForkThreads), 0, st, p);
+  }
   HIP_TRY(hipGetLastError());
   return ATSPEED_OK;
 }
