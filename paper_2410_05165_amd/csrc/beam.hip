@@ -378,10 +378,7 @@ __global__ void __launch_bounds__(kBeamThreads) beam_rows_kernel(BeamArgs p) {
 constexpr int kEach = 4, kJoinLists = 1024;
 constexpr short kItself = -1;              // length of the list of a row that has ended
 
-struct alignas(16) Entry {
-  u64 key;   // the score's order; 0: none
-  u64 who;   // row << 32 | column + 1
-};
+// A candidate: its score's order (0: none), and row << 32 | column + 1.
 __device__ __forceinline__ bool ahead_of(u64 key, u64 who, u64 than_key, u64 than_who) {
   return (key > than_key) | ((key == than_key) & (who < than_who));
 }
@@ -396,19 +393,19 @@ __device__ __forceinline__ uint32_t bin_of(double d) {
 template <class T, int THREADS>
 __global__ void __launch_bounds__(THREADS) beam_join_kernel(BeamArgs p) {
   constexpr int WAVES = THREADS / 64, ROUND = THREADS * kEach, POOL = 2 * ROUND;   // a power of two
-  extern __shared__ Entry entry[];                 // [POOL]
-  double* const base = (double*)(entry + POOL);    // [kJoinLists] of a row: score - log sum
+  extern __shared__ u64 key[];                     // [POOL]
+  u64* const who_of = key + POOL;                  // [POOL]
+  double* const base = (double*)(who_of + POOL);   // [kJoinLists] of a row: score - log sum
   unsigned short* const open = (unsigned short*)(base + kJoinLists);   // [kJoinLists]
   short* const at = (short*)(open + kJoinLists);   // [kJoinLists]
   short* const len = at + kJoinLists;              // [kJoinLists]
-  __shared__ Entry best[kMaxBeams];
-  __shared__ u64 most[WAVES];
+  __shared__ u64 best_key[kMaxBeams], best_who[kMaxBeams], most[WAVES];
   __shared__ int bin[kBins], rank[THREADS], s_n, s_open[2];
   const atspeed_beam_select_args& a = p.a;
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, k = a.k, parts = p.parts, shift = p.shift;
   const int r1 = min(min(a.row_off[b + 1], a.row_off[a.B]), a.n_rows);   // rows that the first kernel read
   const int group = kJoinLists >> shift;           // lists: row << shift | part
-  int n = 0;                                       // best[0 .. n) are the best so far, in order
+  int n = 0;                                       // best_key[0 .. n) are the best so far, in order
   if (tid < 2) s_open[tid] = 0;
   for (int r0 = max(a.row_off[b], 0); r0 < r1; r0 += group) {
     const int rows = min(group, r1 - r0), lists = rows << shift;
@@ -428,17 +425,15 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(BeamArgs p) {
           len[i << shift | q] = in ? (short)p.len[(int64_t)r * parts + q] : ended && q == 0 ? kItself : 0;
         }
         // NaN stays; a part whose largest logit is -infinity has nothing to add
-        const double now = st.x > all ? st.x : all;
-        const double add = st.x > -INFINITY ? a.log_probs ? st.y : st.y * exp_below(st.x, now) : st.x == -INFINITY ? 0.0 : NAN;
-        total = (all > -INFINITY ? total * exp_below(all, now) : total) + add;
+        const double now = st.x > all ? st.x : all, add = st.x > -INFINITY ? st.y : st.x == -INFINITY ? 0.0 : NAN;
+        total = q == l || a.log_probs ? total + add : total * exp_below(all, now) + add * exp_below(st.x, now);
         all = now;
       }
-      for (int o = 1; o < lanes; o <<= 1) {
-        const double x = __shfl_xor(all, o), y = __shfl_xor(total, o), now = fmax(all, x);
-        if (now > -INFINITY) total = total * exp_below(all, now) + y * exp_below(x, now);
-        else total += y;
-        all = now;
-      }
+      double most_of = all;
+      for (int o = 1; o < lanes; o <<= 1) most_of = fmax(most_of, __shfl_xor(most_of, o));
+      if (!a.log_probs && all > -INFINITY) total *= exp_below(all, most_of);
+      all = most_of;
+      for (int o = 1; o < lanes; o <<= 1) total += __shfl_xor(total, o);
       bool none = !(fabs(score) < INFINITY) || !(total == total);
       double x = score;
       if (!ended && !a.log_probs) {
@@ -471,30 +466,27 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(BeamArgs p) {
       while (depth > 0 && 1 << (depth - 1) >= k) --depth;
 
       // a thread's entries, and its place among the best so far
-      u64 mine[kEach + 1], who[kEach + 1], largest = 0;
+      u64 mine[kEach + 1], who[kEach + 1], largest = 0, listed[kEach];
       int from[kEach], next[kEach];                // next: where its list goes on, -1: it ends here, 0: not the last one taken
 #pragma unroll
       for (int i = 0; i < kEach; ++i) {
-        const int e = tid + i * THREADS, o = e >> depth;
-        mine[i] = who[i] = 0;
-        from[i] = -1;
-        if (o >= n_open) continue;
-        const int l = open[o], d = e & ((1 << depth) - 1), j = at[l] + d, length = len[l], i_row = l >> shift, r = r0 + i_row;
-        if (j >= (length == kItself ? 1 : length)) continue;
-        from[i] = l;
-        next[i] = j + 1 >= length ? -1 : d + 1 == 1 << depth ? j + 1 : 0;
-        if (length == kItself) {
-          mine[i] = order64(base[i_row]);
-          who[i] = (u64)r << 32;
-        } else {
-          const u64 c = p.list[((int64_t)r * parts + (l & ((1 << shift) - 1))) * k + j];
-          mine[i] = order64(base[i_row] + (double)logit_of<T>((uint32_t)(c >> 32)));
-          who[i] = ((u64)r << 32) | (unsigned)(column_of(c) + 1);
-        }
+        const int e = tid + i * THREADS, o = min(e >> depth, n_open - 1), l = open[o], d = e & ((1 << depth) - 1);
+        const int j = at[l] + d, length = len[l], n_here = length == kItself ? 1 : length;
+        const bool in = e >> depth < n_open && j < n_here;
+        from[i] = in ? l : -1;
+        next[i] = j + 1 >= n_here ? -1 : d + 1 == 1 << depth ? j + 1 : 0;
+        listed[i] = in && length != kItself ? p.list[((int64_t)(r0 + (l >> shift)) * parts + (l & ((1 << shift) - 1))) * k + j] : 0;
+      }
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const int row = max(from[i], 0) >> shift;
+        const double logit = listed[i] ? (double)logit_of<T>((uint32_t)(listed[i] >> 32)) : 0.0;   // a key is never 0
+        mine[i] = from[i] >= 0 ? order64(base[row] + logit) : 0;
+        who[i] = (u64)(r0 + row) << 32 | (listed[i] ? column_of(listed[i]) + 1 : 0);
         largest = max(largest, mine[i]);
       }
-      mine[kEach] = tid < n ? best[tid].key : 0;
-      who[kEach] = tid < n ? best[tid].who : 0;
+      mine[kEach] = tid < n ? best_key[tid] : 0;
+      who[kEach] = tid < n ? best_who[tid] : 0;
       largest = max(largest, mine[kEach]);
       // Few entries are all ranked.  Of many, those that are at or above the k-th of the threads'
       // largest, in bins of a quarter of their distance to the best of all.
@@ -527,55 +519,71 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(BeamArgs p) {
       }
 #pragma unroll
       for (int i = 0; i <= kEach; ++i)
-        if (mine[i] && (limit == kBins || bin_of(top - score_of(mine[i])) <= limit)) entry[atomicAdd(&s_n, 1)] = {mine[i], who[i]};
+        if (mine[i] && (limit == kBins || bin_of(top - score_of(mine[i])) <= limit)) {
+          const int to = atomicAdd(&s_n, 1);
+          key[to] = mine[i];
+          who_of[to] = who[i];
+        }
       rank[tid] = 0;
       __syncthreads();
       const int came = s_n;
       int size = 64;
       while (size < came) size <<= 1;
       if (size <= THREADS) {
-        // a place is the number of better ones, counted by THREADS / size threads each
-        const int slices = THREADS / size, per = ((came + slices - 1) / slices + 7) & ~7;
-        const int e = tid & (size - 1), j0 = tid / size * per, j1 = min(came, j0 + per);
-        if (e < came && j0 < j1) {
-          const Entry x = entry[e];
-          int before = 0;
-          for (int j = j0; j < j1; j += 8) {
-            Entry y[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = entry[min(j + i, came - 1)];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) before += j + i < j1 && ahead_of(y[i].key, y[i].who, x.key, x.who);
-          }
-          if (before) atomicAdd(&rank[e], before);
-        }
+        // A place is the number of better ones, counted by THREADS / size threads each; equal
+        // scores, which are rare, are told apart behind that.
+        const int per = max(size / (THREADS / size), 8);          // in eights: no entry belongs to two threads' parts
+        const int e = tid & (size - 1), j0 = tid / size * per;
+        if (tid >= came && tid < size) key[tid] = 0;
         __syncthreads();
-        if (tid < came && rank[tid] < k) best[rank[tid]] = entry[tid];
+        const u64 x = key[e];
+        int before = 0, same = 0;
+        for (int j = j0; j < min(came, j0 + per); j += 8) {
+          u64 y[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) y[i] = key[(j + i) & (size - 1)];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            before += y[i] > x;
+            same += y[i] == x;
+          }
+        }
+        if (e < came && same > (e >= j0 && e < j0 + per))
+          for (int j = j0; j < min(came, j0 + per); ++j) before += key[j] == x && who_of[j] < who_of[e];
+        if (e < came && before) atomicAdd(&rank[e], before);
+        __syncthreads();
+        if (tid < came && rank[tid] < k) {
+          best_key[rank[tid]] = key[tid];
+          best_who[rank[tid]] = who_of[tid];
+        }
       } else {
-        for (int i = came + tid; i < size; i += THREADS) entry[i] = {0, ~0ull};
+        for (int i = came + tid; i < size; i += THREADS) key[i] = 0, who_of[i] = ~0ull;
         for (int sorted = 2; sorted <= size; sorted <<= 1)
           for (int step = sorted >> 1; step; step >>= 1) {
             __syncthreads();
             for (int i = tid; i < size / 2; i += THREADS) {
               const int x = 2 * i - (i & (step - 1)), y = x + step;
-              const Entry ex = entry[x], ey = entry[y];
-              if (ahead_of(ex.key, ex.who, ey.key, ey.who) == ((x & sorted) != 0)) {
-                entry[x] = ey;
-                entry[y] = ex;
+              const u64 kx = key[x], ky = key[y], wx = who_of[x], wy = who_of[y];
+              if (ahead_of(kx, wx, ky, wy) == ((x & sorted) != 0)) {
+                key[x] = ky, key[y] = kx;
+                who_of[x] = wy, who_of[y] = wx;
               }
             }
           }
         __syncthreads();
-        if (tid < min(came, k)) best[tid] = entry[tid];
+        if (tid < min(came, k)) {
+          best_key[tid] = key[tid];
+          best_who[tid] = who_of[tid];
+        }
       }
       n = min(came, k);
       __syncthreads();
       // lists at their end or behind the k-th are done
-      const Entry worst = n == k ? best[k - 1] : Entry{0, ~0ull};
+      const u64 worst = n == k ? best_key[k - 1] : 0, worst_who = n == k ? best_who[k - 1] : ~0ull;
 #pragma unroll
       for (int i = 0; i < kEach; ++i)
         if (from[i] >= 0 && next[i]) {
-          if (next[i] < 0 || ahead_of(worst.key, worst.who, mine[i], who[i])) len[from[i]] = 0;
+          if (next[i] < 0 || ahead_of(worst, worst_who, mine[i], who[i])) len[from[i]] = 0;
           else at[from[i]] = (short)next[i];
         }
     }
@@ -585,17 +593,17 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(BeamArgs p) {
   if (tid == 0) a.count[b] = n;
   for (int i = tid; i < k; i += THREADS) {
     const int64_t o = (int64_t)b * k + i;
-    const int r = i < n ? (int)(best[i].who >> 32) : -1, col = i < n ? (int)(unsigned)best[i].who - 1 : -1;
+    const int r = i < n ? (int)(best_who[i] >> 32) : -1, col = i < n ? (int)(unsigned)best_who[i] - 1 : -1;
     a.parent[o] = r < 0 ? -1 : a.row_id ? a.row_id[r] : r;
     a.token[o] = col < 0 ? -1 : a.token_base + col;
-    a.score_out[o] = r < 0 ? -INFINITY : (float)score_of(best[i].key);
+    a.score_out[o] = r < 0 ? -INFINITY : (float)score_of(best_key[i]);
   }
   if (!a.paths) return;
   for (int i = tid; i < k * a.max_path; i += THREADS) {
     const int j = i / a.max_path, s = i % a.max_path;
     int v = -1;
     if (j < n) {
-      const int r = (int)(best[j].who >> 32), col = (int)(unsigned)best[j].who - 1, id = a.row_id ? a.row_id[r] : r;
+      const int r = (int)(best_who[j] >> 32), col = (int)(unsigned)best_who[j] - 1, id = a.row_id ? a.row_id[r] : r;
       const bool known = (unsigned)id < (unsigned)a.n_paths;
       const int held = known ? min(max(a.path_len[id], 0), a.max_path) : 0;
       if (s < held) v = a.paths[(int64_t)id * a.max_path + s];

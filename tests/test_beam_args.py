@@ -30,7 +30,7 @@ def test_beam_refusals():
            (SHAPE, dict(logits_stride=499)), (INVALID, dict(n_paths=0)), (INVALID, dict(max_path=0)),
            (INVALID, dict(max_path=2 ** 16 + 1)), (INVALID, dict(score=P, score_out=P)),
            (INVALID, dict(paths=P, paths_out=P)), (INVALID, dict(path_len=P, path_len_out=P)),
-           (SHAPE, dict(n_rows=2 ** 24))]
+           (SHAPE, dict(n_rows=2 ** 27))]
     bad += nulls("logits", "row_off", "count", "parent", "token", "score_out", "path_len", "paths", "paths_out",
                  "path_len_out")
     refuse("atspeed_beam_select", bd.BeamSelectArgs, BEAM, bad, P, 1 << 40)
