@@ -383,10 +383,10 @@ __device__ __forceinline__ bool ahead_of(u64 key, u64 who, u64 than_key, u64 tha
   return (key > than_key) | ((key == than_key) & (who < than_who));
 }
 
-constexpr int kBins = 256;
-// The bin of a distance: its exponent and two bits of it, from 2^-24 to 2^40.
+constexpr int kBins = 1024;
+// The bin of a distance: its exponent and four bits of it, from 2^-24 to 2^40.
 __device__ __forceinline__ uint32_t bin_of(double d) {
-  const int b = (int)(__float_as_uint((float)d) >> 21) - ((127 - 24) << 2);
+  const int b = (int)(__float_as_uint((float)d) >> 19) - ((127 - 24) << 4);
   return (uint32_t)min(max(b, 0), kBins - 1);
 }
 
@@ -489,29 +489,29 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(BeamArgs p) {
       who[kEach] = tid < n ? best_who[tid] : 0;
       largest = max(largest, mine[kEach]);
       // Few entries are all ranked.  Of many, those that are at or above the k-th of the threads'
-      // largest, in bins of a quarter of their distance to the best of all.
+      // largest, in bins of a sixteenth of their distance to the best of all.
       uint32_t limit = kBins;
       double top = 0.0;
-      if (n_open << depth > THREADS) {
+      if (n_open << depth > 64) {
         u64 high = largest;
         static_for<6>([&](auto s) { high = max(high, (u64)partner<s>((uint32_t)(high >> 32)) << 32 | partner<s>((uint32_t)high)); });
         if (lane == 0) most[wave] = high;
-        if (tid < kBins) bin[tid] = 0;
+        for (int i = tid; i < kBins; i += THREADS) bin[i] = 0;
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) high = max(high, most[w]);
         top = score_of(high);
         if (largest) atomicAdd(&bin[bin_of(top - score_of(largest))], 1);
         __syncthreads();
-        // a lane has four bins: how many there are up to each
-        int upto[4];
+        // a lane has sixteen bins: how many there are up to each
+        int upto[kBins / 64];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) upto[i] = bin[lane * 4 + i] + (i ? upto[i - 1] : 0);
-        const int before = wave_scan(upto[3]) - upto[3];
+        for (int i = 0; i < kBins / 64; ++i) upto[i] = bin[lane * (kBins / 64) + i] + (i ? upto[i - 1] : 0);
+        const int before = wave_scan(upto[kBins / 64 - 1]) - upto[kBins / 64 - 1];
         int mine_limit = kBins;
 #pragma unroll
-        for (int i = 3; i >= 0; --i)
-          if (before + upto[i] >= k) mine_limit = lane * 4 + i;
+        for (int i = kBins / 64 - 1; i >= 0; --i)
+          if (before + upto[i] >= k) mine_limit = lane * (kBins / 64) + i;
         const u64 enough = __ballot(mine_limit < kBins);
         if (enough) limit = __builtin_amdgcn_readlane(mine_limit, __builtin_ctzll(enough));
       } else {
@@ -657,10 +657,11 @@ static atspeed_status check_beam(const atspeed_beam_select_args& a) {
   return ATSPEED_OK;
 }
 
-// Parts of a row: a wave each, enough waves for the card.
+// Parts of a row: a wave each, enough waves for the card, but not many more lists a request
+// than one round of the second kernel takes in.
 static void cut_rows(const atspeed_beam_select_args& a, BeamArgs& p) {
-  const int tiles = (a.n_cols + kTile - 1) / kTile, rows = std::max(a.n_rows, 1);
-  const int most = std::min(tiles, kJoinLists), want = std::min(most, (4096 + rows - 1) / rows);
+  const int tiles = (a.n_cols + kTile - 1) / kTile, rows = std::max(a.n_rows, 1), beams = (rows + a.B - 1) / a.B;
+  const int most = std::max(1, std::min(tiles, kJoinLists / 2 / beams)), want = std::min(most, (4096 + rows - 1) / rows);
   p.tiles = (tiles + want - 1) / want;
   p.parts = (tiles + p.tiles - 1) / p.tiles;
   while (1 << p.shift < p.parts) ++p.shift;
