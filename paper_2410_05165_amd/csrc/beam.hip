@@ -206,22 +206,27 @@ struct Pool {
 
   // Takes in a tile's columns above the bound (c: the lane's first one); k and 64 more have room.
   __device__ __forceinline__ void add(Tile<T> x, int c, int k, uint32_t high, int lane) {
-    u64 in[kLane];
-    int all = 0;
-#pragma unroll
-    for (int e = 0; e < kLane; ++e) {
-      in[e] = __ballot(x[e] > bound);
-      all += __popcll(in[e]);
-    }
-    if (n + all <= CAP) {
+    for (;;) {
+      x.here();
+      u64 in[kLane];
+      int all = 0;
 #pragma unroll
       for (int e = 0; e < kLane; ++e) {
-        if (!in[e]) continue;
-        if (in[e] >> lane & 1)
-          at[n + lanes_before(in[e])] = (u64)__float_as_uint(x[e]) << 32 | (uint32_t)(c + Tile<T>::column(0, e));
-        n += __popcll(in[e]);
+        in[e] = __ballot(x[e] > bound);
+        all += __popcll(in[e]);
       }
-      return;
+      if (n + all <= CAP) {
+#pragma unroll
+        for (int e = 0; e < kLane; ++e) {
+          if (!in[e]) continue;
+          if (in[e] >> lane & 1)
+            at[n + lanes_before(in[e])] = (u64)__float_as_uint(x[e]) << 32 | (uint32_t)(c + Tile<T>::column(0, e));
+          n += __popcll(in[e]);
+        }
+        return;
+      }
+      if (n <= k) break;
+      cut(k, high, lane);                       // few pass the bound that it leaves
     }
     // more than there is room for: 64 at a time, each against the bound that the last cut left
     for (int e = 0; e < kLane; ++e) {
