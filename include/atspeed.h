@@ -697,7 +697,7 @@ ATSPEED_API atspeed_status atspeed_logit_rules(const atspeed_logit_rules_args* a
  * 64 bits of the score, may rank either way).
  * A column of -infinity is no candidate.  A row that holds NaN or +infinity, or whose
  * score is not finite, has none.  A row with done[r] != 0 has ended: its only candidate
- * is itself, with score[r] and token -1; its logits are not read.
+ * is itself, with score[r] and token -1, whatever its logits hold.
  *   logits [n_rows, n_cols] in dtype (ATSPEED_FP32 or ATSPEED_BF16), rows logits_stride
  *     elements apart, at any element; rows past min(row_off[B], n_rows) are not used.
  *   score, done [n_rows] (nullable: 0, none).
@@ -833,10 +833,12 @@ ATSPEED_API atspeed_status atspeed_kv_compact(const atspeed_kv_compact_args* arg
  * logit is -infinity are no tops.  A row without tops, or of weight 0, has loss 0 and
  * gradient 0, whatever its logits hold; columns of logit -infinity have q_v = 0, and where
  * all are, q is 0.  The share of columns more than 2^126 below the largest counts as 0.
+ * NaN or +infinity in a row's logits, tops or tail makes its loss and gradient NaN.
  * Sums and statistics are fp32, what is summed over the tops 64 bits.
  *   logits [n_rows, n_cols], rows logits_stride elements apart, at any element;
  *   teacher_logit [n_rows, n_tops], both in dtype; teacher_index [n_rows, n_tops];
- *   tail, weight [n_rows] fp32 (weight nullable: 1); temperature positive.
+ *   tail, weight [n_rows] fp32 (weight nullable: 1); temperature and its reciprocal positive
+ *   and finite.
  *   loss [n_rows] fp32; saved [n_rows, 2 + n_tops] fp32: what atspeed_distill_grad reads.
  * n_rows from 0, n_cols 1..2^20, n_tops 1..256.  No output may overlap an input. */
 typedef struct {

@@ -120,29 +120,6 @@ __device__ __forceinline__ uint32_t kth_largest(uint32_t (&x)[N], int k, uint32_
   return t;
 }
 
-// The k-th largest of the lanes' numbers, k up to 64, by counting the larger ones (scratch: 64
-// words of LDS): 64 vector compares, where bit by bit costs a round trip to the scalar unit
-// for each (900 cycles to 2,900).
-__device__ __forceinline__ uint32_t kth_lane(uint32_t x, int k, uint32_t* scratch, int lane) {
-  wave_sync();
-  scratch[lane] = x;
-  wave_sync();
-  int ahead = 0;
-#pragma unroll
-  for (int j = 0; j < 64; j += 4) {
-    const u32x4_t y = *reinterpret_cast<const u32x4_t*>(scratch + j);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) ahead += y[i] > x;
-  }
-  wave_sync();
-  // equal numbers have the same count: the largest number with fewer than k ahead and k at least
-  // up to itself is the smallest with fewer than k ahead
-  const u64 in = __ballot(ahead < k);
-  uint32_t least = ahead < k ? x : 0xffffffffu;
-  static_for<6>([&](auto s) { least = min(least, partner<s>(least)); });
-  return in ? __builtin_amdgcn_readfirstlane(least) : 0;
-}
-
 // Lanes before this one with a set bit.
 __device__ __forceinline__ int lanes_before(u64 bits) {
   return __builtin_amdgcn_mbcnt_hi((uint32_t)(bits >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)bits, 0));
@@ -324,18 +301,12 @@ __global__ void __launch_bounds__(kBeamThreads) beam_rows_kernel(BeamArgs p) {
       }
     }
     if (tile == begin) {
-      // At least k columns are at or above the k-th of the lanes' largest, or of the largest of
-      // four groups a lane; of the latter, found bit by bit, the upper 16 bits.
-      uint32_t t;
-      if (k <= 32) {
-        t = kth_lane(order_of<T>(mine), k, reinterpret_cast<uint32_t*>(pool.at), lane);
-      } else {
-        uint32_t o[4];
+      // k of 256 groups' largest are at or above the k-th of them; its upper 16 bits
+      uint32_t o[4];
 #pragma unroll
-        for (int g = 0; g < 4; ++g) o[g] = order_of<T>(most[g]);
-        constexpr int STEPS = 4 * sizeof(T);
-        t = kth_largest<4>(o, k, 0u, STEPS - 1, STEPS - 8);
-      }
+      for (int g = 0; g < 4; ++g) o[g] = order_of<T>(most[g]);
+      constexpr int STEPS = 4 * sizeof(T);
+      const uint32_t t = kth_largest<4>(o, k, 0u, STEPS - 1, STEPS - 8);
       if (t > lowest + 1) {
         pool.least = ((u64)t << 32) - 1;
         pool.bound = logit_of<T>(t - (t == order_of<T>(0.f) ? 2 : 1));   // -0 is no number of its own

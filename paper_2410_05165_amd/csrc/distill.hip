@@ -101,7 +101,9 @@ __global__ void __launch_bounds__(THREADS) distill_loss_kernel(atspeed_distill_l
   t_top = tail;
 #pragma unroll
   for (int w = 0; w < WAVES; ++w) t_top = fmax(t_top, wave_top[w]);
-  const double w = mine >= 0 ? exp_below(t, t_top) : 0.0, w_rest = tail > -INFINITY ? exp_below(tail, t_top) : 0.0;
+  // NaN and +infinity among them go through to the loss, as those of the row's logits
+  const double w = mine < 0 ? 0.0 : t < INFINITY ? exp_below(t, t_top) : NAN;
+  const double w_rest = tail == -INFINITY ? 0.0 : tail < INFINITY ? exp_below(tail, t_top) : NAN;
   const double w_wave = wave_sum(w);
   if ((tid & 63) == 0) wave_all[wave] = w_wave;
   if (tid < m) share[tid] = w;
@@ -151,7 +153,7 @@ __global__ void __launch_bounds__(THREADS) distill_loss_kernel(atspeed_distill_l
   z_top = row_top[0];
 #pragma unroll
   for (int i = 1; i < WAVES; ++i) z_top = max_nan(z_top, row_top[i]);
-  const bool bad = !(z_top < INFINITY);            // NaN and +infinity go through to the loss
+  const bool bad = !(z_top < INFINITY);
   if (bad) z_top = NAN;
   double rest = 0.0, w_all = w_rest;
 #pragma unroll
@@ -265,21 +267,25 @@ static atspeed_status launch_loss(const atspeed_distill_loss_args& a, size_t lds
   HIP_TRY(hipGetLastError());
   return ATSPEED_OK;
 }
-// Long rows that do not fill the card four to a CU take workgroups of 1,024.
+// Rows longer than 16,384 columns that leave CUs empty take workgroups of 1,024 (us, of 256
+// and of 1,024: 16 rows of 131,072 bf16 columns 23.8 and 15.4, 64 of 33,024 10.5 and 9.0, 256 of
+// them 11.1 and 9.9; but 512 of them 13.5 and 17.0, 256 of 8,192 6.6 and 7.7).
 template <class T>
 static atspeed_status run_loss(const atspeed_distill_loss_args& a, size_t lds, float c, hipStream_t st) {
-  return a.n_cols >= 16384 && a.n_rows <= 1024 ? launch_loss<T, 1024>(a, lds, c, st) : launch_loss<T, 256>(a, lds, c, st);
+  return a.n_cols > 16384 && a.n_rows <= 256 ? launch_loss<T, 1024>(a, lds, c, st) : launch_loss<T, 256>(a, lds, c, st);
 }
+
+static float exponent_scale(float temperature) { return (float)(1.4426950408889634 / (double)temperature); }
 
 static atspeed_status check_distill(int dtype, int n_rows, int n_cols, int n_tops, float temperature) {
   if (dtype != ATSPEED_FP32 && dtype != ATSPEED_BF16) return fail(ATSPEED_E_INVALID, "dtype");
   if (n_rows < 0) return fail(ATSPEED_E_INVALID, "n_rows must be >= 0");
   if (n_cols < 1 || n_cols > (1 << 20)) return fail(ATSPEED_E_INVALID, "n_cols must be 1..2^20");
   if (n_tops < 1 || n_tops > kMaxTops) return fail(ATSPEED_E_INVALID, "n_tops must be 1..256");
-  if (!(temperature > 0.f) || !(temperature < INFINITY)) return fail(ATSPEED_E_INVALID, "temperature must be positive");
+  if (!(temperature > 0.f) || !(temperature < INFINITY) || !(exponent_scale(temperature) < INFINITY))
+    return fail(ATSPEED_E_INVALID, "temperature must be positive, its reciprocal finite");
   return ATSPEED_OK;
 }
-static float exponent_scale(float temperature) { return (float)(1.4426950408889634 / (double)temperature); }
 
 }  // namespace atspeed
 

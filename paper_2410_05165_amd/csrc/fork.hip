@@ -23,7 +23,10 @@ typedef unsigned long long u64;
 // their own for count, claim and decide (one workgroup), and write; one workgroup does it all
 // where there is little to do.
 constexpr int kForkThreads = 256, kForkOne = 1024;
-constexpr int kForkFew = 4096;       // entries of the tables, and pages, that one workgroup takes by itself
+// What one workgroup takes by itself: rows, and entries of the tables and pages (us, one launch
+// and three: 10 rows of 6 entries 6.3 and 13.4, 100 of 40 13.1 and 15.8; but 320 of 13 20.7 and
+// 15.8, 400 of 20 26.2 and 15.9).
+constexpr int kForkRows = 128, kForkFew = 4096;
 constexpr int kPieces = 1024;        // of the pool, at most
 constexpr int kRun = 8;              // consecutive rows of a thread that counts
 
@@ -206,7 +209,6 @@ template <class Row>
 __device__ __forceinline__ void write_piece(const ForkArgs& p, const Stack& s, int i, int lane, Row row) {
   const int begin = i * p.piece, end = min(begin + p.piece, p.a.n_pool);
   int at = s.F + fresh(&p.gone[i]);
-#pragma unroll 4
   for (int c0 = begin; c0 < end; c0 += 64) {
     const int c = c0 + lane, left = c < end ? fresh(&p.a.shared[c]) : 0;
     const u64 out = __ballot(left == -1);
@@ -230,7 +232,6 @@ __device__ __forceinline__ void write_row(const ForkArgs& p, const Stack& s, int
   const bool copies = rank > 0 && rank <= s.have, refused = rank > s.have;
   if (r.from >= 0 && r.from != j) {
     const int n = r.full + (r.over && !rank);
-#pragma unroll 4
     for (int c = lane; c < n; c += 64) p.a.block_table[(int64_t)j * most + c] = p.next[(int64_t)j * most + c];
   }
   if (lane) return;
@@ -450,7 +451,7 @@ atspeed_status atspeed_page_fork(const atspeed_page_fork_args* args, void* works
     return fail(ATSPEED_E_WORKSPACE, "page fork: workspace is too small or not 16-byte aligned");
   lay_out(p, (char*)workspace);
   const hipStream_t st = (hipStream_t)stream;
-  if (args->B * (long long)args->max_pages <= kForkFew && args->n_pool <= kForkFew) {
+  if (args->B <= kForkRows && args->B * (long long)args->max_pages <= kForkFew && args->n_pool <= kForkFew) {
     hipLaunchKernelGGL(fork_one_kernel, dim3(1), dim3(kForkOne), 0, st, p);
   } else {
     hipLaunchKernelGGL(fork_count_kernel, dim3((unsigned)count), dim3(kForkThreads), 0, st, p, columns);

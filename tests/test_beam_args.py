@@ -78,7 +78,7 @@ def test_distill_refusals():
     both = [(INVALID, dict(dtype=2)), (INVALID, dict(n_rows=-1)), (INVALID, dict(n_cols=0)), (INVALID, dict(n_cols=2 ** 20 + 1)),
             (INVALID, dict(n_tops=0)), (INVALID, dict(n_tops=257)), (INVALID, dict(temperature=0.0)),
             (INVALID, dict(temperature=-1.0)), (INVALID, dict(temperature=float("nan"))),
-            (INVALID, dict(temperature=float("inf"))), (SHAPE, dict(logits_stride=99)), (SHAPE, dict(n_rows=2 ** 24))]
+            (INVALID, dict(temperature=float("inf"))), (INVALID, dict(temperature=1e-40)), (SHAPE, dict(logits_stride=99)), (SHAPE, dict(n_rows=2 ** 24))]
     refuse("atspeed_distill_loss", bd.DistillLossArgs, LOSS,
            both + [(INVALID, dict(reverse=1, tail=None))] + nulls("logits", "teacher_logit", "teacher_index", "loss", "saved"))
     refuse("atspeed_distill_grad", bd.DistillGradArgs, GRAD,

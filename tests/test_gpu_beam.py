@@ -203,6 +203,42 @@ def test_rows_past_the_last_request_are_left_out():
     assert none.count.tolist() == [0, 0] and bool((none.parent == -1).all())
 
 
+@pytest.mark.parametrize("k", [3, 40, 130])
+@pytest.mark.parametrize("rows", [1, 70])
+def test_lists_that_need_several_rounds(k, rows):
+    """One beam has every candidate, far down in its parts' lists; the others have the next best heads."""
+    c = case(k + rows, [rows, 2], 20000, k, F32, ids=False)
+    c["logits"][0] = torch.linspace(3, 3.001, 20000, device=DEV)
+    c["score"][:] = -1.5
+    c["score"][0] = 4.0
+    check(c)
+    c["logits"][0, :2000] = 5.0                                # the first parts have equal ones
+    check(c)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("cols", [1024, 1025, 3000])
+def test_rising_and_falling_rows(dtype, cols):
+    """Every tile is better, or worse, than all before it: the pool is cut again and again, or never."""
+    c = case(cols, [4], cols, 30, dtype, ids=False)
+    v = torch.arange(cols, device=DEV).float()
+    c["logits"][0], c["logits"][1] = v / 64, -v / 64
+    c["logits"][2], c["logits"][3] = (v // 300) / 8, -(v // 300) / 8
+    check(c)
+    for k in (64, 65, 192, 193, 256):
+        check(dict(c, k=k))
+
+
+def test_scores_whose_order_hangs_on_the_last_bits():
+    """Beams of one distribution whose scores differ by one step of fp32: their candidates alternate in that order."""
+    c = case(31, [6], 500, 60, F32, ids=False)
+    c["logits"][:] = c["logits"][:1].clone()
+    for i in range(1, 6):
+        c["score"][i] = np.nextafter(c["score"][i - 1], np.float32(0), dtype=np.float32)
+    got = check(c)
+    assert got.parent[0, :6].tolist() == [5, 4, 3, 2, 1, 0]
+
+
 def test_offsets_past_32_bits():
     """Rows whose first element lies past 2^31 and 2^32 elements."""
     stride = (1 << 31) + 8
@@ -214,7 +250,7 @@ def test_offsets_past_32_bits():
 
 def test_repeats_bit_for_bit_on_streams_and_in_graphs():
     """Two calls that alternate on two streams and in two graphs equal their eager results."""
-    cases = [case(20 + i, [5, 9, 1], 9000 + i, 12, BF16, done=0.1, path=4) for i in range(2)]
+    cases = [case(20 + i, [5, 9, 1] if i else [5, 9], 9000 + i, 12 if i else 200, BF16, done=0.1, path=4) for i in range(2)]
     held = [dict(c, **{n: ints(c[n]) for n in ("row_off", "done", "row_id", "paths", "path_len")}, score=floats(c["score"]))
             for c in cases]
     want = [check(c) for c in cases]

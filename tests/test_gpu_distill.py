@@ -176,6 +176,29 @@ def test_nan_in_a_row_stays_in_it(dtype):
                 assert torch.equal(loss[r], clean_loss[r]) and torch.equal(grad[r], clean[r])
 
 
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("m", [7, 100])
+def test_a_teacher_that_is_no_number_makes_its_row_nan(bad, m):
+    for tail, reverse in FORMS:
+        c = case(10, 5, 900, m, F32, tail, reverse)
+        c["teacher_index"][1] = torch.arange(m, device=DEV) * 3
+        clean_loss, clean = check(c)
+        x = dict(c, teacher_logit=c["teacher_logit"].clone())
+        x["teacher_logit"][1, m - 1] = bad
+        rows = [1]
+        if tail:
+            x["tail"] = c["tail"].clone()
+            x["tail"][3] = bad
+            rows.append(3)
+        loss, saved = atspeed_distill_loss(**x)
+        grad = atspeed_distill_grad(x["logits"], x["teacher_index"], saved)
+        for r in range(5):
+            if r in rows:
+                assert math.isnan(float(loss[r])) and bool(torch.isnan(grad[r]).all())
+            else:
+                assert torch.equal(loss[r], clean_loss[r]) and torch.equal(grad[r], clean[r])
+
+
 def test_padded_teachers_may_hold_nan():
     c = case(10, 4, 400, 8)
     c["teacher_index"][:, 5:] = -1
@@ -316,6 +339,31 @@ def test_a_training_step_in_a_graph():
         want = step(eager)
         torch.cuda.synchronize()
         assert torch.equal(got, want) and torch.equal(graphed, eager)
+
+
+def test_rows_long_enough_to_need_more_lds_in_a_graph():
+    c = case(21, 3, 600_000, 30, BF16)
+    want = check(c)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        loss, saved = atspeed_distill_loss(**c)
+        grad = atspeed_distill_grad(c["logits"], c["teacher_index"], saved)
+    for _ in range(3):
+        loss.zero_(), grad.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(loss, want[0]) and torch.equal(grad, want[1])
+
+
+@pytest.mark.parametrize("m", [1, 64, 65, 256])
+@pytest.mark.parametrize("tail,reverse", FORMS)
+@pytest.mark.parametrize("rows", [2, 1200])
+def test_every_size_of_workgroup(m, tail, reverse, rows):
+    """Few long rows, many of them, tops of one wave and of several."""
+    c = case(22 + m, rows, 17000 if rows == 2 else 600, m, BF16, tail, reverse)
+    c["teacher_index"][0] = torch.arange(m, device=DEV).int() // 2       # every column twice
+    check(c)
 
 
 def test_offsets_past_32_bits():
