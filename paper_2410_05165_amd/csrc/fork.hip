@@ -320,8 +320,9 @@ __global__ void __launch_bounds__(kMoveThreads) page_copy_kernel(MoveArgs a) {
   }
 }
 
-// A workgroup a request and layer.  A thread moves its chunk of every token, in the path's
-// order: a place is written only behind the moves that read it, since path[i] >= i.
+// A workgroup a request and layer.  A thread moves its chunk of every token, eight tokens at a
+// time in the path's order: a place is written only behind the moves that read it, since
+// path[i] >= i.
 constexpr int kMaxPath = 4096;
 
 __global__ void __launch_bounds__(kMoveThreads) kv_compact_kernel(MoveArgs a) {
@@ -357,8 +358,14 @@ __global__ void __launch_bounds__(kMoveThreads) kv_compact_kernel(MoveArgs a) {
     auto at = [&](int slot) {
       return reinterpret_cast<u32x4_t*>(base + (int64_t)(slot >> a.page_shift) * p.page + (int64_t)(slot & tail) * p.token);
     };
-    for (int i = 0; i < n; ++i)
-      if (from[i] != to[i]) *at(to[i]) = *at(from[i]);
+    for (int i0 = 0; i0 < n; i0 += 8) {
+      u32x4_t x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = *at(from[min(i0 + i, n - 1)]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i0 + i < n && from[i0 + i] != to[i0 + i]) *at(to[i0 + i]) = x[i];
+    }
   }
 }
 
