@@ -394,11 +394,17 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(BeamArgs p) {
       const bool ended = a.done && a.done[r];
       double all = -INFINITY, total = 0.0;
       for (int q = l; q < 1 << shift; q += lanes) {
-        const bool in = q < parts && !ended;
-        const double2 st = in ? p.stat[(int64_t)r * parts + q] : double2{-INFINITY, 0.0};
+        // asked for before it is known whether the row has ended, and then left alone
+        double2 st = {-INFINITY, 0.0};
+        int length = 0;
+        if (q < parts) {
+          st = p.stat[(int64_t)r * parts + q];
+          length = p.len[(int64_t)r * parts + q];
+        }
+        if (ended) st = {-INFINITY, 0.0};
         if (i < rows) {
           at[i << shift | q] = 0;
-          len[i << shift | q] = in ? (short)p.len[(int64_t)r * parts + q] : ended && q == 0 ? kItself : 0;
+          len[i << shift | q] = !ended ? (short)length : q == 0 ? kItself : 0;
         }
         // NaN stays; a part whose largest logit is -infinity has nothing to add
         const double now = st.x > all ? st.x : all, add = st.x > -INFINITY ? st.y : st.x == -INFINITY ? 0.0 : NAN;
@@ -567,28 +573,30 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(BeamArgs p) {
   __syncthreads();
 
   if (tid == 0) a.count[b] = n;
+  int* const id_of = reinterpret_cast<int*>(key);   // [k] what parent names an entry's row by
+  int* const held_of = id_of + kMaxBeams;           // [k] the length of its path
   for (int i = tid; i < k; i += THREADS) {
     const int64_t o = (int64_t)b * k + i;
     const int r = i < n ? (int)(best_who[i] >> 32) : -1, col = i < n ? (int)(unsigned)best_who[i] - 1 : -1;
-    a.parent[o] = r < 0 ? -1 : a.row_id ? a.row_id[r] : r;
+    const int id = r < 0 ? -1 : a.row_id ? a.row_id[r] : r;
+    a.parent[o] = id;
     a.token[o] = col < 0 ? -1 : a.token_base + col;
     a.score_out[o] = r < 0 ? -INFINITY : (float)score_of(best_key[i]);
+    if (a.paths) {
+      const bool known = r >= 0 && (unsigned)id < (unsigned)a.n_paths;
+      const int held = known ? min(max(a.path_len[id], 0), a.max_path) : 0;
+      a.path_len_out[o] = held + (col >= 0 && held < a.max_path);
+      id_of[i] = id;
+      held_of[i] = held;
+    }
   }
   if (!a.paths) return;
+  __syncthreads();
   for (int i = tid; i < k * a.max_path; i += THREADS) {
-    const int j = i / a.max_path, s = i % a.max_path;
-    int v = -1;
-    if (j < n) {
-      const int r = (int)(best_who[j] >> 32), col = (int)(unsigned)best_who[j] - 1, id = a.row_id ? a.row_id[r] : r;
-      const bool known = (unsigned)id < (unsigned)a.n_paths;
-      const int held = known ? min(max(a.path_len[id], 0), a.max_path) : 0;
-      if (s < held) v = a.paths[(int64_t)id * a.max_path + s];
-      else if (s == held && col >= 0) v = a.token_base + col;
-      if (s == 0) a.path_len_out[(int64_t)b * k + j] = held + (col >= 0 && held < a.max_path);
-    } else if (s == 0) {
-      a.path_len_out[(int64_t)b * k + j] = 0;
-    }
-    a.paths_out[((int64_t)b * k + j) * a.max_path + s] = v;
+    const int j = i / a.max_path, s = i % a.max_path, held = held_of[j];
+    const int col = j < n ? (int)(unsigned)best_who[j] - 1 : -1;
+    const int there = a.paths[s < held ? (int64_t)id_of[j] * a.max_path + s : 0];
+    a.paths_out[((int64_t)b * k + j) * a.max_path + s] = s < held ? there : s == held && col >= 0 ? a.token_base + col : -1;
   }
 }
 
