@@ -5,10 +5,10 @@
 // and leaves the normaliser's sum and the k best logits of each part of a row; a second one
 // ranks a request's lists by score[r] - log sum + logit.
 //
-// Scores of different beams are compared, so the normaliser must not move them past each
-// other: it is taken in 64 bits (exponentials to 2.4e-10), where fp32 exponentials (1e-7 of the sum)
-// would swap one pair of neighbours in some thousand lists.  64-bit vector instructions
-// run at the rate of 32-bit ones here.
+// Scores of different beams are compared, so their normalisers must not move them past each
+// other.  They are taken in 64 bits, the exponentials to 2.4e-10: fp32 ones, off by 1e-7, would
+// leave to chance which of two candidates that close comes first.  A 64-bit vector instruction
+// takes the time of a 32-bit one here (1.8 ns a wave and SIMD), an fp32 exponential that of two.
 #include <algorithm>
 #include <cmath>
 
@@ -248,7 +248,12 @@ struct BeamArgs {
 };
 
 // A wave takes a part of a row by itself, tile by tile: the running maximum and 64-bit sum
-// of its exponentials, and its k best columns behind a bound that rises with them.
+// of its exponentials, and its k best columns behind a bound that rises with them.  No barrier,
+// and the whole row where there are rows enough: parts cost a pool and a first bound each.
+// Bound by vector instructions, of which a tile's exponentials are half and the selection,
+// which grows with k, a quarter: 5,661 rows of 33,024 bf16 columns with 50 beams each 190 us
+// (374 MB, 2.0 TB/s; with 10 beams 170, without exponentials or selection 80), 287 rows with 10
+// 17.5.  A workgroup per row with a sorted pool took 393 and 39.
 template <class T, int P, bool PROBS>
 __global__ void __launch_bounds__(kBeamThreads) beam_rows_kernel(BeamArgs p) {
   __shared__ u64 keys[kBeamWaves * P * 64];
@@ -286,7 +291,6 @@ __global__ void __launch_bounds__(kBeamThreads) beam_rows_kernel(BeamArgs p) {
       top = now;
       high = __builtin_amdgcn_readfirstlane(order_of<T>(top));
     }
-    x.here();
     if (!PROBS && top > -INFINITY) {
       // the exponential wants finite differences: where there are others, they are held at what
       // leaves nothing
@@ -350,7 +354,8 @@ __global__ void __launch_bounds__(kBeamThreads) beam_rows_kernel(BeamArgs p) {
 // A workgroup a request.  Rounds: every list that may still count gives its next few
 // entries, as many as the workgroup holds; the k-th of the threads' largest is a bound that
 // few more than k of them pass; these are ranked, the k best stay.  A list is left once its
-// last entry is behind them.  Mostly one round or two.
+// last entry is behind them.  Mostly one round or two.  Bound by latency, a chain of loads and
+// barriers: ten lists of ten 7.3 us, 32 requests of 99 lists of ten 10.5, 128 of 45 lists of 50 15.
 constexpr int kEach = 4, kJoinLists = 1024;
 constexpr short kItself = -1;              // length of the list of a row that has ended
 
@@ -611,7 +616,9 @@ static atspeed_status launch_join(const BeamArgs& p, hipStream_t st) {
 }
 template <class T>
 static atspeed_status run_join(const BeamArgs& p, hipStream_t st) {
-  // few entries a request or many requests: smaller workgroups, more of them on a CU
+  // Few entries a request, or many requests: smaller workgroups, more of them on a CU (both
+  // kernels, us, 256 threads and 1,024: 10 rows of 1,024 columns 12.7 and 15.7, 32 requests of 9
+  // rows of 33,024 with 10 beams 26.4 and 28.4; but 128 of 45 rows with 50 250 and 224).
   const long long entries = (long long)p.a.n_rows * p.parts * p.a.k;
   return p.a.B > 256 || entries <= 1024LL * p.a.B ? launch_join<T, 256>(p, st) : launch_join<T, 1024>(p, st);
 }
@@ -642,7 +649,9 @@ static atspeed_status check_beam(const atspeed_beam_select_args& a) {
 }
 
 // Parts of a row: a wave each, enough waves for the card, but not many more lists a request
-// than one round of the second kernel takes in.
+// than one round of the second kernel takes in (64 rows of one request, 128 beams: parts of one
+// tile 107 us, of three 63; 287 rows of 32 requests: 7 parts 27.2, 11 26.4, 17 30.0; 5,661 rows:
+// 1 part 216, 2 222).
 static void cut_rows(const atspeed_beam_select_args& a, BeamArgs& p) {
   const int tiles = (a.n_cols + kTile - 1) / kTile, rows = std::max(a.n_rows, 1), beams = (rows + a.B - 1) / a.B;
   const int most = std::max(1, std::min(tiles, kJoinLists / 2 / beams)), want = std::min(most, (4096 + rows - 1) / rows);

@@ -46,6 +46,9 @@ __device__ __forceinline__ double sum_tops(double x, bool one_wave, double* part
 
 // A workgroup a row.  Three barriers for up to 64 tops: the tops' bits and the teacher's
 // largest logit, the teacher's sum, the row's largest and sum; then the tops' wave is alone.
+// Bound by memory: 8,192 rows of 33,024 fp32 columns (1.08 GB) 232 us, 4.7 TB/s; 2,048 bf16 ones
+// (135 MB) 32; 640 rows of 1,024 6.4, where it is the chain of loads, barriers and logarithms
+// (with a barrier for every sum 271, 42 and 10.4).
 template <class T, int THREADS>
 __global__ void __launch_bounds__(THREADS) distill_loss_kernel(atspeed_distill_loss_args a, float c) {
   constexpr int VEC = 16 / sizeof(T), WAVES = THREADS / 64, STEP = THREADS * VEC;
@@ -218,7 +221,8 @@ __global__ void __launch_bounds__(THREADS) distill_loss_kernel(atspeed_distill_l
   }
 }
 
-// A workgroup a row and 4,096 columns.
+// A workgroup a row and 4,096 columns.  Bound by memory: 8,192 rows of 33,024 fp32 columns
+// (2.16 GB) 384 us, 2,048 bf16 ones (270 MB) 43.
 constexpr int kDistThreads = 256;
 constexpr int kGradVecs = 16;   // columns a thread
 
