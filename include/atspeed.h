@@ -757,8 +757,9 @@ ATSPEED_API atspeed_status atspeed_beam_select(const atspeed_beam_select_args* a
  *   copy_src, copy_dst, copy_len [B]: the pages to copy; -1, -1 and 0 where there are none
  * block_table [B, max_pages], free_pages [n_pool], n_free [1] and shared are updated in
  * place; table entries from ceil(length / page_size) on and free_pages from n_free on are
- * undefined.  Table entries outside 0 .. n_pool - 1 are handed on and otherwise ignored.  No
- * output may overlap an input.  B, page_size, n_pool and B * max_pages as for
+ * undefined.  Table entries outside 0 .. n_pool - 1 are handed on and otherwise ignored; a page
+ * that rows hold more often than shared says goes back once, with what that does to those who
+ * still hold it.  No output may overlap an input.  B, page_size, n_pool and B * max_pages as for
  * atspeed_page_plan.  workspace as for atspeed_tree_attention. */
 typedef struct {
   int32_t B, page_size, max_pages, n_pool;

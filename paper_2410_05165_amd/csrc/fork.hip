@@ -14,10 +14,10 @@ typedef unsigned long long u64;
 // before:
 //   count   shared[page] loses one for each old entry and gains one for each new full one; the
 //           new tables are put down beside the old ones, which other rows still read,
-//   claim   a last page that is left without a holder (-1) goes to the lowest row that wants
-//           it,
+//   claim   a last page that is left without a holder (-1; below it where rows held the page
+//           more often than shared said) goes to the lowest row that wants it,
 //   decide  the other rows that want one copy; they are numbered, and so are the pages that
-//           come free (-1) in pieces of the pool,
+//           come free (below 0) in pieces of the pool,
 //   write   tables, holders, free list.
 // Sums and minima of whole numbers: the order of the atomics changes nothing.  Launches of
 // their own for count, claim and decide (one workgroup), and write; one workgroup does it all
@@ -171,7 +171,7 @@ __device__ __forceinline__ void decide(const ForkArgs& p) {
     }
 #pragma unroll
     for (int o = 0; o < 8; ++o) {
-      const int n = __popcll(__ballot(left[o] == -1));
+      const int n = __popcll(__ballot(left[o] < 0));
       if (n && lane == 0) atomicAdd(&gone[(c0 + o * (kForkOne / 64)) * 64 / p.piece], n);
     }
   }
@@ -213,8 +213,8 @@ __device__ __forceinline__ void write_piece(const ForkArgs& p, const Stack& s, i
   int at = s.F + fresh(&p.gone[i]);
   for (int c0 = begin; c0 < end; c0 += 64) {
     const int c = c0 + lane, left = c < end ? fresh(&p.a.shared[c]) : 0;
-    const u64 out = __ballot(left == -1);
-    if (left == -1) {
+    const u64 out = __ballot(left < 0);
+    if (left < 0) {
       p.a.shared[c] = 0;
       const int place = at + __popcll(out & ((1ull << lane) - 1));
       if (place < s.top) {

@@ -89,7 +89,7 @@ def fork(held, keep, table, free, n_free, shared, page, src=None):
     for p in sorted(set(old)):
         left = outside[p] + stays[p] + (p in taken)
         shared[p] = max(left, 0)
-        if left < 0:
+        if left < 0 and p not in taken:
             gone.append(p)
     stack = [int(p) for p in free[:n_free]] + gone
     copies = [(-1, -1, 0)] * B

@@ -103,6 +103,54 @@ def test_dropping_tokens_without_a_fork(seed):
     check_fork(c, 8, with_src=False, with_keep=False)        # nothing changes
 
 
+@pytest.mark.parametrize("rows,pool", [(3, 5), (3, 700), (200, 600)])
+def test_pages_held_more_often_than_counted(rows, pool):
+    """They are counted below -1: taken once, or back once, and the pages behind keep their places in the free list."""
+    table = np.full((rows, 2), -1)
+    table[:, 0] = 0
+    table[0, 1], table[1, 1] = pool - 1, pool - 1            # dropped by both, in the pool's last piece
+    held = np.full(rows, 4)
+    held[:2] = 8
+    free = np.full(pool, -1)
+    shared = np.zeros(pool, np.int64)
+    src = np.full(rows, -1)
+    src[2] = 2                                               # goes on with part of page 0, which is its own now
+    keep = np.where(src < 0, 0, 3)
+    for n_free in (0, 1):
+        free[:n_free] = 1
+        got = check_fork((held, keep, table, free, n_free, shared, src), 4)
+        assert got.copy_dst.tolist() == [-1] * rows and got.length.tolist() == [3 if j == 2 else 0 for j in range(rows)]
+
+
+@pytest.mark.parametrize("rows,most,pool", [(8, 5, 60), (300, 5, 1500), (300, 5, 400)])
+@pytest.mark.parametrize("seed", range(4))
+def test_whatever_shared_holds_nothing_leaves_its_buffer(rows, most, pool, seed):
+    rng = np.random.default_rng(seed)
+    page, edge = 4, 64
+    held = rng.integers(0, most * page + 1, rows)
+    src = rng.integers(-1, rows, rows)
+    keep = rng.integers(0, np.where(src < 0, 0, held[np.maximum(src, 0)]) + 1)
+    shared = rng.integers(-3, 4, pool)
+    shared[rng.integers(0, pool, 3)] = [-2**31, 2**31 - 1, -2**31 + 1]
+    table = rng.integers(0, pool, (rows, most))
+    n_free = int(rng.integers(0, pool + 1))
+
+    def inside(a):
+        whole = torch.full((a.size + 2 * edge,), -77, dtype=torch.int32, device=DEV)
+        whole[edge:edge + a.size] = ints(a).view(-1)
+        return whole, whole[edge:edge + a.size].view(a.shape)
+
+    (t_all, t), (f_all, f), (s_all, s) = inside(table), inside(rng.permutation(pool)), inside(shared)
+    n_all, n = inside(np.array([n_free]))
+    got = atspeed_page_fork(ints(held), ints(keep), t, f, n, s, page, src=ints(src))
+    for whole, size in ((t_all, rows * most), (f_all, pool), (s_all, pool), (n_all, 1)):
+        assert bool((whole[:edge] == -77).all()) and bool((whole[edge + size:] == -77).all())
+    left = int(n)
+    assert 0 <= left <= pool and all(0 <= p < pool for p in f.tolist()) and all(0 <= p < pool for p in t.view(-1).tolist())
+    for j, (length, dst, size) in enumerate(zip(got.length.tolist(), got.copy_dst.tolist(), got.copy_len.tolist())):
+        assert 0 <= length <= most * page and -1 <= dst < pool and 0 <= size < page
+
+
 @pytest.mark.parametrize("seed", range(12))
 def test_fork_with_too_few_pages_and_malformed_rows(seed):
     rng = np.random.default_rng(seed)
