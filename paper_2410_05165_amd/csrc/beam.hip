@@ -617,8 +617,8 @@ static atspeed_status launch_join(const BeamArgs& p, hipStream_t st) {
 template <class T>
 static atspeed_status run_join(const BeamArgs& p, hipStream_t st) {
   // Few entries a request, or many requests: smaller workgroups, more of them on a CU (both
-  // kernels, us, 256 threads and 1,024: 10 rows of 1,024 columns 12.7 and 15.7, 32 requests of 9
-  // rows of 33,024 with 10 beams 26.4 and 28.4; but 128 of 45 rows with 50 250 and 224).
+  // kernels, us, 256 threads and 1,024: 10 rows of 1,024 columns 12.4 and 15.9, 32 requests of 9
+  // rows of 33,024 with 10 beams 26.6 and 28.4; but 128 of 45 rows with 50 220 and 189).
   const long long entries = (long long)p.a.n_rows * p.parts * p.a.k;
   return p.a.B > 256 || entries <= 1024LL * p.a.B ? launch_join<T, 256>(p, st) : launch_join<T, 1024>(p, st);
 }
@@ -650,8 +650,8 @@ static atspeed_status check_beam(const atspeed_beam_select_args& a) {
 
 // Parts of a row: a wave each, enough waves for the card, but not many more lists a request
 // than one round of the second kernel takes in (64 rows of one request, 128 beams: parts of one
-// tile 107 us, of three 63; 287 rows of 32 requests: 7 parts 27.2, 11 26.4, 17 30.0; 5,661 rows:
-// 1 part 216, 2 222).
+// tile 113 us, of two 89, of five 67; 287 rows of 32 requests: 7 parts 27.6, 11 26.6, 17 27.9;
+// 5,661 rows: 1 part 189, 2 197).
 static void cut_rows(const atspeed_beam_select_args& a, BeamArgs& p) {
   const int tiles = (a.n_cols + kTile - 1) / kTile, rows = std::max(a.n_rows, 1), beams = (rows + a.B - 1) / a.B;
   const int most = std::max(1, std::min(tiles, kJoinLists / 2 / beams)), want = std::min(most, (4096 + rows - 1) / rows);
