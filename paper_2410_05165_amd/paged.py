@@ -216,6 +216,7 @@ class PagedKV:
     def compact(self, plan: StepPlan, path, n_path):
         """Moves each request's accepted rows path[b][:n_path[b]] of the plan behind its context, in every layer.
 
+        The row numbers ascend strictly, as those down a tree do; a path that does not moves nothing.
         Returns what the next plan keeps: the context and the path (the context alone where n_path is below 1 or the
         request was refused: then its length).
         """
