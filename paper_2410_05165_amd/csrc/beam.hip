@@ -22,6 +22,7 @@ constexpr int kBeamThreads = 256, kBeamWaves = kBeamThreads / 64;
 constexpr int kLane = 16;              // columns of a lane in a tile
 constexpr int kTile = 64 * kLane;      // columns of a tile, which a wave takes at once
 constexpr int kMaxBeams = 256;         // k
+constexpr int kSlots = 4096;           // waves on the card at once, four a SIMD
 
 // Logits (no NaN) to whole numbers of the same order and as many bits, -0 as 0; and back.
 template <class T>
@@ -241,25 +242,28 @@ __device__ __forceinline__ void add_exps(double& sum, float top, F x) {
 
 struct BeamArgs {
   atspeed_beam_select_args a;
-  u64* list;        // [n_rows, parts, k] the best columns, best first
-  double2* stat;    // [n_rows, parts] largest logit and sum of exponentials; NaN: the row has no candidates
-  int* len;         // [n_rows, parts]
-  int parts, tiles, shift; // parts of a row, tiles of a part; parts <= 1 << shift
+  u64* list;        // [lists, k] the best columns, best first: a list a row, from row `whole` on `parts` a row
+  double2* stat;    // [lists] largest logit and sum of exponentials; NaN: the row has no candidates
+  int* len;         // [lists]
+  int whole, parts, tiles, shift; // tiles of a part; parts <= 1 << shift
+
+  __host__ __device__ int64_t list_of(int r) const { return r < whole ? r : whole + (int64_t)(r - whole) * parts; }
 };
 
 // A wave takes a part of a row by itself, tile by tile: the running maximum and 64-bit sum
 // of its exponentials, and its k best columns behind a bound that rises with them.  No barrier,
-// and the whole row where there are rows enough: parts cost a pool and a first bound each.
+// and the whole row where that fills the card: parts cost a pool and a first bound each.
 // Bound by vector instructions, of which a tile's exponentials are half and the selection,
-// which grows with k, a quarter: 5,661 rows of 33,024 bf16 columns with 50 beams each 190 us
-// (374 MB, 2.0 TB/s; with 10 beams 170, without exponentials or selection 80), 287 rows with 10
+// which grows with k, a quarter: 5,661 rows of 33,024 bf16 columns with 50 beams each 184 us
+// (374 MB, 2.0 TB/s; with 10 beams 160, without exponentials or selection 80), 287 rows with 10
 // 17.5.  A workgroup per row with a sorted pool took 393 and 39.
 template <class T, int P, bool PROBS>
 __global__ void __launch_bounds__(kBeamThreads) beam_rows_kernel(BeamArgs p) {
   __shared__ u64 keys[kBeamWaves * P * 64];
   const atspeed_beam_select_args& a = p.a;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int q = blockIdx.x * kBeamWaves + wave, r = q / p.parts, part = q % p.parts;
+  const int q = blockIdx.x * kBeamWaves + wave, cut = max(q - p.whole, 0), part = cut % p.parts;
+  const int r = min(q, p.whole) + cut / p.parts;
   if (r >= a.n_rows) return;
   const int k = a.k, n_cols = a.n_cols;
   const T* row = static_cast<const T*>(a.logits) + (int64_t)r * a.logits_stride;
@@ -269,7 +273,7 @@ __global__ void __launch_bounds__(kBeamThreads) beam_rows_kernel(BeamArgs p) {
   double sum = 0.0;
   uint32_t high = 0;
 
-  const int begin = part * p.tiles, end = min(begin + p.tiles, (n_cols + kTile - 1) / kTile);
+  const int tiles = (n_cols + kTile - 1) / kTile, begin = part * p.tiles, end = q < p.whole ? tiles : min(begin + p.tiles, tiles);
   // the last tile of a row ends with it and drops what the one before had
   const int last = n_cols - kTile;
   Tile<T> x, next;
@@ -355,7 +359,8 @@ __global__ void __launch_bounds__(kBeamThreads) beam_rows_kernel(BeamArgs p) {
 // entries, as many as the workgroup holds; the k-th of the threads' largest is a bound that
 // few more than k of them pass; these are ranked, the k best stay.  A list is left once its
 // last entry is behind them.  Mostly one round or two.  Bound by latency, a chain of loads and
-// barriers: ten lists of ten 7.3 us, 32 requests of 99 lists of ten 10.5, 128 of 45 lists of 50 15.
+// barriers: ten lists of ten 7.3 us, 32 requests of 99 lists of ten 10.5, 128 of 45
+// rows, a third of them in three parts, 19.
 constexpr int kEach = 4, kJoinLists = 1024;
 constexpr short kItself = -1;              // length of the list of a row that has ended
 
@@ -383,7 +388,7 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(BeamArgs p) {
   __shared__ u64 best_key[kMaxBeams], best_who[kMaxBeams], most[WAVES];
   __shared__ int bin[kBins], rank[THREADS], s_n, s_open[2];
   const atspeed_beam_select_args& a = p.a;
-  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, k = a.k, parts = p.parts, shift = p.shift;
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, k = a.k, shift = p.shift;
   const int r1 = min(min(a.row_off[b + 1], a.row_off[a.B]), a.n_rows);   // rows that the first kernel read
   const int group = kJoinLists >> shift;           // lists: row << shift | part
   int n = 0;                                       // best_key[0 .. n) are the best so far, in order
@@ -397,14 +402,15 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(BeamArgs p) {
       const int i = i0 + (tid >> wide), r = min(r0 + i, r1 - 1), l = tid & (lanes - 1);
       const double score = a.score ? (double)a.score[r] : 0.0;
       const bool ended = a.done && a.done[r];
+      const int parts = r < p.whole ? 1 : p.parts;
       double all = -INFINITY, total = 0.0;
       for (int q = l; q < 1 << shift; q += lanes) {
         // asked for before it is known whether the row has ended, and then left alone
         double2 st = {-INFINITY, 0.0};
         int length = 0;
         if (q < parts) {
-          st = p.stat[(int64_t)r * parts + q];
-          length = p.len[(int64_t)r * parts + q];
+          st = p.stat[p.list_of(r) + q];
+          length = p.len[p.list_of(r) + q];
         }
         if (ended) st = {-INFINITY, 0.0};
         if (i < rows) {
@@ -462,7 +468,7 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(BeamArgs p) {
         const bool in = e >> depth < n_open && j < n_here;
         from[i] = in ? l : -1;
         next[i] = j + 1 >= n_here ? -1 : d + 1 == 1 << depth ? j + 1 : 0;
-        listed[i] = in && length != kItself ? p.list[((int64_t)(r0 + (l >> shift)) * parts + (l & ((1 << shift) - 1))) * k + j] : 0;
+        listed[i] = in && length != kItself ? p.list[(p.list_of(r0 + (l >> shift)) + (l & ((1 << shift) - 1))) * k + j] : 0;
       }
 #pragma unroll
       for (int i = 0; i < kEach; ++i) {
@@ -619,7 +625,7 @@ static atspeed_status run_join(const BeamArgs& p, hipStream_t st) {
   // Few entries a request, or many requests: smaller workgroups, more of them on a CU (both
   // kernels, us, 256 threads and 1,024: 10 rows of 1,024 columns 12.4 and 15.9, 32 requests of 9
   // rows of 33,024 with 10 beams 26.6 and 28.4; but 128 of 45 rows with 50 220 and 189).
-  const long long entries = (long long)p.a.n_rows * p.parts * p.a.k;
+  const long long entries = p.list_of(p.a.n_rows) * p.a.k;
   return p.a.B > 256 || entries <= 1024LL * p.a.B ? launch_join<T, 256>(p, st) : launch_join<T, 1024>(p, st);
 }
 
@@ -650,18 +656,23 @@ static atspeed_status check_beam(const atspeed_beam_select_args& a) {
 
 // Parts of a row: a wave each, enough waves for the card, but not many more lists a request
 // than one round of the second kernel takes in (64 rows of one request, 128 beams: parts of one
-// tile 113 us, of two 89, of five 67; 287 rows of 32 requests: 7 parts 27.6, 11 26.6, 17 27.9;
-// 5,661 rows: 1 part 189, 2 197).
+// tile 113 us, of two 89, of five 67; 287 rows of 32 requests: 7 parts 27.6, 11 26.6, 17 27.9).
+// As many rows as fill the card whole are not cut; few waves behind them would leave it half
+// empty, so that those rows are (both kernels, us, with them in 1 part, 2 and 3: 4,300 rows 162,
+// 144 and 139, 5,661 185, 184 and 177; 7,000 217, 215 and 221, 8,100 240, 249 and 255; all of
+// 5,661 rows in 2: 4% slower).
 static void cut_rows(const atspeed_beam_select_args& a, BeamArgs& p) {
   const int tiles = (a.n_cols + kTile - 1) / kTile, rows = std::max(a.n_rows, 1), beams = (rows + a.B - 1) / a.B;
-  const int most = std::max(1, std::min(tiles, kJoinLists / 2 / beams)), want = std::min(most, (4096 + rows - 1) / rows);
+  p.whole = rows / kSlots * kSlots;
+  const int rest = std::max(rows - p.whole, 1), most = std::max(1, std::min(tiles, kJoinLists / 2 / beams));
+  const int want = std::min(most, std::max(1, (kSlots + rest / 2) / rest));
   p.tiles = (tiles + want - 1) / want;
   p.parts = (tiles + p.tiles - 1) / p.tiles;
   while (1 << p.shift < p.parts) ++p.shift;
 }
 
 static size_t lay_out(BeamArgs& p, char* base) {
-  const size_t lists = (size_t)std::max(p.a.n_rows, 1) * p.parts;
+  const size_t lists = p.list_of(std::max(p.a.n_rows, 1));
   size_t at = 0;
   auto take = [&](size_t bytes) {
     char* q = base ? base + at : nullptr;
@@ -711,7 +722,7 @@ atspeed_status atspeed_beam_select(const atspeed_beam_select_args* args, void* w
   BeamArgs p{};
   p.a = *args;
   cut_rows(*args, p);
-  const long long groups = ((long long)args->n_rows * p.parts + kBeamWaves - 1) / kBeamWaves;
+  const long long groups = (p.list_of(args->n_rows) + kBeamWaves - 1) / kBeamWaves;
   if (groups > kMaxGroups) return fail(ATSPEED_E_SHAPE, "beam select: too many rows x columns");
   const size_t need = lay_out(p, nullptr);
   if (!workspace || !aligned16(workspace) || ws_bytes < need)

@@ -173,6 +173,13 @@ def test_many_rows(counts, cols, k):
     check(case(len(counts), counts, cols, k, F32, masked=0.3))
 
 
+@pytest.mark.parametrize("counts,cols,k,log_probs", [([7] * 600, 2100, 10, False), ([7] * 600, 2100, 70, True), ([9] * 456 + [1] * 3, 1500, 5, False),
+                                                     ([4] * 1024, 1100, 4, False), ([4100], 1100, 20, False)])
+def test_more_rows_than_waves_on_the_card(counts, cols, k, log_probs):
+    """4,096 rows go to a wave each, those behind them in parts; one request has rows of both sorts."""
+    check(case(cols + k, counts, cols, k, BF16, done=0.05, log_probs=log_probs, path=3))
+
+
 def test_without_scores_and_names():
     c = case(6, [3, 2], 400, 7, F32, ids=False, path=2)
     check(dict(c, score=None))
