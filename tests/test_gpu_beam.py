@@ -236,6 +236,22 @@ def test_rising_and_falling_rows(dtype, cols):
         check(dict(c, k=k))
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("k", [20, 55, 56, 57, 64, 103, 104, 105, 160, 256])
+def test_pools_that_overflow_within_a_tile(dtype, k):
+    """More columns pass a bound than there is room for: flat rows, few levels (equal logits everywhere), and few columns left."""
+    c = case(k, [3, 4], 7000, k, dtype, ids=False)
+    check(c)
+    g = torch.Generator(device=DEV).manual_seed(k)
+    c["logits"][1] = torch.randint(0, 3, (7000,), generator=g, device=DEV).to(dtype)
+    c["logits"][2] = 0.5
+    c["logits"][3] = torch.randint(0, 200, (7000,), generator=g, device=DEV).to(dtype) / 16
+    c["logits"][4, 300:6900] = -math.inf
+    c["logits"][5, 1024:2048] = c["logits"][5, :1024]          # the second tile again holds what the first one had
+    c["logits"][6] = torch.randn(7000, generator=g, device=DEV).to(dtype) - (torch.arange(7000, device=DEV) < 1024) * 8.0
+    check(c)
+
+
 def test_scores_whose_order_hangs_on_the_last_bits():
     """Beams of one distribution whose scores differ by one step of fp32: their candidates alternate in that order."""
     c = case(31, [6], 500, 60, F32, ids=False)
