@@ -229,14 +229,20 @@ struct Pool {
   }
 };
 
-// sum += e^(x(e) - top) over a lane's columns, four chains at a time.
-template <class F>
-__device__ __forceinline__ void add_exps(double& sum, float top, F x) {
+// sum += e^(x[e] - top) over a lane's columns, four chains at a time.  FAR: differences below
+// kLeast, those of -infinity among them, are held at it, which leaves nothing; in 64 bits, since
+// fp32 has no numbers just below a `top` of 2^34.
+template <bool FAR, class T>
+__device__ __forceinline__ void add_exps(double& sum, float top, Tile<T> x) {
+  if (FAR) x.here();                      // conversions of its own: shared ones would take registers in both branches
 #pragma unroll
   for (int e = 0; e < kLane; e += 4) {
     double d[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) d[i] = (double)x(e + i) - (double)top;
+    for (int i = 0; i < 4; ++i) {
+      d[i] = (double)x[e + i] - (double)top;
+      if (FAR) d[i] = fmax(d[i], (double)kLeast);
+    }
     exp_64(d);
     sum += (d[0] + d[1]) + (d[2] + d[3]);
   }
@@ -298,17 +304,12 @@ __global__ void __launch_bounds__(kBeamThreads) beam_rows_kernel(BeamArgs p) {
       high = __builtin_amdgcn_readfirstlane(order_of<T>(top));
     }
     if (!PROBS && top > -INFINITY) {
-      // the exponential wants finite differences: where there are others, they are held at what
-      // leaves nothing
+      // the exponential wants finite differences, and none past its range
       float few = INFINITY;
 #pragma unroll
       for (int e = 0; e < kLane; ++e) few = fminf(few, x[e]);
-      if (__any(!(few >= top - 1e6f))) {
-        const float least = top + kLeast;
-        add_exps(sum, top, [&](int e) { return max_nan(x[e], least); });
-      } else {
-        add_exps(sum, top, [&](int e) { return x[e]; });
-      }
+      if (__any(!(few >= top - 1e6f))) add_exps<true>(sum, top, x);
+      else add_exps<false>(sum, top, x);
     }
     if (tile == begin) {
       // k of 256 groups' largest are at or above the k-th of them; its upper 16 bits

@@ -1,0 +1,54 @@
+"""Beam selection of rows whose logits are very large, very low or far apart, against PyTorch's
+log_softmax in 64 bits."""
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+from paper_2410_05165_amd.paged import atspeed_beam_select  # noqa: E402
+
+DEV = "cuda:0"
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def ints(a):
+    return torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).to(DEV)
+
+
+def check(logits, off, k, score):
+    """Scores are one rounding to fp32, a 64-bit sum of numbers up to the row's largest, and the logarithm of a sum of exponentials that
+    are off by 2.4e-10 each; candidates further apart than that rank as they do in 64 bits."""
+    got = atspeed_beam_select(logits, ints(off), k, score=score)
+    largest = logits.double().amax(1).abs().cpu().numpy()
+    lp = torch.log_softmax(logits.double().cpu(), 1).numpy() + score.double().cpu().numpy()[:, None]
+    for b in range(len(off) - 1):
+        every = sorted((-lp[r, v], r, v) for r in range(off[b], off[b + 1]) for v in range(lp.shape[1]) if lp[r, v] > -math.inf)
+        want = every[:k]
+        n = int(got.count[b])
+        assert n == len(want)
+        score_of = got.score[b, :n].double().cpu().numpy()
+        exact = np.array([-z for z, _, _ in want])
+        room = 2.0 ** -24 * np.abs(exact) + 2.0 ** -51 * (np.abs(exact) + largest[[r for _, r, _ in want]]) + 2.5e-10
+        assert (np.abs(score_of - exact) <= room).all(), (b, score_of[:5], exact[:5])
+        parent, token = got.parent[b, :n].tolist(), got.token[b, :n].tolist()
+        assert [(p, t) for p, t in zip(parent, token)] == [(r, v) for _, r, v in want]
+    return got
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("cols", [5, 900, 1024, 1500, 2048, 33024])
+@pytest.mark.parametrize("top", [2.0 ** 35, -2.0 ** 35, 1e12, -1e12, 1.5e10, -1.5e10])
+@pytest.mark.parametrize("others", ["far", "-infinity"])
+def test_columns_far_below_a_large_logit_add_nothing(dtype, cols, top, others):
+    """One logit, or a few, of very large magnitude: what lies far below them, columns behind a tile's end and masked
+    ones among it, is no part of the row's sum."""
+    x = torch.full((3, cols), -math.inf if others == "-infinity" else min(2 * top, -1.0) if top < 0 else 0.0).to(dtype)
+    x[0, cols // 2] = top
+    x[1, ::3] = top
+    x[2] = top
+    score = torch.tensor([-1.0, -2.5, -0.5], device=DEV)
+    check(x.to(DEV), [0, 1, 3], 6, score)
