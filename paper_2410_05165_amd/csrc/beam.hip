@@ -229,20 +229,16 @@ struct Pool {
   }
 };
 
-// sum += e^(x[e] - top) over a lane's columns, four chains at a time.  FAR: differences below
-// kLeast, those of -infinity among them, are held at it, which leaves nothing; in 64 bits, since
-// fp32 has no numbers just below a `top` of 2^34.
-template <bool FAR, class T>
-__device__ __forceinline__ void add_exps(double& sum, float top, Tile<T> x) {
-  if (FAR) x.here();                      // conversions of its own: shared ones would take registers in both branches
+// sum += e^(x[e] - top) over a lane's columns, four chains at a time.  Differences below kLeast,
+// those of -infinity among them, are held at it, which leaves nothing; in 64 bits, since fp32 has
+// no numbers just below a `top` of 2^34.
+template <class T>
+__device__ __forceinline__ void add_exps(double& sum, float top, const Tile<T>& x) {
 #pragma unroll
   for (int e = 0; e < kLane; e += 4) {
     double d[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      d[i] = (double)x[e + i] - (double)top;
-      if (FAR) d[i] = fmax(d[i], (double)kLeast);
-    }
+    for (int i = 0; i < 4; ++i) d[i] = fmax((double)x[e + i] - (double)top, (double)kLeast);
     exp_64(d);
     sum += (d[0] + d[1]) + (d[2] + d[3]);
   }
@@ -303,14 +299,7 @@ __global__ void __launch_bounds__(kBeamThreads) beam_rows_kernel(BeamArgs p) {
       top = now;
       high = __builtin_amdgcn_readfirstlane(order_of<T>(top));
     }
-    if (!PROBS && top > -INFINITY) {
-      // the exponential wants finite differences, and none past its range
-      float few = INFINITY;
-#pragma unroll
-      for (int e = 0; e < kLane; ++e) few = fminf(few, x[e]);
-      if (__any(!(few >= top - 1e6f))) add_exps<true>(sum, top, x);
-      else add_exps<false>(sum, top, x);
-    }
+    if (!PROBS && top > -INFINITY) add_exps(sum, top, x);
     if (tile == begin) {
       // k of 256 groups' largest are at or above the k-th of them; its upper 16 bits
       uint32_t o[4];
