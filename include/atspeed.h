@@ -692,9 +692,10 @@ ATSPEED_API atspeed_status atspeed_logit_rules(const atspeed_logit_rules_args* a
  * row_off[b] .. row_off[b + 1] - 1.  Candidate (r, v) has the score
  *   score[r] + logit[r][v] - log sum_u exp(logit[r][u]),
  * or score[r] + logit[r][v] with log_probs (the logits are log-probabilities already).
- * Scores are computed and compared in 64 bits and rounded to fp32 at the end; equal ones
- * rank by the lower row, then the lower column (logits of one row that differ, but not in
- * 64 bits of the score, may rank either way).
+ * Scores are computed and compared in 64 bits, the row's largest logit taken from its logits
+ * and from the sum before score[r] comes in, and rounded to fp32 at the end; equal ones rank
+ * by the lower row, then the lower column (logits of one row that differ, but not in 64 bits
+ * of the score, may rank either way).
  * A column of -infinity is no candidate.  A row that holds NaN or +infinity, or whose
  * score is not finite, has none.  A row with done[r] != 0 has ended: its only candidate
  * is itself, with score[r] and token -1, whatever its logits hold.

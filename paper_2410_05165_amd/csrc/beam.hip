@@ -3,7 +3,8 @@
 //
 // Within a row the order is that of the logits, so a first kernel reads every logit once
 // and leaves the normaliser's sum and the k best logits of each part of a row; a second one
-// ranks a request's lists by score[r] - log sum + logit.
+// ranks a request's lists by (score[r] - log sum) + (logit - largest).  In that order: a score is
+// lost beside a logit of 3e38, and a row masked by such a number would rank as if it had none.
 //
 // Scores of different beams are compared, so their normalisers must not move them past each
 // other.  They are taken in 64 bits, the exponentials to 2.4e-10: fp32 ones, off by 1e-7, would
@@ -373,8 +374,9 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(BeamArgs p) {
   constexpr int WAVES = THREADS / 64, ROUND = THREADS * kEach, POOL = 2 * ROUND;   // a power of two
   extern __shared__ u64 key[];                     // [POOL]
   u64* const who_of = key + POOL;                  // [POOL]
-  double* const base = (double*)(who_of + POOL);   // [kJoinLists] of a row: score - log sum
-  unsigned short* const open = (unsigned short*)(base + kJoinLists);   // [kJoinLists]
+  double* const base = (double*)(who_of + POOL);   // [kJoinLists] of a row: score - log sum,
+  float* const largest_of = (float*)(base + kJoinLists);               // [kJoinLists] and what its logits are less
+  unsigned short* const open = (unsigned short*)(largest_of + kJoinLists);   // [kJoinLists]
   short* const at = (short*)(open + kJoinLists);   // [kJoinLists]
   short* const len = at + kJoinLists;              // [kJoinLists]
   __shared__ u64 best_key[kMaxBeams], best_who[kMaxBeams], most[WAVES];
@@ -422,10 +424,13 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(BeamArgs p) {
       bool none = !(fabs(score) < INFINITY) || !(total == total);
       double x = score;
       if (!ended && !a.log_probs) {
-        x = score - (all + log(total));
+        x = score - log(total);                    // without columns: infinite
         none = none || !(fabs(x) < INFINITY);
       }
-      if (i < rows && l == 0) base[i] = x;
+      if (i < rows && l == 0) {
+        base[i] = x;
+        largest_of[i] = a.log_probs ? 0.f : (float)all;
+      }
       if (i < rows && none)
         for (int q = l; q < 1 << shift; q += lanes) len[i << shift | q] = 0;
     }
@@ -465,8 +470,8 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(BeamArgs p) {
 #pragma unroll
       for (int i = 0; i < kEach; ++i) {
         const int row = max(from[i], 0) >> shift;
-        const double logit = listed[i] ? (double)logit_of<T>((uint32_t)(listed[i] >> 32)) : 0.0;   // a key is never 0
-        mine[i] = from[i] >= 0 ? order64(base[row] + logit) : 0;
+        const double below = listed[i] ? (double)logit_of<T>((uint32_t)(listed[i] >> 32)) - (double)largest_of[row] : 0.0;   // a key is never 0
+        mine[i] = from[i] >= 0 ? order64(base[row] + below) : 0;
         who[i] = (u64)(r0 + row) << 32 | (listed[i] ? column_of(listed[i]) + 1 : 0);
         largest = max(largest, mine[i]);
       }
@@ -605,7 +610,7 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(BeamArgs p) {
 
 template <class T, int THREADS>
 static atspeed_status launch_join(const BeamArgs& p, hipStream_t st) {
-  constexpr int lds = 2 * THREADS * kEach * 16 + kJoinLists * 14;
+  constexpr int lds = 2 * THREADS * kEach * 16 + kJoinLists * 18;
   if (lds > (64 << 10))
     HIP_TRY(hipFuncSetAttribute((const void*)beam_join_kernel<T, THREADS>, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
   hipLaunchKernelGGL((beam_join_kernel<T, THREADS>), dim3(p.a.B), dim3(THREADS), lds, st, p);

@@ -26,7 +26,8 @@ def select(logits, row_off, k, score=None, done=None, token_base=0, log_probs=Fa
             if np.isnan(x).any() or (x == math.inf).any() or not (x > -math.inf).any():
                 continue
             top = x.max()
-            z = s + x if log_probs else (s - (top + math.log(np.exp(x - top).sum()))) + x
+            # the largest logit is taken from the others before the score comes in: beside a logit of 3e38 a score is lost
+            z = s + x if log_probs else (s - math.log(np.exp(x - top).sum())) + (x - top)
             best = np.lexsort((np.arange(cols), -z))[:k]
             cand += [(-z[v], r, int(v)) for v in best if x[v] > -math.inf]
         cand = sorted(cand)[:k]

@@ -20,10 +20,9 @@ def ints(a):
 
 
 def check(logits, off, k, score):
-    """Scores are one rounding to fp32, a 64-bit sum of numbers up to the row's largest, and the logarithm of a sum of exponentials that
+    """Scores are one rounding to fp32, a 64-bit sum of three numbers, and the logarithm of a sum of exponentials that
     are off by 2.4e-10 each; candidates further apart than that rank as they do in 64 bits."""
     got = atspeed_beam_select(logits, ints(off), k, score=score)
-    largest = logits.double().amax(1).abs().cpu().numpy()
     lp = torch.log_softmax(logits.double().cpu(), 1).numpy() + score.double().cpu().numpy()[:, None]
     for b in range(len(off) - 1):
         every = sorted((-lp[r, v], r, v) for r in range(off[b], off[b + 1]) for v in range(lp.shape[1]) if lp[r, v] > -math.inf)
@@ -32,16 +31,35 @@ def check(logits, off, k, score):
         assert n == len(want)
         score_of = got.score[b, :n].double().cpu().numpy()
         exact = np.array([-z for z, _, _ in want])
-        room = 2.0 ** -24 * np.abs(exact) + 2.0 ** -51 * (np.abs(exact) + largest[[r for _, r, _ in want]]) + 2.5e-10
+        room = 2.0 ** -24 * np.abs(exact) + 2.0 ** -51 * np.abs(exact) + 2.5e-10
         assert (np.abs(score_of - exact) <= room).all(), (b, score_of[:5], exact[:5])
         parent, token = got.parent[b, :n].tolist(), got.token[b, :n].tolist()
         assert [(p, t) for p, t in zip(parent, token)] == [(r, v) for _, r, v in want]
     return got
 
 
+LOWS = [("min", None), ("-1e30", -1e30), ("-1e20", -1e20), ("-1e12", -1e12)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("cols", [7, 1000, 1024, 1500, 33024])
+@pytest.mark.parametrize("name,low", LOWS)
+def test_a_beam_without_an_allowed_token_ranks_by_its_score(dtype, cols, name, low):
+    """All of a row's logits the mask's number: each token has the score less log n, behind the live beams' tokens."""
+    rng = np.random.default_rng(cols)
+    low = torch.finfo(dtype).min if low is None else low
+    x = torch.from_numpy(rng.normal(0, 1, (5, cols))).float().to(dtype)
+    x[1] = low
+    x[2, 3:] = low                                         # three tokens left
+    x[4] = low
+    score = torch.tensor([-1.0, -9.0, -2.0, -4.0, -3.0], device=DEV)
+    got = check(x.to(DEV), [0, 3, 5], min(12, 2 * cols), score)
+    assert got.parent[0, 0].item() in (0, 2)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("cols", [5, 900, 1024, 1500, 2048, 33024])
-@pytest.mark.parametrize("top", [2.0 ** 35, -2.0 ** 35, 1e12, -1e12, 1.5e10, -1.5e10])
+@pytest.mark.parametrize("top", [2.0 ** 35, -2.0 ** 35, 1e12, -1e12, 1e20, 1.5e10, -1.5e10])
 @pytest.mark.parametrize("others", ["far", "-infinity"])
 def test_columns_far_below_a_large_logit_add_nothing(dtype, cols, top, others):
     """One logit, or a few, of very large magnitude: what lies far below them, columns behind a tile's end and masked
