@@ -54,7 +54,7 @@ __global__ void __launch_bounds__(THREADS) distill_loss_kernel(atspeed_distill_l
   constexpr int VEC = 16 / sizeof(T), WAVES = THREADS / 64, STEP = THREADS * VEC;
   extern __shared__ uint32_t bits[];               // a bit a column: a top
   __shared__ int index[kMaxTops], twice;
-  __shared__ double share[kMaxTops], part[4], wave_top[WAVES], wave_all[WAVES];
+  __shared__ double far_of[kMaxTops], part[4], wave_top[WAVES], wave_all[WAVES];
   __shared__ float row_top[WAVES], row_sum[WAVES];
   const int r = blockIdx.x, tid = threadIdx.x, wave = tid >> 6, m = a.n_tops, V = a.n_cols;
   const T* row = static_cast<const T*>(a.logits) + (int64_t)r * a.logits_stride;
@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(THREADS) distill_loss_kernel(atspeed_distill_l
   const double w_rest = tail == -INFINITY ? 0.0 : tail < INFINITY ? exp_below(tail, t_top) : NAN;
   const double w_wave = wave_sum(w);
   if ((tid & 63) == 0) wave_all[wave] = w_wave;
-  if (tid < m) share[tid] = w;
+  if (tid < m) far_of[tid] = t - t_top;
   __syncthreads();
   // one pass over the logits: the largest, and the sum of the others' exponentials
   float top = -INFINITY, sum = 0.f;
@@ -164,18 +164,25 @@ __global__ void __launch_bounds__(THREADS) distill_loss_kernel(atspeed_distill_l
     if (row_top[i] > -INFINITY) rest += (double)(row_sum[i] * __builtin_amdgcn_exp2f((row_top[i] - z_top) * c));
     w_all += wave_all[i];
   }
-  // columns that were named twice: the first one has the sum
+  // p and its logarithm, which goes on where p is 0: (t - t_top) - log w_all.  Columns that were
+  // named twice: the first one has the sum, its logarithm taken around their largest
+  const double log_w = log(w_all);
   bool first = mine >= 0;
-  double p = w;
+  double p = w, log_p = t - t_top;
   if (twice && mine >= 0) {
-    p = 0.0;
     for (int j = 0; j < m; ++j)
       if (index[j] == mine) {
         if (j < tid) first = false;
-        p += share[j];
+        log_p = fmax(log_p, far_of[j]);
       }
+    double all_mine = 0.0;
+    for (int j = 0; j < m; ++j)
+      if (index[j] == mine) all_mine += exp_below(far_of[j], log_p);
+    p = all_mine * exp_below(log_p, 0.0);
+    log_p += log(all_mine);
   }
   p /= w_all;
+  log_p -= log_w;
   const double e = mine >= 0 ? (double)weight_of(z, z_top, c) : 0.0;
   const double all = rest + sum_tops(first ? e : 0.0, one_wave, part);
 
@@ -185,8 +192,7 @@ __global__ void __launch_bounds__(THREADS) distill_loss_kernel(atspeed_distill_l
   const double p_rest = w_rest / w_all;
   const double log_all = log(all);
   const double log_q = z == -INFINITY ? -INFINITY : (double)(z - z_top) * inv_t - log_all;
-  const double log_qr = rest == 0.0 ? -INFINITY : log(rest) - log_all, log_pr = tail - (t_top + log(w_all));
-  const double log_p = log(p);
+  const double log_qr = rest == 0.0 ? -INFINITY : log(rest) - log_all, log_pr = (tail - t_top) - log_w;
   double mass = 0.0, far = 0.0, mass_r = 0.0, far_r = 0.0;     // a bucket's weight, log of the quotient
   if (a.reverse) {
     mass = first && e > 0.0 ? q : 0.0;

@@ -143,6 +143,11 @@ def distill(logits, teacher, index, tail=None, weight=None, T=1.0, reverse=False
         for v, t in entries:
             tops[v] = tops.get(v, 0.0) + math.exp(t / T - t_top) / total
         p_rest = math.exp(rest_t - t_top) / total
+        # log p without p, which is 0 from 745 below the largest on: around the largest entry of each bucket
+        log_p, log_p_rest = {}, (rest_t - t_top) - math.log(total)
+        for v in tops:
+            mine = [t / T for u, t in entries if u == v]
+            log_p[v] = (max(mine) - t_top) + math.log(sum(math.exp(t - max(mine)) for t in mine)) - math.log(total)
         cols_of = np.array(sorted(tops))
         p = np.array([tops[v] for v in cols_of])
         others = np.ones(cols, bool)
@@ -163,8 +168,8 @@ def distill(logits, teacher, index, tail=None, weight=None, T=1.0, reverse=False
             rel_rest = ((e * err)[others].sum() / e[others].sum() if q_rest > 0 else 0.0) + add
             log_q = d - math.log(e.sum())
         with np.errstate(divide="ignore", invalid="ignore"):
-            lp, lq = np.log(p), log_q[cols_of]
-            lpr = math.log(p_rest) if p_rest > 0 else -math.inf
+            lp, lq = np.array([log_p[v] for v in cols_of]), log_q[cols_of]
+            lpr = log_p_rest
             lqr = math.log(q_rest) if q_rest > 0 else -math.inf
             step = w * T
             qt = q[cols_of]
