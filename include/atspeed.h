@@ -834,7 +834,9 @@ ATSPEED_API atspeed_status atspeed_kv_compact(const atspeed_kv_compact_args* arg
  * sum of their probabilities.  Entries whose index is outside 0 .. n_cols - 1 or whose
  * logit is -infinity are no tops.  A row without tops, or of weight 0, has loss 0 and
  * gradient 0, whatever its logits hold; columns of logit -infinity have q_v = 0, and where
- * all are, q is 0.  The share of columns more than 2^126 below the largest counts as 0.
+ * all are, q is 0.  The share of columns more than 2^126 below the largest counts as 0, and
+ * what multiplies exp(logit / temperature - largest) in the gradient of the columns that are
+ * no tops is held at fp32's largest number.
  * NaN or +infinity in a row's logits, tops or tail makes its loss and gradient NaN.
  * Sums and statistics are fp32, what is summed over the tops 64 bits.
  *   logits [n_rows, n_cols], rows logits_stride elements apart, at any element;

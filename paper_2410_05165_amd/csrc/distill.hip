@@ -240,7 +240,11 @@ __global__ void __launch_bounds__(kDistThreads) distill_grad_kernel(atspeed_dist
   T* out = static_cast<T*>(a.grad) + (int64_t)r * a.grad_stride;
   const float* saved = a.saved + (int64_t)r * (2 + m);
   const float g = a.grad_loss ? a.grad_loss[r] : 1.f;
-  const float top = saved[0], scale = saved[1] == 0.f ? 0.f : saved[1] * g;
+  // a factor of the rest's size may have no fp32 product with a scaled loss's g: g then comes
+  // behind the exponential, which may be 0
+  const float top = saved[0], both = saved[1] == 0.f ? 0.f : saved[1] * g;
+  const bool apart = !(fabsf(both) <= FLT_MAX);
+  const float scale = apart ? saved[1] : both, behind = apart ? g : 1.f;
 #pragma unroll
   for (int k = 0; k < kGradVecs / VEC; ++k) {
     const int v = v0 + (k * kDistThreads + tid) * VEC;
@@ -249,7 +253,7 @@ __global__ void __launch_bounds__(kDistThreads) distill_grad_kernel(atspeed_dist
       float x[VEC];
       unpack<T>(*reinterpret_cast<const u32x4_any_t*>(row + v), x);
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) x[i] = scale == 0.f ? 0.f : scale * weight_of(x[i], top, c);
+      for (int i = 0; i < VEC; ++i) x[i] = scale == 0.f ? 0.f : scale * weight_of(x[i], top, c) * behind;
       u32x4_t raw;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -257,7 +261,7 @@ __global__ void __launch_bounds__(kDistThreads) distill_grad_kernel(atspeed_dist
                           : (uint32_t)f2bf(x[VEC == 4 ? 0 : 2 * i]) | (uint32_t)f2bf(x[VEC == 4 ? 0 : 2 * i + 1]) << 16;
       *reinterpret_cast<u32x4_any_t*>(out + v) = raw;
     } else {
-      for (int i = v; i < V; ++i) St<T>::st(out + i, scale == 0.f ? 0.f : scale * weight_of(St<T>::ld(row + i), top, c));
+      for (int i = v; i < V; ++i) St<T>::st(out + i, scale == 0.f ? 0.f : scale * weight_of(St<T>::ld(row + i), top, c) * behind);
     }
   }
   __syncthreads();               // the tops' own values come behind

@@ -1,4 +1,5 @@
-"""Distillation where logits lie far apart, against the definition in 64 bits."""
+"""Distillation where logits lie far apart and where the student's rest is next to nothing, against
+the definition in 64 bits."""
 import math
 
 import numpy as np
@@ -32,3 +33,25 @@ def test_teacher_logits_far_below_the_best(dtype, tail, reverse, m, T, far):
         c["tail"] = torch.logsumexp(c["teacher_logit"].double() / T, 1).float() - 1.0
         c["tail"][5] = -far / T if far < math.inf else torch.finfo(F32).min
     check(c)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("reverse", [False, True])
+@pytest.mark.parametrize("gap", [60.0, 80.0, 86.0])
+def test_gradients_of_scaled_losses_over_a_rest_of_next_to_nothing(dtype, reverse, gap):
+    """A student that is sure of its tops, most other columns masked, the loss scaled up: no NaN, and the columns that
+    are left keep their gradient."""
+    c = case(32, 5, 900, 6, dtype, True, reverse, spread=1.0, weight=False)
+    c["teacher_index"][:] = 7 * torch.arange(6, device=DEV) + 3
+    inside = torch.zeros((5, 900), dtype=torch.bool, device=DEV)
+    inside.scatter_(1, c["teacher_index"].long(), True)
+    c["logits"].masked_fill_(~inside, -math.inf)
+    left = torch.zeros_like(inside)
+    left[:, 11::100] = True
+    c["logits"][left] = c["logits"].masked_fill(~inside, -math.inf).amax(1)[:, None].expand(5, 900)[left] - gap
+    c["logits"][:, 5::90] = torch.finfo(dtype).min             # masked by a number
+    for scale in (1.0, 65536.0, 2.0 ** 100):
+        _, grad = check(c, torch.full((5,), scale, device=DEV))
+        assert bool(torch.isfinite(grad).all())
+        assert bool((grad[left] != 0).all()) or reverse
+        assert not bool(grad[~inside & ~left].any())
