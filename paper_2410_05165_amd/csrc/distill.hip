@@ -156,14 +156,15 @@ __global__ void __launch_bounds__(THREADS) distill_loss_kernel(atspeed_distill_l
   z_top = row_top[0];
 #pragma unroll
   for (int i = 1; i < WAVES; ++i) z_top = max_nan(z_top, row_top[i]);
-  const bool bad = !(z_top < INFINITY);
-  if (bad) z_top = NAN;
-  double rest = 0.0, w_all = w_rest;
+  double w_all = w_rest;
 #pragma unroll
-  for (int i = 0; i < WAVES; ++i) {
+  for (int i = 0; i < WAVES; ++i) w_all += wave_all[i];
+  const bool bad = !(z_top < INFINITY) || !(w_all == w_all);   // of the row's own or the teacher's
+  if (bad) z_top = NAN;
+  double rest = 0.0;
+#pragma unroll
+  for (int i = 0; i < WAVES; ++i)
     if (row_top[i] > -INFINITY) rest += (double)(row_sum[i] * __builtin_amdgcn_exp2f((row_top[i] - z_top) * c));
-    w_all += wave_all[i];
-  }
   // p and its logarithm, which goes on where p is 0: (t - t_top) - log w_all.  Columns that were
   // named twice: the first one has the sum, its logarithm taken around their largest
   const double log_w = log(w_all);

@@ -1,5 +1,5 @@
-"""Distillation where logits lie far apart and where the student's rest is next to nothing, against
-the definition in 64 bits."""
+"""Distillation where the teacher's logits lie far apart, where the student's rest is next to
+nothing, and where a row holds no numbers: against the definition in 64 bits."""
 import math
 
 import numpy as np
@@ -9,6 +9,7 @@ pytestmark = pytest.mark.gpu
 
 torch = pytest.importorskip("torch")
 
+from paper_2410_05165_amd.align import atspeed_distill_grad, atspeed_distill_loss  # noqa: E402
 from test_gpu_distill import BF16, DEV, F32, FORMS, case, check  # noqa: E402
 
 
@@ -55,3 +56,32 @@ def test_gradients_of_scaled_losses_over_a_rest_of_next_to_nothing(dtype, revers
         assert bool(torch.isfinite(grad).all())
         assert bool((grad[left] != 0).all()) or reverse
         assert not bool(grad[~inside & ~left].any())
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("tail,reverse", FORMS)
+@pytest.mark.parametrize("m", [7, 100])
+def test_a_teacher_that_is_no_number_beside_masked_students(bad, tail, reverse, m):
+    """Where the student's rest, one of its tops or all of its logits are -infinity, the row is NaN as any other."""
+    c = case(33, 5, 900, m, F32, tail, reverse)
+    c["teacher_index"][:] = torch.arange(m, device=DEV) * 3
+    c["teacher_index"][:, 1] = 0                               # twice
+    inside = torch.zeros((5, 900), dtype=torch.bool, device=DEV)
+    inside.scatter_(1, c["teacher_index"].long(), True)
+    c["logits"][0] = torch.where(inside[0], c["logits"][0], -math.inf)
+    c["logits"][1] = -math.inf
+    c["logits"][2, 6] = -math.inf
+    rows = [0, 1, 2]
+    c["teacher_logit"][:3, m - 1] = bad
+    loss, saved = atspeed_distill_loss(**c)
+    grad = atspeed_distill_grad(c["logits"], c["teacher_index"], saved)
+    for r in range(5):
+        assert math.isnan(float(loss[r])) == (r in rows)
+        assert bool(torch.isnan(grad[r]).all()) if r in rows else bool(torch.isfinite(grad[r]).all())
+    if tail:
+        c["teacher_logit"][:3, m - 1] = 0.0
+        c["tail"][:3] = bad
+        loss, saved = atspeed_distill_loss(**c)
+        grad = atspeed_distill_grad(c["logits"], c["teacher_index"], saved)
+        for r in rows:
+            assert math.isnan(float(loss[r])) and bool(torch.isnan(grad[r]).all())
