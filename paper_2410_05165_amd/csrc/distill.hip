@@ -192,7 +192,7 @@ __global__ void __launch_bounds__(THREADS) distill_loss_kernel(atspeed_distill_l
   const double inv_all = 1.0 / all, q = empty ? 0.0 : e * inv_all, q_rest = empty ? 0.0 : rest * inv_all;
   const double p_rest = w_rest / w_all;
   const double log_all = log(all);
-  const double log_q = z == -INFINITY ? -INFINITY : (double)(z - z_top) * inv_t - log_all;
+  const double log_q = z == -INFINITY ? -INFINITY : ((double)z - (double)z_top) * inv_t - log_all;
   const double log_qr = rest == 0.0 ? -INFINITY : log(rest) - log_all, log_pr = (tail - t_top) - log_w;
   double mass = 0.0, far = 0.0, mass_r = 0.0, far_r = 0.0;     // a bucket's weight, log of the quotient
   if (a.reverse) {

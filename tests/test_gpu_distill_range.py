@@ -85,3 +85,16 @@ def test_a_teacher_that_is_no_number_beside_masked_students(bad, tail, reverse, 
         grad = atspeed_distill_grad(c["logits"], c["teacher_index"], saved)
         for r in rows:
             assert math.isnan(float(loss[r])) and bool(torch.isnan(grad[r]).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_student_logits_further_apart_than_fp32_reaches(dtype):
+    """A top 5e38 below the largest logit: the forward form takes p times that distance, not infinity."""
+    c = case(34, 4, 300, 5, dtype, False, False, weight=False)
+    c["teacher_index"][:] = torch.arange(5, device=DEV) * 11 + 2
+    c["teacher_logit"][:] = torch.tensor([2.0, 1.0, -6.0, -7.0, -5.0], device=DEV)
+    c["logits"][1:, 2] = 2.5e38
+    c["logits"][1, 24] = -2.5e38
+    c["logits"][2:, 35] = -2.5e38
+    loss, _ = check(c)
+    assert bool(torch.isfinite(loss).all())
