@@ -18,6 +18,7 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/core/LegacyTypeDispatch.h>
 #include <ATen/ops/empty.h>
+#include <ATen/ops/zeros.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/atspeed.h"
@@ -470,16 +471,25 @@ PyObject* beam_select(PyObject*, PyObject* const* o, Py_ssize_t n) {
     a.row_id = want_i32(o[7], "row_id", {x.rows}, dev);
     const bool with_paths = o[8] != Py_None;
     if (with_paths != (o[9] != Py_None)) bad("paths and path_len go together");
+    at::Tensor empty_path;
+    int64_t P = 0;
     if (with_paths) {
       const at::Tensor& paths = tensor(o[8], "paths");
-      if (paths.dim() != 2) bad("paths: want [n, max_path]");
+      if (paths.dim() != 2 || paths.size(1) < 1) bad("paths: want [n, max_path], max_path of 1 at least");
       a.n_paths = int32(paths.size(0), "paths");
       a.max_path = int32(paths.size(1), "max_path");
+      P = std::min(a.max_path, 1 << 16);   // larger ones are refused below
       a.paths = want_i32(o[8], "paths", {paths.size(0), paths.size(1)}, dev);
     }
     a.path_len = want_i32(o[9], "path_len", {a.n_paths}, dev);
+    if (with_paths && a.n_paths == 0) {   // a tensor of no paths has no address: one path of no tokens is none, either
+      empty_path = at::zeros({1 + P}, at::TensorOptions().dtype(i32).device(dev));
+      a.n_paths = 1;
+      a.path_len = address<int32_t>(empty_path);
+      a.paths = a.path_len + 1;
+    }
     if (B < 1 || a.k < 1) bad("want row_off of two numbers at least, and k of 1 at least");
-    const int64_t k = std::min(a.k, 256), P = a.max_path;   // a larger k is refused below
+    const int64_t k = std::min(a.k, 256);   // larger ones are refused below
     const at::Tensor count = fresh({B}, i32, dev), parent = fresh({B, k}, i32, dev), token = fresh({B, k}, i32, dev),
                      score = fresh({B, k}, f32, dev);
     at::Tensor paths, path_len, ws;

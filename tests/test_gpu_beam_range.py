@@ -9,6 +9,7 @@ pytestmark = pytest.mark.gpu
 
 torch = pytest.importorskip("torch")
 
+from paper_2410_05165_amd.binding import AtspeedError  # noqa: E402
 from paper_2410_05165_amd.paged import atspeed_beam_select  # noqa: E402
 
 DEV = "cuda:0"
@@ -70,3 +71,42 @@ def test_columns_far_below_a_large_logit_add_nothing(dtype, cols, top, others):
     x[2] = top
     score = torch.tensor([-1.0, -2.5, -0.5], device=DEV)
     check(x.to(DEV), [0, 1, 3], 6, score)
+
+
+def test_paths_of_no_beams():
+    """Empty paths: every parent is unknown and has an empty one; without rows there is nothing but padding."""
+    x = torch.randn((4, 60), device=DEV, generator=torch.Generator(device=DEV).manual_seed(1))
+    none, length = ints(np.zeros((0, 3))), ints([])
+    for _ in range(3):
+        torch.full((1 << 16,), 77, dtype=torch.int32, device=DEV)      # what fresh memory may hold
+        got = atspeed_beam_select(x, ints([0, 3, 4]), 5, paths=none, path_len=length)
+        assert torch.equal(got.paths[..., 0], got.token) and bool((got.paths[..., 1:] == -1).all())
+        assert bool((got.path_len == 1).all())
+        got = atspeed_beam_select(x[:0], ints([0, 0]), 2, paths=none, path_len=length)
+        assert got.count.tolist() == [0] and bool((got.paths == -1).all()) and not bool(got.path_len.any())
+    with pytest.raises(ValueError, match="max_path"):
+        atspeed_beam_select(x, ints([0, 4]), 5, paths=ints(np.zeros((4, 0))), path_len=ints(np.zeros(4)))
+
+
+def test_paths_of_no_beams_in_a_graph():
+    x = torch.randn((4, 60), device=DEV, generator=torch.Generator(device=DEV).manual_seed(1))
+    none, length, off = ints(np.zeros((0, 3))), ints([]), ints([0, 3, 4])
+    want = atspeed_beam_select(x, off, 5, paths=none, path_len=length)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = atspeed_beam_select(x, off, 5, paths=none, path_len=length)
+    for _ in range(3):
+        for t in got:
+            t.fill_(9)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        torch.full((1 << 16,), 77, dtype=torch.int32, device=DEV)
+
+
+def test_paths_too_wide_are_refused_without_room_for_them():
+    x = torch.randn((4, 60), device=DEV)
+    for most in (1 << 30, (1 << 31) - 1):
+        with pytest.raises(AtspeedError, match="max_path"):
+            atspeed_beam_select(x, ints([0, 4]), 5, paths=ints(np.zeros((0, 1))).expand(0, most), path_len=ints([]))
