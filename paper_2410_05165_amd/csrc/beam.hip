@@ -247,13 +247,31 @@ __device__ __forceinline__ void add_exps(double& sum, float top, const Tile<T>& 
 
 struct BeamArgs {
   atspeed_beam_select_args a;
-  u64* list;        // [lists, k] the best columns, best first: a list a row, from row `whole` on `parts` a row
+  u64* list;        // [lists, k] the best columns, best first: a list a row, from some row on `parts` a row
   double2* stat;    // [lists] largest logit and sum of exponentials; NaN: the row has no candidates
   int* len;         // [lists]
-  int whole, parts, tiles, shift; // tiles of a part; parts <= 1 << shift
+  int whole, slack, parts, tiles, shift;   // rows below about `whole` have one list; tiles of a part; parts <= 1 << shift
 
-  __host__ __device__ int64_t list_of(int r) const { return r < whole ? r : whole + (int64_t)(r - whole) * parts; }
+  // The first list of row r where rows are cut from `from` on.
+  __host__ __device__ int64_t list_of(int r, int from) const { return r < from ? r : from + (int64_t)(r - from) * parts; }
+  __host__ __device__ int64_t most_lists(int rows) const { return list_of(rows, whole - slack); }
 };
+
+// The row from which on rows are cut: where the request that row `whole` lies in begins, or ends
+// where it begins more than `slack` rows before.  A sum by parts differs from one of the whole row
+// in its last bits, and rows of one request that are alike rank by their numbers: all of a
+// request's rows are taken in one way.  The whole wave's call.
+__device__ __forceinline__ int first_cut(const BeamArgs& p, int lane) {
+  if (!p.slack) return p.whole;
+  const int B = p.a.B, step = (B + 64) / 64, n_rows = p.a.n_rows;
+  const u64 far = __ballot(p.a.row_off[min((lane + 1) * step - 1, B)] >= p.whole);
+  if (!far) return n_rows;
+  const int at = min((int)__builtin_ctzll(far) * step + min(lane, step - 1), B);
+  const int end = p.a.row_off[at], begin = p.a.row_off[max(at - 1, 0)];
+  const int first = __builtin_ctzll(__ballot(end >= p.whole));
+  const int e = __builtin_amdgcn_readlane(end, first), b = __builtin_amdgcn_readlane(begin, first);
+  return e > p.whole && b < p.whole && b >= p.whole - p.slack ? b : min(e, n_rows);
+}
 
 // A wave takes a part of a row by itself, tile by tile: the running maximum and 64-bit sum
 // of its exponentials, and its k best columns behind a bound that rises with them.  No barrier,
@@ -267,8 +285,8 @@ __global__ void __launch_bounds__(kBeamThreads) beam_rows_kernel(BeamArgs p) {
   __shared__ u64 keys[kBeamWaves * P * 64];
   const atspeed_beam_select_args& a = p.a;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int q = blockIdx.x * kBeamWaves + wave, cut = max(q - p.whole, 0), part = cut % p.parts;
-  const int r = min(q, p.whole) + cut / p.parts;
+  const int q = blockIdx.x * kBeamWaves + wave, from = q < p.whole - p.slack ? p.whole : first_cut(p, lane);
+  const int cut = max(q - from, 0), part = cut % p.parts, r = min(q, from) + cut / p.parts;
   if (r >= a.n_rows) return;
   const int k = a.k, n_cols = a.n_cols;
   const T* row = static_cast<const T*>(a.logits) + (int64_t)r * a.logits_stride;
@@ -278,7 +296,7 @@ __global__ void __launch_bounds__(kBeamThreads) beam_rows_kernel(BeamArgs p) {
   double sum = 0.0;
   uint32_t high = 0;
 
-  const int tiles = (n_cols + kTile - 1) / kTile, begin = part * p.tiles, end = q < p.whole ? tiles : min(begin + p.tiles, tiles);
+  const int tiles = (n_cols + kTile - 1) / kTile, begin = part * p.tiles, end = q < from ? tiles : min(begin + p.tiles, tiles);
   // the last tile of a row ends with it and drops what the one before had
   const int last = n_cols - kTile;
   Tile<T> x, next;
@@ -385,6 +403,7 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(BeamArgs p) {
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, k = a.k, shift = p.shift;
   const int r1 = min(min(a.row_off[b + 1], a.row_off[a.B]), a.n_rows);   // rows that the first kernel read
   const int group = kJoinLists >> shift;           // lists: row << shift | part
+  const int cut_from = first_cut(p, lane);
   int n = 0;                                       // best_key[0 .. n) are the best so far, in order
   if (tid < 2) s_open[tid] = 0;
   for (int r0 = max(a.row_off[b], 0); r0 < r1; r0 += group) {
@@ -396,15 +415,15 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(BeamArgs p) {
       const int i = i0 + (tid >> wide), r = min(r0 + i, r1 - 1), l = tid & (lanes - 1);
       const double score = a.score ? (double)a.score[r] : 0.0;
       const bool ended = a.done && a.done[r];
-      const int parts = r < p.whole ? 1 : p.parts;
+      const int parts = r < cut_from ? 1 : p.parts;
       double all = -INFINITY, total = 0.0;
       for (int q = l; q < 1 << shift; q += lanes) {
         // asked for before it is known whether the row has ended, and then left alone
         double2 st = {-INFINITY, 0.0};
         int length = 0;
         if (q < parts) {
-          st = p.stat[p.list_of(r) + q];
-          length = p.len[p.list_of(r) + q];
+          st = p.stat[p.list_of(r, cut_from) + q];
+          length = p.len[p.list_of(r, cut_from) + q];
         }
         if (ended) st = {-INFINITY, 0.0};
         if (i < rows) {
@@ -465,7 +484,7 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(BeamArgs p) {
         const bool in = e >> depth < n_open && j < n_here;
         from[i] = in ? l : -1;
         next[i] = j + 1 >= n_here ? -1 : d + 1 == 1 << depth ? j + 1 : 0;
-        listed[i] = in && length != kItself ? p.list[(p.list_of(r0 + (l >> shift)) + (l & ((1 << shift) - 1))) * k + j] : 0;
+        listed[i] = in && length != kItself ? p.list[(p.list_of(r0 + (l >> shift), cut_from) + (l & ((1 << shift) - 1))) * k + j] : 0;
       }
 #pragma unroll
       for (int i = 0; i < kEach; ++i) {
@@ -622,7 +641,7 @@ static atspeed_status run_join(const BeamArgs& p, hipStream_t st) {
   // Few entries a request, or many requests: smaller workgroups, more of them on a CU (both
   // kernels, us, 256 threads and 1,024: 10 rows of 1,024 columns 12.4 and 15.9, 32 requests of 9
   // rows of 33,024 with 10 beams 26.6 and 28.4; but 128 of 45 rows with 50 220 and 189).
-  const long long entries = p.list_of(p.a.n_rows) * p.a.k;
+  const long long entries = p.most_lists(p.a.n_rows) * p.a.k;
   return p.a.B > 256 || entries <= 1024LL * p.a.B ? launch_join<T, 256>(p, st) : launch_join<T, 1024>(p, st);
 }
 
@@ -666,10 +685,12 @@ static void cut_rows(const atspeed_beam_select_args& a, BeamArgs& p) {
   p.tiles = (tiles + want - 1) / want;
   p.parts = (tiles + p.tiles - 1) / p.tiles;
   while (1 << p.shift < p.parts) ++p.shift;
+  // the cut moves to where a request begins: twice the requests' average is room for most
+  if (p.whole && p.parts > 1) p.slack = std::min(2 * beams, p.whole);
 }
 
 static size_t lay_out(BeamArgs& p, char* base) {
-  const size_t lists = p.list_of(std::max(p.a.n_rows, 1));
+  const size_t lists = p.most_lists(std::max(p.a.n_rows, 1));
   size_t at = 0;
   auto take = [&](size_t bytes) {
     char* q = base ? base + at : nullptr;
@@ -722,7 +743,7 @@ atspeed_status atspeed_beam_select(const atspeed_beam_select_args* args, void* w
   BeamArgs p{};
   p.a = *args;
   cut_rows(*args, p);
-  const long long groups = (p.list_of(args->n_rows) + kBeamWaves - 1) / kBeamWaves;
+  const long long groups = (p.most_lists(args->n_rows) + kBeamWaves - 1) / kBeamWaves;
   if (groups > kMaxGroups) return fail(ATSPEED_E_SHAPE, "beam select: too many rows x columns");
   const size_t need = lay_out(p, nullptr);
   if (!workspace || !aligned16(workspace) || ws_bytes < need)

@@ -73,6 +73,30 @@ def test_columns_far_below_a_large_logit_add_nothing(dtype, cols, top, others):
     check(x.to(DEV), [0, 1, 3], 6, score)
 
 
+@pytest.mark.parametrize("rows,cols", [(4104, 33024), (4104, 17000), (4104, 2048), (5400, 9000), (8196, 3000)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_equal_rows_on_both_sides_of_the_cut_go_to_the_lower_one(rows, cols, dtype):
+    """Rows that fill the card go to a wave each, those behind them in parts (4,096 or 8,192 come first), and the sums of
+    the two differ in their last bits: no request has rows of both sorts, and its rows that are alike rank in order."""
+    rng = np.random.default_rng(cols)
+    whole, k, n = rows // 4096 * 4096, 24, 6 if rows < 6000 else 12
+    off = np.arange(0, rows + 1, n)
+    across = int(np.searchsorted(off, whole, "right")) - 1
+    assert off[-1] == rows and off[across] < whole < off[across] + n
+    x = torch.empty((rows, cols), dtype=dtype, device=DEV)
+    for _ in range(3):
+        x[:] = torch.from_numpy(rng.normal(0, 3, cols)).float().to(dtype).to(DEV)
+        got = atspeed_beam_select(x, ints(off), k)
+        best = torch.sort(x[0].float(), descending=True, stable=True)
+        z, col = best.values[:k].tolist(), best.indices[:k].tolist()
+        want = [(r, v) for _, r, v in sorted((-a, r, v) for a, v in zip(z, col) for r in range(n))][:k]
+        for b in (0, across - 1, across, across + 1):
+            if b >= len(off) - 1:
+                continue
+            assert [(p - int(off[b]), t) for p, t in zip(got.parent[b].tolist(), got.token[b].tolist())] == want, b
+            assert bool((got.score[b] - got.score[0]).abs().max() <= 2.0 ** -23 * got.score[0].abs().max())
+
+
 def test_paths_of_no_beams():
     """Empty paths: every parent is unknown and has an empty one; without rows there is nothing but padding."""
     x = torch.randn((4, 60), device=DEV, generator=torch.Generator(device=DEV).manual_seed(1))
@@ -110,3 +134,30 @@ def test_paths_too_wide_are_refused_without_room_for_them():
     for most in (1 << 30, (1 << 31) - 1):
         with pytest.raises(AtspeedError, match="max_path"):
             atspeed_beam_select(x, ints([0, 4]), 5, paths=ints(np.zeros((0, 1))).expand(0, most), path_len=ints([]))
+
+
+@pytest.mark.parametrize("what", ["one", "wide", "empty", "short"])
+def test_every_place_of_the_cut_among_the_requests(what):
+    """The cut inside the last request, inside one of hundreds of rows, between empty ones, behind the rows that are used:
+    every request has the ranking that it has by itself."""
+    rng = np.random.default_rng(3)
+    rows, cols, k = 4200, 2500, 7
+    counts = {"one": [6] * 682 + [108], "wide": [1] * 3800 + [400], "empty": [0, 6] * 700, "short": [4] * 1023}[what]
+    if what == "wide":
+        counts = [5] * 760 + [400]
+    off = np.concatenate([[0], np.cumsum(counts)])
+    if what == "empty":
+        off = np.concatenate([off[:1000], [4200]])
+    x = torch.randn((rows, cols), generator=torch.Generator(device=DEV).manual_seed(4), device=DEV).to(BF16)
+    score = torch.from_numpy(-rng.gamma(4, 2, rows)).float().to(DEV)
+    got = atspeed_beam_select(x, ints(off), k, score=score)
+    for b in {0, len(off) - 2, len(off) // 2} | {int(np.searchsorted(off, 4096, "right")) + d for d in (-3, -2, -1, 0)}:
+        if not 0 <= b < len(off) - 1:
+            continue
+        r0, r1 = int(off[b]), int(off[b + 1])
+        alone = atspeed_beam_select(x[r0:r1], ints([0, r1 - r0]), k, score=score[r0:r1].contiguous())
+        n = int(alone.count[0])
+        assert int(got.count[b]) == n == min(k, (r1 - r0) * cols)
+        assert (got.parent[b, :n] - r0).tolist() == alone.parent[0, :n].tolist()
+        assert got.token[b].tolist() == alone.token[0].tolist()
+        torch.testing.assert_close(got.score[b, :n], alone.score[0, :n], rtol=2.0 ** -23, atol=0)
