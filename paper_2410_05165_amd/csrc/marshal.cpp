@@ -210,6 +210,18 @@ at::Tensor fresh(c10::IntArrayRef shape, c10::ScalarType type, const at::Device&
   return at::empty(shape, at::TensorOptions().dtype(type).device(dev));
 }
 
+// The arguments of a plan that say which rows are added.
+void plan_rows(atspeed_page_plan_args& a, PyObject* add, PyObject* max_rows, PyObject* parent, int64_t B, const at::Device& dev) {
+  a.max_rows = int32(max_rows, "max_rows");
+  if (a.max_rows < 0) bad("max_rows must be >= 0");
+  a.add = want_i32(add, "add", {B}, dev);
+  if (parent == Py_None) return;
+  const at::Tensor& p = tensor(parent, "parent");
+  if (p.dim() != 2) bad("parent: want [B, max_nodes]");
+  a.max_nodes = int32(p.size(1), "max_nodes");
+  a.parent = want_i32(parent, "parent", {B, p.size(1)}, dev);
+}
+
 // held, keep, add, block_table, free_pages, n_free, page_size, max_rows, parent, stream
 PyObject* page_plan(PyObject*, PyObject* const* o, Py_ssize_t n) {
   return guarded(n, 10, [&]() -> PyObject* {
@@ -221,24 +233,17 @@ PyObject* page_plan(PyObject*, PyObject* const* o, Py_ssize_t n) {
     a.B = int32(B, "B");
     a.max_pages = int32(most, "max_pages");
     a.page_size = int32(o[6], "page_size");
-    a.max_rows = int32(o[7], "max_rows");
-    if (a.max_rows < 0) bad("max_rows must be >= 0");
+    plan_rows(a, o[2], o[7], o[8], B, dev);
     const int64_t R = a.max_rows, pool = tensor(o[4], "free_pages").numel();
     a.n_pool = int32(pool, "free_pages");
     a.held = want_i32(o[0], "held", {B}, dev);
     a.keep = want_i32(o[1], "keep", {B}, dev);
-    a.add = want_i32(o[2], "add", {B}, dev);
     a.block_table = want_i32(o[3], "block_table", {B, most}, dev);
     a.free_pages = want_i32(o[4], "free_pages", {pool}, dev);
     a.n_free = want_i32(o[5], "n_free", {1}, dev);
     at::Tensor mask;
     if (o[8] != Py_None) {
-      const at::Tensor& parent = tensor(o[8], "parent");
-      if (parent.dim() != 2) bad("parent: want [B, max_nodes]");
-      const int64_t nodes = parent.size(1);
-      a.max_nodes = int32(nodes, "max_nodes");
-      a.parent = want_i32(o[8], "parent", {B, nodes}, dev);
-      mask = fresh({R, (nodes + 63) / 64}, c10::ScalarType::Long, dev);
+      mask = fresh({R, ((int64_t)a.max_nodes + 63) / 64}, c10::ScalarType::Long, dev);
       a.mask = address<uint64_t>(mask);
     }
     // one allocation; its pieces are the outputs
@@ -588,6 +593,25 @@ void set_layers(A& a, const Layers& l) {
   a.v_layer_stride = l.v_stride;
 }
 
+// add, block_table, max_rows, parent, k_cache, v_cache: what page_copy and page_plan will look at behind a fork, which
+// changes the tables.  Launches nothing.
+PyObject* fork_check(PyObject*, PyObject* const* o, Py_ssize_t n) {
+  return guarded(n, 6, [&]() -> PyObject* {
+    const at::Tensor& table = gpu_tensor(o[1], "block_table");
+    if (table.dim() != 2) bad("block_table: want [B, max_pages]");
+    atspeed_page_plan_args a{};
+    plan_rows(a, o[0], o[2], o[3], table.size(0), table.device());
+    if (!a.add && table.size(0) > 0) bad("add: want a tensor");
+    if (o[3] != Py_None && (a.max_nodes < 1 || a.max_nodes > 4096)) bad("parent: want [B, max_nodes], max_nodes 1..4096");
+    const Layers l = layers(o[4], o[5]);
+    if (l.c.dev != table.device()) bad("the caches and the block_table want one device");
+    atspeed_page_copy_args c{};
+    set_layers(c, l);
+    check(atspeed_page_copy(&c, nullptr));   // of no pages
+    Py_RETURN_NONE;
+  });
+}
+
 // k_cache, v_cache, src, dst, length, stream
 PyObject* page_copy(PyObject*, PyObject* const* o, Py_ssize_t n) {
   return guarded(n, 6, [&]() -> PyObject* {
@@ -709,7 +733,7 @@ PyObject* set_error(PyObject*, PyObject* cls) {
 
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(page_plan), FAST(kv_append), FAST(tree_attention), FAST(logit_rules),
-                         FAST(beam_select), FAST(page_fork), FAST(page_copy), FAST(kv_compact), FAST(distill_loss),
+                         FAST(beam_select), FAST(page_fork), FAST(fork_check), FAST(page_copy), FAST(kv_compact), FAST(distill_loss),
                          FAST(distill_grad),
                          {"set_error", set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

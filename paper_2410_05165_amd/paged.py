@@ -185,18 +185,25 @@ class PagedKV:
 
         With ``share``: row b goes on with keep[b] tokens (keep None: all) of row src[b] (-1: none; src None: its own).
         A row that the fork refuses is refused by the plan too, as a request that keeps more than it holds.
+        Arguments that do not fit are found before anything changes.  What fails behind the fork all the same (memory that
+        runs out) leaves the rows forked and nothing added: go on with keep None and src None.
         """
-        held = self.length
         if self.shared is not None:
-            f = atspeed_page_fork(held, keep, self.block_table, self.free_pages, self.n_free, self.shared, self.page_size,
-                                  src=src)
-            atspeed_page_copy(self.k, self.v, f.copy_src, f.copy_dst, f.copy_len)
-            held = f.length
-            keep = torch.where(f.refused == 0, held, held + 1)
-        elif src is not None:
+            _marshal.fork_check(add, self.block_table, max_rows, parent, self.k, self.v)
+            f = atspeed_page_fork(self.length, keep, self.block_table, self.free_pages, self.n_free, self.shared,
+                                  self.page_size, src=src)
+            try:
+                atspeed_page_copy(self.k, self.v, f.copy_src, f.copy_dst, f.copy_len)
+                return self._add(f.length, torch.where(f.refused == 0, f.length, f.length + 1), add, max_rows, parent)
+            except BaseException:
+                with torch.inference_mode():
+                    self.length.copy_(f.length)          # of the tables as they are now
+                raise
+        if src is not None:
             raise ValueError("src: rows go on as others in caches with share=True alone")
-        elif keep is None:
-            keep = held
+        return self._add(self.length, self.length if keep is None else keep, add, max_rows, parent)
+
+    def _add(self, held, keep, add, max_rows, parent) -> StepPlan:
         p = atspeed_page_plan(held, keep, add, self.block_table, self.free_pages, self.n_free, self.page_size, max_rows,
                               parent)
         with torch.inference_mode():                     # caches made under it are written outside it, too
