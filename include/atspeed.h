@@ -802,8 +802,10 @@ ATSPEED_API atspeed_status atspeed_page_copy(const atspeed_page_copy_args* args,
  * level-ordered tree).  ctx[b] + n_path[b] is then what the next step keeps.  A request with
  * a negative ctx, an n_path outside 0 .. max_path, a path that is not strictly ascending from
  * 0 up, or a position whose table entry is missing or outside 0 .. n_pool - 1 is left as it
- * was.  No two requests may hold a page that one of them writes.  Types, heads, strides and
- * paging as for atspeed_kv_append; B 1..1024, max_path 1..4096, n_layers 1..1024. */
+ * was and keeps ctx[b] alone.  Table entries behind a request's pages need not be its own: its
+ * row numbers must be of rows that it has (atspeed_kv_compact_keep looks).  No two requests may
+ * hold a page that one of them writes.  Types, heads, strides and paging as for
+ * atspeed_kv_append; B 1..1024, max_path 1..4096, n_layers 1..1024. */
 typedef struct {
   int32_t dtype, B, n_layers, n_kv_heads, d_head, page_size, max_pages, n_pool, max_path;
   atspeed_pages k_pages, v_pages;
@@ -814,6 +816,12 @@ typedef struct {
   const int32_t* n_path;
 } atspeed_kv_compact_args;
 ATSPEED_API atspeed_status atspeed_kv_compact(const atspeed_kv_compact_args* args, void* stream);
+/* The same, knowing the tokens whose pages each request holds (length [B], as atspeed_page_plan
+ * gives them) and saying what each keeps: a path with a row at or past length[b] - ctx[b] moves
+ * nothing, either; keep [B] gets ctx[b] + n_path[b] where the path was moved, ctx[b] where nothing
+ * was, length[b] where ctx[b] is negative (a refused request).  keep may be none of the inputs. */
+ATSPEED_API atspeed_status atspeed_kv_compact_keep(const atspeed_kv_compact_args* args, const int32_t* length,
+                                                   int32_t* keep, void* stream);
 
 /* Distillation of a draft from a teacher's top logits, per row: the divergence between the
  * teacher's distribution p and the draft's q over buckets -- each top column a bucket, all

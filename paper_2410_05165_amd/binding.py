@@ -28,6 +28,7 @@ SYMBOLS = ("atspeed_workspace_bytes", "atspeed_create", "atspeed_destroy", "atsp
            "atspeed_tree_attention_workspace_bytes", "atspeed_tree_attention", "atspeed_logit_rules",
            "atspeed_set_logit_rules", "atspeed_beam_select_workspace_bytes", "atspeed_beam_select",
            "atspeed_page_fork_workspace_bytes", "atspeed_page_fork", "atspeed_page_copy", "atspeed_kv_compact",
+           "atspeed_kv_compact_keep",
            "atspeed_distill_loss", "atspeed_distill_grad")
 KERNEL_CLASSES = ("qkv", "o", "gu", "down", "lm_head", "attention", "row", "select")
 

@@ -1,6 +1,7 @@
 // Pages of forked requests (atspeed_page_fork), copies of pages (atspeed_page_copy) and
 // accepted paths moved together (atspeed_kv_compact).
 #include <algorithm>
+#include <climits>
 
 #include "common.h"
 #include "paged.h"
@@ -298,6 +299,8 @@ struct MoveArgs {
   const int* ctx;
   const int* path;
   const int* n_path;
+  const int* held;             // [B], null: not known
+  int* keep;                   // [B], null: nobody asks
   int layers, chunks, head_shift, page_shift, n_pool, max_pages, max_path;
 };
 
@@ -334,6 +337,9 @@ __global__ void __launch_bounds__(kMoveThreads) kv_compact_kernel(MoveArgs a) {
   __shared__ int from[kMaxPath], to[kMaxPath];     // cache slots
   const int b = blockIdx.x / a.layers, layer = blockIdx.x % a.layers;
   const int n = a.n_path[b], ctx = a.ctx[b], tail = (1 << a.page_shift) - 1;
+  const int held = a.held ? a.held[b] : INT_MAX;
+  const bool says = a.keep && layer == 0 && threadIdx.x == 0;
+  if (says) a.keep[b] = ctx < 0 ? held : ctx;
   if (n < 1 || n > a.max_path || ctx < 0) return;
   const int* path = a.path + (int64_t)b * a.max_path;
   const int* table = a.table + (int64_t)b * a.max_pages;
@@ -346,12 +352,13 @@ __global__ void __launch_bounds__(kMoveThreads) kv_compact_kernel(MoveArgs a) {
   };
   for (int i = threadIdx.x; i < n; i += kMoveThreads) {
     const int row = path[i];
-    ok = ok && row > (i ? path[i - 1] : -1);
+    ok = ok && row > (i ? path[i - 1] : -1) && (long long)ctx + row < held;
     if (!ok) break;
     from[i] = slot_of((long long)ctx + row);
     to[i] = slot_of((long long)ctx + i);
   }
   if (!__syncthreads_and(ok)) return;
+  if (says) a.keep[b] = ctx + n;
   const char* k = a.kp.data + layer * a.k_layer;
   const char* v = a.vp.data + layer * a.v_layer;
   for (int c = threadIdx.x; c < 2 * a.chunks; c += kMoveThreads) {
@@ -435,6 +442,24 @@ static size_t lay_out(ForkArgs& p, char* base) {
   return at;
 }
 
+static atspeed_status compact(const atspeed_kv_compact_args* args, const int32_t* length, int32_t* keep, void* stream) {
+  if (!args) return fail(ATSPEED_E_INVALID, "args is null");
+  MoveArgs p{};
+  ST_TRY(move_args(*args, p));
+  if (args->B < 1 || args->B > kMaxRequests) return fail(ATSPEED_E_INVALID, "B must be 1..1024");
+  if (args->max_pages < 1) return fail(ATSPEED_E_INVALID, "max_pages must be >= 1");
+  if (args->max_path < 1 || args->max_path > kMaxPath) return fail(ATSPEED_E_INVALID, "max_path must be 1..4096");
+  if (!args->block_table || !args->ctx || !args->path || !args->n_path)
+    return fail(ATSPEED_E_INVALID, "kv compact: null pointer");
+  p.table = args->block_table; p.ctx = args->ctx; p.path = args->path; p.n_path = args->n_path;
+  p.max_pages = args->max_pages; p.max_path = args->max_path;
+  p.held = length; p.keep = keep;
+  const long long groups = (long long)args->B * args->n_layers;
+  hipLaunchKernelGGL(kv_compact_kernel, dim3((unsigned)groups), dim3(kMoveThreads), 0, (hipStream_t)stream, p);
+  HIP_TRY(hipGetLastError());
+  return ATSPEED_OK;
+}
+
 }  // namespace atspeed
 
 using namespace atspeed;
@@ -491,20 +516,16 @@ atspeed_status atspeed_page_copy(const atspeed_page_copy_args* args, void* strea
 }
 
 atspeed_status atspeed_kv_compact(const atspeed_kv_compact_args* args, void* stream) {
-  if (!args) return fail(ATSPEED_E_INVALID, "args is null");
-  MoveArgs p{};
-  ST_TRY(move_args(*args, p));
-  if (args->B < 1 || args->B > kMaxRequests) return fail(ATSPEED_E_INVALID, "B must be 1..1024");
-  if (args->max_pages < 1) return fail(ATSPEED_E_INVALID, "max_pages must be >= 1");
-  if (args->max_path < 1 || args->max_path > kMaxPath) return fail(ATSPEED_E_INVALID, "max_path must be 1..4096");
-  if (!args->block_table || !args->ctx || !args->path || !args->n_path)
-    return fail(ATSPEED_E_INVALID, "kv compact: null pointer");
-  p.table = args->block_table; p.ctx = args->ctx; p.path = args->path; p.n_path = args->n_path;
-  p.max_pages = args->max_pages; p.max_path = args->max_path;
-  const long long groups = (long long)args->B * args->n_layers;
-  hipLaunchKernelGGL(kv_compact_kernel, dim3((unsigned)groups), dim3(kMoveThreads), 0, (hipStream_t)stream, p);
-  HIP_TRY(hipGetLastError());
-  return ATSPEED_OK;
+  return compact(args, nullptr, nullptr, stream);
+}
+
+atspeed_status atspeed_kv_compact_keep(const atspeed_kv_compact_args* args, const int32_t* length, int32_t* keep, void* stream) {
+  if (!length || !keep) return fail(ATSPEED_E_INVALID, "kv compact: length or keep is null");
+  if (args)
+    for (const void* in : {(const void*)args->block_table, (const void*)args->ctx, (const void*)args->path,
+                           (const void*)args->n_path, (const void*)length})
+      if (in == keep) return fail(ATSPEED_E_INVALID, "kv compact: an output is one of the inputs");
+  return compact(args, length, keep, stream);
 }
 
 }  // extern "C"

@@ -631,9 +631,9 @@ PyObject* page_copy(PyObject*, PyObject* const* o, Py_ssize_t n) {
   });
 }
 
-// k_cache, v_cache, block_table, ctx, path, n_path, stream
+// k_cache, v_cache, block_table, ctx, path, n_path, length, stream
 PyObject* kv_compact(PyObject*, PyObject* const* o, Py_ssize_t n) {
-  return guarded(n, 7, [&]() -> PyObject* {
+  return guarded(n, 8, [&]() -> PyObject* {
     const Layers l = layers(o[0], o[1]);
     const at::Tensor& table = tensor(o[2], "block_table");
     const at::Tensor& path = tensor(o[4], "path");
@@ -648,10 +648,15 @@ PyObject* kv_compact(PyObject*, PyObject* const* o, Py_ssize_t n) {
     a.ctx = want_i32(o[3], "ctx", {B}, l.c.dev);
     a.path = want_i32(o[4], "path", {B, P}, l.c.dev);
     a.n_path = want_i32(o[5], "n_path", {B}, l.c.dev);
-    void* const st = stream_of(o[6]);
-    enqueue([&] { return atspeed_kv_compact(&a, st); });
+    const int32_t* const length = want_i32(o[6], "length", {B}, l.c.dev);
+    at::Tensor keep;
+    if (length) keep = fresh({B}, c10::ScalarType::Int, l.c.dev);
+    int32_t* const to = length ? address<int32_t>(keep) : nullptr;
+    void* const st = stream_of(o[7]);
+    enqueue([&] { return length ? atspeed_kv_compact_keep(&a, length, to, st) : atspeed_kv_compact(&a, st); });
     written(o[0]);
     written(o[1]);
+    if (length) return THPVariable_Wrap(keep);
     Py_RETURN_NONE;
   });
 }

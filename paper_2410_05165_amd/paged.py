@@ -149,12 +149,14 @@ def atspeed_page_copy(k_cache, v_cache, src, dst, length):
     _run(_marshal.page_copy, k_cache, k_cache, v_cache, src, dst, length)
 
 
-def atspeed_kv_compact(k_cache, v_cache, block_table, ctx, path, n_path):
+def atspeed_kv_compact(k_cache, v_cache, block_table, ctx, path, n_path, length=None):
     """Moves the new rows path[b][:n_path[b]] (ascending row numbers) of each request to positions ctx[b], ctx[b] + 1, ...
 
-    Caches as for atspeed_page_copy; block_table [B, max_pages], ctx, n_path [B], path [B, max_path] int32.
+    Caches as for atspeed_page_copy; block_table [B, max_pages], ctx, n_path [B], path [B, max_path] int32.  With length
+    [B], the tokens whose pages each request holds, returns what each keeps [B]: the context and the path, the context
+    alone where the path was not moved, the length where the context is negative (atspeed_kv_compact_keep).
     """
-    _run(_marshal.kv_compact, k_cache, k_cache, v_cache, block_table, ctx, path, n_path)
+    return _run(_marshal.kv_compact, k_cache, k_cache, v_cache, block_table, ctx, path, n_path, length)
 
 
 class PagedKV:
@@ -223,9 +225,8 @@ class PagedKV:
     def compact(self, plan: StepPlan, path, n_path):
         """Moves each request's accepted rows path[b][:n_path[b]] of the plan behind its context, in every layer.
 
-        The row numbers ascend strictly, as those down a tree do; a path that does not moves nothing.
-        Returns what the next plan keeps: the context and the path (the context alone where n_path is below 1 or the
-        request was refused: then its length).
+        The row numbers ascend strictly from 0 or above, as those down a tree do, and are of rows that the plan added; a
+        path that is otherwise, or longer than path's width, moves nothing.  Returns what the next plan keeps: the context
+        and the path, the context alone where nothing is moved, the length of a request that was refused.
         """
-        atspeed_kv_compact(self.k, self.v, self.block_table, plan.ctx, path, n_path)
-        return torch.where(plan.ctx < 0, self.length, plan.ctx + n_path.clamp(min=0))
+        return atspeed_kv_compact(self.k, self.v, self.block_table, plan.ctx, path, n_path, self.length)

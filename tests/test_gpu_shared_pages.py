@@ -1,4 +1,4 @@
-"""PagedKV with shared pages where a call is refused."""
+"""PagedKV where a call is refused or given what it should not be."""
 import numpy as np
 import pytest
 
@@ -7,7 +7,7 @@ pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
 from paper_2410_05165_amd import paged  # noqa: E402
-from paper_2410_05165_amd.paged import PagedKV  # noqa: E402
+from paper_2410_05165_amd.paged import PagedKV, atspeed_kv_compact  # noqa: E402
 
 DEV = "cuda:0"
 F32 = torch.float32
@@ -87,3 +87,69 @@ def test_what_fails_behind_the_fork_leaves_tables_and_lengths_that_fit(monkeypat
     assert not bool(a.refused.any()) and torch.equal(a.slot, b.slot) and torch.equal(a.ctx, b.ctx)
     for name in ("length", "n_free", "shared", "k", "v"):
         assert torch.equal(getattr(kv, name), getattr(other, name)), name
+
+
+@pytest.mark.parametrize("share", [False, True])
+def test_paths_that_are_none_move_nothing_and_keep_the_context(share):
+    """Paths that do not ascend, that are longer than given or name rows that the request did not add: what is kept is the
+    context, the caches of every request are as they were, and good paths beside them move."""
+    B = 9
+    kv = PagedKV(2, 60, 4, 1, 64, B, 40, dtype=F32, share=share)
+    fill(kv, kv.plan(ints([0] * B), ints([6] * B), 6 * B), 6 * B, 1)
+    plan = kv.plan(kv.length.clone(), ints([5] * B), 5 * B)
+    fill(kv, plan, 5 * B, 100)
+    before = kv.k.clone()
+    path = ints([[0, 2, 4], [0, 2, 1], [2, 2, 3], [0, 1, 2], [0, 2, 5], [-1, 1, 2], [0, 3, 30], [1, 2, 3],
+                 [2 ** 31 - 1, -2 ** 31, 0]])
+    n_path = ints([3, 3, 2, 4, 3, 2, 3, -2, 3])
+    keep = kv.compact(plan, path, n_path)
+    assert keep.tolist() == [9] + [6] * 8
+    assert keep.dtype == torch.int32
+    x = kv.k[0, :, :, 0, 0].reshape(-1)
+    slot = lambda b, p: int(kv.block_table[b, p // 4]) * 4 + p % 4  # noqa: E731
+    assert [float(x[slot(0, p)]) for p in (6, 7, 8)] == [100.0, 102.0, 104.0]
+    mine = torch.zeros(kv.k.shape[1], dtype=torch.bool)
+    mine[kv.block_table[0, :3].cpu().long()] = True
+    assert torch.equal(kv.k[:, ~mine.to(DEV)], before[:, ~mine.to(DEV)])
+    # the next step goes on behind what was kept
+    p = kv.plan(keep, ints([1] * B), B)
+    assert not bool(p.refused.any()) and p.row_pos.tolist() == [9] + [6] * 8
+
+
+def test_compact_keeps_the_length_of_refused_requests():
+    kv = grown(share=False)
+    fill(kv, kv.plan(ints([0] * 4), ints([3] * 4), 12), 12, 1)
+    plan = kv.plan(ints([3, 9, 2, 3]), ints([2, 2, 0, 2]), 12)       # the second keeps more than it holds
+    keep = kv.compact(plan, ints([[0, 1]] * 4), ints([1, 2, 0, 2]))
+    assert keep.tolist() == [4, 3, 2, 5]
+
+
+def test_compact_refuses_what_the_call_refuses():
+    kv = grown(share=False)
+    fill(kv, kv.plan(ints([0] * 4), ints([3] * 4), 12), 12, 1)
+    plan = kv.plan(ints([3] * 4), ints([2] * 4), 8)
+    path, n = ints([[0, 1]] * 4), ints([1] * 4)
+    before = kv.k.clone()
+    for p, m in ((path.long(), n), (path, n.long()), (path[:2], n), (path, n[:2]), (path[0], n), (path[:, :0], n), (path.t(), n),
+                 (path, n[:, None]), (path.cpu(), n)):
+        with pytest.raises((ValueError, RuntimeError)):
+            kv.compact(plan, p, m)
+    assert torch.equal(kv.k, before)
+    assert kv.compact(plan, path, n).tolist() == [4] * 4
+
+
+def test_rows_past_a_requests_pages_do_not_reach_another_ones():
+    """Table entries behind a request's pages are what they were: a path that names rows there moves nothing."""
+    k = torch.arange(6 * 64, dtype=F32, device=DEV).view(6, 1, 1, 64).clone()
+    v = -k
+    table, ctx = ints([[0, 1, 4, 5], [4, 5, 2, 3]]), ints([1, 1])     # the first row's last two entries are the second's pages
+    path, n = ints([[0, 2], [0, 2]]), ints([2, 2])
+    before = k.clone()
+    keep = atspeed_kv_compact(k, v, table, ctx, path, n, ints([2, 4]))
+    assert keep.tolist() == [1, 3]
+    before[2] = before[3]                                             # position 3 of the second request to position 2
+    assert torch.equal(k, before) and torch.equal(v, -before)
+    assert atspeed_kv_compact(k, v, table, ctx, path, n) is None
+    for wrong in (ctx.long(), ctx[:1], ctx.cpu()):
+        with pytest.raises(ValueError):
+            atspeed_kv_compact(k, v, table, ctx, path, n, wrong)
