@@ -146,7 +146,7 @@ constexpr int kSlots = 2 * kForkOne;
 
 __device__ __forceinline__ void decide(const ForkArgs& p) {
   __shared__ int part[kForkOne / 64], gone[kPieces], page[kSlots], lowest[kSlots];
-  const int j = threadIdx.x, B = p.a.B, lane = j & 63, chunks = (p.a.n_pool + 63) / 64;
+  const int j = threadIdx.x, B = p.a.B, lane = j & 63, chunks = (int)(((long long)p.a.n_pool + 63) / 64);
   const int q = j < B ? fresh(&p.last[j]) : -1;
   for (int i = j; i < kSlots; i += kForkOne) {
     page[i] = -1;
@@ -167,13 +167,13 @@ __device__ __forceinline__ void decide(const ForkArgs& p) {
     int left[8];
 #pragma unroll
     for (int o = 0; o < 8; ++o) {
-      const int i = (c0 + o * (kForkOne / 64)) * 64 + lane;
-      left[o] = i < p.a.n_pool ? fresh(&p.a.shared[i]) : 0;
+      const unsigned i = (unsigned)(c0 + o * (kForkOne / 64)) * 64 + lane;     // past 2^31 behind the largest pools
+      left[o] = i < (unsigned)p.a.n_pool ? fresh(&p.a.shared[i]) : 0;
     }
 #pragma unroll
     for (int o = 0; o < 8; ++o) {
       const int n = __popcll(__ballot(left[o] < 0));
-      if (n && lane == 0) atomicAdd(&gone[(c0 + o * (kForkOne / 64)) * 64 / p.piece], n);
+      if (n && lane == 0) atomicAdd(&gone[(unsigned)(c0 + o * (kForkOne / 64)) * 64 / p.piece], n);
     }
   }
   sync_memory();                           // nobody looks at the pool any more
@@ -210,20 +210,21 @@ __device__ __forceinline__ Stack stack_of(const ForkArgs& p) {
 // Holders and free list of a piece of the pool, a wave.
 template <class Row>
 __device__ __forceinline__ void write_piece(const ForkArgs& p, const Stack& s, int i, int lane, Row row) {
-  const int begin = i * p.piece, end = min(begin + p.piece, p.a.n_pool);
-  int at = s.F + fresh(&p.gone[i]);
-  for (int c0 = begin; c0 < end; c0 += 64) {
-    const int c = c0 + lane, left = c < end ? fresh(&p.a.shared[c]) : 0;
+  const unsigned begin = (unsigned)i * p.piece, end = min(begin + p.piece, (unsigned)p.a.n_pool);
+  long long at = (long long)s.F + fresh(&p.gone[i]);
+  for (unsigned c0 = begin; c0 < end; c0 += 64) {
+    const unsigned c = c0 + lane;
+    const int left = c < end ? fresh(&p.a.shared[c]) : 0;
     const u64 out = __ballot(left < 0);
     if (left < 0) {
       p.a.shared[c] = 0;
-      const int place = at + __popcll(out & ((1ull << lane) - 1));
+      const long long place = at + __popcll(out & ((1ull << lane) - 1));
       if (place < s.top) {
-        p.a.free_pages[place] = c;
+        p.a.free_pages[place] = (int)c;
       } else if (place < s.have) {
         const int j = fresh(&p.taker[s.have - 1 - place]);
-        p.a.block_table[(int64_t)j * p.a.max_pages + row(j).full] = c;
-        p.a.copy_dst[j] = c;
+        p.a.block_table[(int64_t)j * p.a.max_pages + row(j).full] = (int)c;
+        p.a.copy_dst[j] = (int)c;
       }
     }
     at += __popcll(out);
@@ -430,8 +431,8 @@ static size_t lay_out(ForkArgs& p, char* base) {
     return q;
   };
   p.piece = 256;
-  while (p.piece < (a.n_pool + kPieces - 1) / kPieces) p.piece *= 2;
-  p.pieces = (a.n_pool + p.piece - 1) / p.piece;
+  while (p.piece < ((long long)a.n_pool + kPieces - 1) / kPieces) p.piece *= 2;
+  p.pieces = (int)(((long long)a.n_pool + p.piece - 1) / p.piece);
   p.shift = log2_of(a.page_size);
   p.next = (int*)take((size_t)a.B * a.max_pages * 4);
   p.last = (int*)take((size_t)a.B * 4);

@@ -7,7 +7,7 @@ pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
 from paper_2410_05165_amd import paged  # noqa: E402
-from paper_2410_05165_amd.paged import PagedKV, atspeed_kv_compact  # noqa: E402
+from paper_2410_05165_amd.paged import PagedKV, atspeed_kv_compact, atspeed_page_fork  # noqa: E402
 
 DEV = "cuda:0"
 F32 = torch.float32
@@ -153,3 +153,21 @@ def test_rows_past_a_requests_pages_do_not_reach_another_ones():
     for wrong in (ctx.long(), ctx[:1], ctx.cpu()):
         with pytest.raises(ValueError):
             atspeed_kv_compact(k, v, table, ctx, path, n, wrong)
+
+
+def test_a_pool_of_nearly_two_to_the_31_pages():
+    """The last pages of the largest pools: their numbers, holders and pieces stay inside 32 bits."""
+    for pool in ((1 << 31) - 1, (1 << 31) - 70):
+        shared = torch.zeros(pool, dtype=torch.int32, device=DEV)
+        free = torch.full((pool,), -1, dtype=torch.int32, device=DEV)
+        free[:3] = ints([50, 60, 70])
+        n_free, last = ints([3]), pool - 1
+        table = ints([[0, 5, last], [last - 1, 3, 9], [1 << 20, last - 64, 8]])
+        f = atspeed_page_fork(ints([3, 3, 3]), ints([1, 0, 3]), table, free, n_free, shared, 1, src=ints([0, -1, 1]))
+        # row 0 keeps page 0, row 1 nothing, row 2 goes on as row 1: its own pages come free, ascending
+        assert f.length.tolist() == [1, 0, 3] and f.refused.tolist() == [0, 0, 0]
+        assert table[2].tolist() == [last - 1, 3, 9] and int(table[0, 0]) == 0
+        assert int(n_free) == 8
+        assert free[:8].tolist() == [50, 60, 70, 5, 8, 1 << 20, last - 64, last]
+        assert int(shared.min()) == int(shared.max()) == 0
+        del shared, free
