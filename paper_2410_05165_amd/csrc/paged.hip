@@ -152,14 +152,16 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(PlanArgs p) {
   };
   auto stack = [&](int s) { return s < F ? a.free_pages[s] : released(s - F); };
 
-  const int step = gridDim.x * kPlanThreads, at = blockIdx.x * kPlanThreads + tid;
-  for (int t = at; t < T; t += step) {
-    const int b = owner(take_off, B, t);
+  // unsigned: numbers below 2^31 and a step more
+  const unsigned step = gridDim.x * kPlanThreads, at = blockIdx.x * kPlanThreads + tid;
+  for (unsigned i = at; i < (unsigned)T; i += step) {
+    const int t = (int)i, b = owner(take_off, B, t);
     a.block_table[(size_t)b * most + before_s[b] + (t - take_off[b])] = stack(have - 1 - t);
   }
-  for (int s = F + at; s < top; s += step) a.free_pages[s] = released(s - F);
+  for (unsigned s = F + at; s < (unsigned)top; s += step) a.free_pages[s] = released((int)(s - F));
 
-  for (int r = at; r < a.max_rows; r += step) {
+  for (unsigned row = at; row < (unsigned)a.max_rows; row += step) {
+    const int r = (int)row;
     int user = -1, pos = -1, slot = -1, ts = -1, b = 0, i = 0, depth = 0;
     if (r < n_rows) {
       b = owner(row_off, B, r);
