@@ -12,23 +12,11 @@ the target's top logits: ``distill`` is the loss with its gradient for autograd,
 """
 from __future__ import annotations
 
+import functools
 import math
 from typing import Optional
 
-import torch
-
 from .binding import AlignArgs, Engine
-
-try:
-    from .paged import _marshal, _run
-except ImportError as e:                                 # AlignTrainer needs libatspeed.so alone
-    _missing = str(e)
-
-    class _marshal:
-        distill_loss = distill_grad = None
-
-    def _run(*args):
-        raise ImportError(_missing)
 
 MODES = {"S": 0, "R": 1}
 
@@ -43,6 +31,13 @@ def cosine_lr(step: int, total: int, peak: float, warmup: int) -> float:
     return 0.5 * peak * (1.0 + math.cos(math.pi * x))
 
 
+# Loaded by the first call: the schedule and the trainer come without PyTorch and _marshal.so.
+@functools.lru_cache(maxsize=None)
+def _calls():
+    from .paged import _marshal, _run
+    return _run, _marshal
+
+
 def atspeed_distill_loss(logits, teacher_logit, teacher_index, tail=None, weight=None, temperature: float = 1.0,
                          reverse: bool = False):
     """The divergence of a draft's logits [rows, cols] (fp32 or bf16) from a teacher's top logits, a number a row.
@@ -52,28 +47,36 @@ def atspeed_distill_loss(logits, teacher_logit, teacher_index, tail=None, weight
     has none); weight [rows] fp32.  reverse: sum q log(q / p), which needs the tail, for sum p log(p / q).  Returns
     (loss [rows], saved), saved for atspeed_distill_grad.
     """
-    return _run(_marshal.distill_loss, logits, logits, teacher_logit, teacher_index, tail, weight, temperature, reverse)
+    run, calls = _calls()
+    return run(calls.distill_loss, logits, logits, teacher_logit, teacher_index, tail, weight, temperature, reverse)
 
 
 def atspeed_distill_grad(logits, teacher_index, saved, grad_loss=None, temperature: float = 1.0, out=None):
     """The gradient of atspeed_distill_loss with respect to the logits, in their type; grad_loss [rows] fp32 (None: 1)."""
-    return _run(_marshal.distill_grad, logits, logits, teacher_index, saved, grad_loss, temperature, out)
+    run, calls = _calls()
+    return run(calls.distill_grad, logits, logits, teacher_index, saved, grad_loss, temperature, out)
 
 
-class _Distill(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, logits, teacher_logit, teacher_index, tail, weight, temperature, reverse):
-        loss, saved = atspeed_distill_loss(logits, teacher_logit, teacher_index, tail, weight, temperature, reverse)
-        ctx.save_for_backward(logits, teacher_index, saved)
-        ctx.temperature = temperature
-        return loss
+@functools.lru_cache(maxsize=None)
+def _autograd():
+    import torch
 
-    @staticmethod
-    @torch.autograd.function.once_differentiable
-    def backward(ctx, grad_loss):
-        logits, teacher_index, saved = ctx.saved_tensors
-        grad = atspeed_distill_grad(logits, teacher_index, saved, grad_loss.contiguous(), ctx.temperature)
-        return grad, None, None, None, None, None, None
+    class Distill(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, logits, teacher_logit, teacher_index, tail, weight, temperature, reverse):
+            loss, saved = atspeed_distill_loss(logits, teacher_logit, teacher_index, tail, weight, temperature, reverse)
+            ctx.save_for_backward(logits, teacher_index, saved)
+            ctx.temperature = temperature
+            return loss
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, grad_loss):
+            logits, teacher_index, saved = ctx.saved_tensors
+            grad = atspeed_distill_grad(logits, teacher_index, saved, grad_loss.contiguous(), ctx.temperature)
+            return grad, None, None, None, None, None, None
+
+    return Distill
 
 
 def distill(logits, teacher_logit, teacher_index, tail=None, weight=None, temperature: float = 1.0, reverse: bool = False):
@@ -85,7 +88,7 @@ def distill(logits, teacher_logit, teacher_index, tail=None, weight=None, temper
     for name, t in (("teacher_logit", teacher_logit), ("tail", tail), ("weight", weight)):
         if t is not None and t.requires_grad:
             raise ValueError(f"{name}: no gradient flows to it; detach it")
-    return _Distill.apply(logits, teacher_logit, teacher_index, tail, weight, temperature, reverse)
+    return _autograd().apply(logits, teacher_logit, teacher_index, tail, weight, temperature, reverse)
 
 
 class AlignTrainer:
@@ -98,6 +101,7 @@ class AlignTrainer:
 
     def __init__(self, eng: Engine, mode: str, alpha: float = 1.0, lr: float = 1e-3, betas=(0.9, 0.999),
                  eps: float = 1e-8, weight_decay: float = 0.01):
+        torch = eng.torch
         if eng.draft_dev is None:
             raise ValueError("the engine has no draft model")
         self.eng = eng
