@@ -19,6 +19,7 @@
 
 #include "common.h"
 #include "paged.h"
+#include "wave.h"
 
 namespace atspeed {
 
@@ -64,21 +65,6 @@ __device__ __forceinline__ int new_rows(const TreeAttnArgs& a, int b, int& r0) {
   return sane ? end - begin : 0;
 }
 
-// Lane i: the sum of lanes 0 .. i.
-template <class N>
-__device__ __forceinline__ N wave_scan(N x) {
-  const auto from = [&](auto ctrl, auto rows) {
-    return __builtin_bit_cast(N, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), ctrl.value, rows.value, 0xf, false));
-  };
-  typedef std::integral_constant<int, 0xf> All;
-  x += from(std::integral_constant<int, 0x111>{}, All{});   // row_shr: 1, 2, 4, 8 lanes of a row of 16
-  x += from(std::integral_constant<int, 0x112>{}, All{});
-  x += from(std::integral_constant<int, 0x114>{}, All{});
-  x += from(std::integral_constant<int, 0x118>{}, All{});
-  x += from(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});   // row_bcast: 15 to the next row
-  x += from(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});   // 31 to the rows behind
-  return x;
-}
 __device__ __forceinline__ int round_up64(int n) { return (n + 63) & ~63; }
 
 // One workgroup's share: a request, a key/value head, a tile of its queries (row i, head

@@ -1,6 +1,8 @@
 // Reductions over a wave, 64-bit exponentials and loads at any element, for the operators on
 // rows of logits.
 #pragma once
+#include <type_traits>
+
 #include "common.h"
 
 namespace atspeed {
@@ -69,14 +71,19 @@ __device__ __forceinline__ F wave_sum(F x) {
   return x;
 }
 
-// Sum of the lanes up to this one.
-__device__ __forceinline__ int wave_scan(int x) {
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);     // row_shr 1, 2, 4, 8
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, true);     // the rows before: row_bcast 15, 31
-  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, true);
+// Lane i: the sum of lanes 0 .. i.
+template <class N>
+__device__ __forceinline__ N wave_scan(N x) {
+  const auto from = [&](auto ctrl, auto rows) {
+    return __builtin_bit_cast(N, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), ctrl.value, rows.value, 0xf, false));
+  };
+  typedef std::integral_constant<int, 0xf> All;
+  x += from(std::integral_constant<int, 0x111>{}, All{});   // row_shr: 1, 2, 4, 8 lanes of a row of 16
+  x += from(std::integral_constant<int, 0x112>{}, All{});
+  x += from(std::integral_constant<int, 0x114>{}, All{});
+  x += from(std::integral_constant<int, 0x118>{}, All{});
+  x += from(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});   // row_bcast: 15 to the next row
+  x += from(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});   // 31 to the rows behind
   return x;
 }
 
