@@ -1,4 +1,6 @@
-"""PagedKV where a call is refused or given what it should not be."""
+"""PagedKV where a call is refused or given what it should not be, beams that end, the largest pools."""
+import math
+
 import numpy as np
 import pytest
 
@@ -7,7 +9,7 @@ pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
 from paper_2410_05165_amd import paged  # noqa: E402
-from paper_2410_05165_amd.paged import PagedKV, atspeed_kv_compact, atspeed_page_fork  # noqa: E402
+from paper_2410_05165_amd.paged import PagedKV, atspeed_beam_select, atspeed_kv_compact, atspeed_page_fork  # noqa: E402
 
 DEV = "cuda:0"
 F32 = torch.float32
@@ -153,6 +155,65 @@ def test_rows_past_a_requests_pages_do_not_reach_another_ones():
     for wrong in (ctx.long(), ctx[:1], ctx.cpu()):
         with pytest.raises(ValueError):
             atspeed_kv_compact(k, v, table, ctx, path, n, wrong)
+
+
+def test_beams_that_end_are_padded_rows_of_a_captured_step():
+    """A row a beam by the plan's row_off, ended and missing beams among them, without a word to the host: captured and
+    replayed it gives the beams of a search over whole sequences."""
+    U, K, V, P, eos, steps = 2, 3, 11, 5, 4, 4
+    rng = np.random.default_rng(0)
+    table = torch.from_numpy(rng.normal(0, 2, (V, V))).float().to(DEV)   # logits behind a token
+    table[:, 9:] = -math.inf
+    lp = torch.log_softmax(table.double(), 1).cpu().numpy()
+    kv = PagedKV(2, 80, 4, 1, 64, U * K, 24, dtype=F32, share=True)
+    add = ints([3, 0, 0, 3, 0, 0])
+    kv.plan(None, add, 6)
+    first = ints([2, 7])
+    every = ints(np.arange(U + 1) * K)
+    b = atspeed_beam_select(table[first.long()], ints(range(U + 1)), K, row_id=ints([0, K]),
+                            paths=ints(np.zeros((U * K, P))), path_len=ints(np.zeros(U * K)))
+    state = dict(parent=b.parent.view(-1).clone(), token=b.token.view(-1).clone(), score=b.score.view(-1).clone(),
+                 paths=b.paths.view(U * K, P).clone(), path_len=b.path_len.view(-1).clone())
+
+    def step():
+        parent, token = state["parent"], state["token"]
+        live = (parent >= 0) & (token >= 0) & (token != eos)
+        ended = (parent >= 0) & ~live
+        p = kv.plan(None, live.int(), U * K, src=parent)
+        logits = table[token[p.row_user.clamp(min=0).long()].clamp(min=0).long()]
+        x = torch.ones((U * K, 1, 64), device=DEV)
+        for layer in range(2):
+            kv.append(layer, p, x, x)
+        wide = logits[p.row_off[:-1].clamp(max=U * K - 1).long()]
+        b = atspeed_beam_select(wide, every, K, score=state["score"], done=ended.int(), paths=state["paths"],
+                                path_len=state["path_len"])
+        for name, x in (("parent", b.parent), ("token", b.token), ("score", b.score), ("paths", b.paths), ("path_len", b.path_len)):
+            state[name].copy_(x.view(state[name].shape))
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(steps - 1):
+        graph.replay()
+        torch.cuda.synchronize()
+    for u in range(U):
+        beams = [([], 0.0, False, int(first[u]))]
+        for _ in range(steps + 1):
+            cand = []
+            for i, (path, s, done, last) in enumerate(beams):
+                if done:
+                    cand.append((-s, i, -1, path, True, last))
+                else:
+                    cand += [(-(s + lp[last, v]), i, v, path + [v], v == eos, v) for v in range(V) if lp[last, v] > -math.inf]
+            cand.sort(key=lambda c: c[:3])
+            beams = [(c[3], -c[0], c[4], c[5]) for c in cand[:K]]
+        for j, (path, s, done, _) in enumerate(beams):
+            at = u * K + j
+            assert state["paths"][at, :int(state["path_len"][at])].tolist() == path
+            # rounded to fp32 in each of steps + 1, behind a logarithm that is off by 2.4e-10
+            assert abs(float(state["score"][at]) - s) <= (steps + 1) * (2.0 ** -24 * abs(s) + 2.5e-10)
 
 
 def test_a_pool_of_nearly_two_to_the_31_pages():
