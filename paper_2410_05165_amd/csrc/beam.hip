@@ -23,7 +23,7 @@ constexpr int kBeamThreads = 256, kBeamWaves = kBeamThreads / 64;
 constexpr int kLane = 16;              // columns of a lane in a tile
 constexpr int kTile = 64 * kLane;      // columns of a tile, which a wave takes at once
 constexpr int kMaxBeams = 256;         // k
-constexpr int kSlots = 4096;           // waves on the card at once, four a SIMD
+constexpr int kSlots = 4096;           // waves on the card at once, four a SIMD (five with small pools)
 
 // Logits (no NaN) to whole numbers of the same order and as many bits, -0 as 0; and back.
 template <class T>
@@ -277,9 +277,9 @@ __device__ __forceinline__ int first_cut(const BeamArgs& p, int lane) {
 // of its exponentials, and its k best columns behind a bound that rises with them.  No barrier,
 // and the whole row where that fills the card: parts cost a pool and a first bound each.
 // Bound by vector instructions, of which a tile's exponentials are half and the selection,
-// which grows with k, a quarter: 5,661 rows of 33,024 bf16 columns with 50 beams each 184 us
-// (374 MB, 2.0 TB/s; with 10 beams 160, without exponentials or selection 80), 287 rows with 10
-// 17.5.  A workgroup per row with a sorted pool took 393 and 39.
+// which grows with k, a quarter: 5,661 rows of 33,024 bf16 columns with 50 beams each 180 to 186 us
+// (374 MB, 2.0 TB/s; the call with 10 beams 153), 287 rows with 10 17.6.  A workgroup per row with
+// a sorted pool took 393 and 39; without exponentials or selection it was 80.
 template <class T, int P, bool PROBS>
 __global__ void __launch_bounds__(kBeamThreads) beam_rows_kernel(BeamArgs p) {
   __shared__ u64 keys[kBeamWaves * P * 64];
@@ -370,8 +370,8 @@ __global__ void __launch_bounds__(kBeamThreads) beam_rows_kernel(BeamArgs p) {
 // entries, as many as the workgroup holds; the k-th of the threads' largest is a bound that
 // few more than k of them pass; these are ranked, the k best stay.  A list is left once its
 // last entry is behind them.  Mostly one round or two.  Bound by latency, a chain of loads and
-// barriers: ten lists of ten 7.3 us, 32 requests of 99 lists of ten 10.5, 128 of 45
-// rows, a third of them in three parts, 19.
+// barriers: ten lists of ten 7.4 us, 32 requests of 99 lists of ten 10.9, 128 of 45
+// rows, a third of them in three parts, 20.
 constexpr int kEach = 4, kJoinLists = 1024;
 constexpr short kItself = -1;              // length of the list of a row that has ended
 
@@ -639,8 +639,8 @@ static atspeed_status launch_join(const BeamArgs& p, hipStream_t st) {
 template <class T>
 static atspeed_status run_join(const BeamArgs& p, hipStream_t st) {
   // Few entries a request, or many requests: smaller workgroups, more of them on a CU (both
-  // kernels, us, 256 threads and 1,024: 10 rows of 1,024 columns 12.4 and 15.9, 32 requests of 9
-  // rows of 33,024 with 10 beams 26.6 and 28.4; but 128 of 45 rows with 50 220 and 189).
+  // kernels, us, 256 threads and 1,024: 10 rows of 1,024 columns 13.0 and 15.9, 32 requests of 9
+  // rows of 33,024 with 10 beams 27.2 and 28.4; but 128 of 45 rows with 50 189 and 187).
   const long long entries = p.most_lists(p.a.n_rows) * p.a.k;
   return p.a.B > 256 || entries <= 1024LL * p.a.B ? launch_join<T, 256>(p, st) : launch_join<T, 1024>(p, st);
 }
@@ -672,11 +672,11 @@ static atspeed_status check_beam(const atspeed_beam_select_args& a) {
 
 // Parts of a row: a wave each, enough waves for the card, but not many more lists a request
 // than one round of the second kernel takes in (64 rows of one request, 128 beams: parts of one
-// tile 113 us, of two 89, of five 67; 287 rows of 32 requests: 7 parts 27.6, 11 26.6, 17 27.9).
+// tile 89 us, of two 56, of five 50; 287 rows of 32 requests: 7 parts 27.8, 11 26.5, 17 27.3).
 // As many rows as fill the card whole are not cut; few waves behind them would leave it half
-// empty, so that those rows are (both kernels, us, with them in 1 part, 2 and 3: 4,300 rows 162,
-// 144 and 139, 5,661 185, 184 and 177; 7,000 217, 215 and 221, 8,100 240, 249 and 255; all of
-// 5,661 rows in 2: 4% slower).
+// empty, so that those rows are (both kernels, us, with them in 1 part, 2 and 3: 4,300 rows 159,
+// 138 and 138, 5,661 187, 184 and 180; 7,000 215, 216 and 221, 8,100 239, 246 and 251; all of
+// 5,661 rows in 2 was 4% slower).
 static void cut_rows(const atspeed_beam_select_args& a, BeamArgs& p) {
   const int tiles = (a.n_cols + kTile - 1) / kTile, rows = std::max(a.n_rows, 1), beams = (rows + a.B - 1) / a.B;
   p.whole = rows / kSlots * kSlots;
@@ -711,9 +711,9 @@ static void launch_rows(const BeamArgs& p, unsigned grid, hipStream_t st) {
     hipLaunchKernelGGL((beam_rows_kernel<T, P, false>), dim3(grid), dim3(kBeamThreads), 0, st, p);
 }
 // A pool holds k columns and 64 more at least, and better the k and those that pass the first
-// bound in a tile, 1.1 k for small k, more for large: what has no room waits for a cut (this
-// kernel, us, smaller pool and larger: 5,632 rows of 33,024 bf16 columns, k = 50, 194 and 214, 56
-// 207 and 211, 64 231 and 217; 200 fp32 rows, 56 23.9 and 22.1, 110 31.6 and 28.0, 192 48.1 and 36.7).
+// bound in a tile, 1.1 k for small k, more for large: what has no room waits for a cut (both
+// kernels, us, smaller pool and larger: 5,632 rows of 33,024 bf16 columns, k = 50, 178 and 191, 56
+// 189 and 196, 64 204 and 201; 200 fp32 rows, 56 37 and 33, 110 47 and 43, 192 88 and 75).
 template <class T>
 static void launch_pool(const BeamArgs& p, unsigned grid, hipStream_t st) {
   if (p.a.k <= 56) launch_rows<T, 2>(p, grid, st);

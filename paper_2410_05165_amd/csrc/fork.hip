@@ -23,8 +23,10 @@ typedef unsigned long long u64;
 // Sums and minima of whole numbers: the order of the atomics changes nothing.  Launches of
 // their own for count, claim and decide (one workgroup), and write; one workgroup does it all
 // where there is little to do.  Bound by latency, chains of dependent loads: the ten beams of one
-// user 6.4 us, 1,000 rows of up to 257 pages 7.6 + 8.9 + 5.6 (counters of their own, cleared first,
-// and a scan of the pool by its pieces took four launches, 17 and 33 us).
+// user 6.4 us, 1,000 rows of up to 257 pages 7.7 + 9.0 + 5.7 (counters of their own, cleared first,
+// and a scan of the pool by its pieces took four launches, 17 and 33 us).  The scan in `decide`
+// grows with the pool, 8,192 pages a step, and not with what was touched: the call takes 21 us with
+// 20,000 pages, 28 with 60,000, 41 with 140,000, 245 with a million.
 constexpr int kForkThreads = 256, kForkOne = 1024;
 // What one workgroup takes by itself: rows, and entries of the tables and pages (us, one launch
 // and three: 10 rows of 6 entries 6.3 and 13.4, 100 of 40 13.1 and 15.8; but 320 of 13 20.7 and
