@@ -483,7 +483,7 @@ atspeed_status atspeed_page_fork(const atspeed_page_fork_args* args, void* works
   ST_TRY(check_fork(*args));
   ForkArgs p{};
   p.a = *args;
-  const int columns = (args->max_pages + kForkThreads - 1) / kForkThreads;
+  const int columns = (int)(((long long)args->max_pages + kForkThreads - 1) / kForkThreads);
   const long long count = (long long)columns * ((args->B + kRun - 1) / kRun);
   if (count > kMaxGroups) return fail(ATSPEED_E_SHAPE, "page fork: too many rows x pages");
   const size_t need = lay_out(p, nullptr);

@@ -232,3 +232,14 @@ def test_a_pool_of_nearly_two_to_the_31_pages():
         assert free[:8].tolist() == [50, 60, 70, 5, 8, 1 << 20, last - 64, last]
         assert int(shared.min()) == int(shared.max()) == 0
         del shared, free
+
+
+def test_a_table_of_nearly_two_to_the_31_pages():
+    """One row whose table is as wide as it may be: the pages behind what it keeps come back."""
+    most = (1 << 31) - 1
+    table = torch.empty((1, most), dtype=torch.int32, device=DEV)
+    table[0, :5] = ints([6, 3, 0, 5, 2])
+    shared, free, n_free = ints(np.zeros(9)), ints(np.full(9, -1)), ints([0])
+    f = atspeed_page_fork(ints([5]), ints([2]), table, free, n_free, shared, 1)
+    assert f.length.tolist() == [2] and f.refused.tolist() == [0] and table[0, :2].tolist() == [6, 3]
+    assert int(n_free) == 3 and free[:3].tolist() == [0, 2, 5] and not bool(shared.any())
